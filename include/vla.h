@@ -244,7 +244,7 @@ int vla_debug_bump_dependency(vla_ctx* ctx, int32_t stream, int32_t slot, int32_
 int vla_debug_guards(vla_ctx* ctx, int32_t fill, size_t* n_bad);
 
 /* ---- stand-alone operators on caller-owned DEVICE tensors --------------------------------------------------
- * Both run asynchronously on `stream` (a cudaStream_t; NULL = default stream). */
+ * All run asynchronously on `stream` (a cudaStream_t; NULL = default stream). */
 
 /* Fused attention, softmax(Q K^T / sqrt(hd)) V per head with grouped KV heads -- the attention of the VLM
  * decoder layers and of the action head (Section 2.1, Figure 1).  q [tq, hq*hd], k and v [tkv, hkv*hd],
@@ -281,12 +281,60 @@ int vla_op_attention_static(const void* q, const void* k, const void* v, void* o
 int vla_op_linear(const void* a, const void* w, float* out32, void* out16, int32_t m, int32_t n, int32_t k, int32_t act,
                   void* stream);
 
+/* Values to 8 bits (e4m3) with a scale for each block of block_rows x 128 (no counterpart in the paper, like the operators
+ * below: what a decoder layer of the caller's own needs around vla_op_linear and vla_op_attention).
+ *   scales[i / block_rows, j / 128] = max(largest |x| of the block / 448, 2^-126),  q[i,j] = e4m3(x[i,j] / scale)
+ * in fp32 divisions, rounded to nearest, ties to even.  An infinity or NaN makes its whole block NaN once it is scaled back.
+ * x [m,k] bf16 (x_f32 = 0) or fp32, rows ld elements apart; q [m,k] e4m3 without gaps; scales fp32 [ceil(m / block_rows),
+ * ceil(k / 128)].  block_rows: 1 (activations: a scale per row) or 128 (weights).  k a multiple of 16; x, q and x's rows
+ * 16-byte aligned.  All DEVICE, on the current device, like everything below; q and scales overlap no input. */
+int vla_op_quantize(const void* x, int32_t x_f32, int64_t ld, void* q, float* scales, int32_t m, int32_t k, int32_t block_rows,
+                    void* stream);
+
+/* Linear layer on 8-bit operands with block scales, y = act(A W^T) where A[i,j] = a[i,j] * scale_a[i, j / 128] and W[i,j] =
+ * w[i,j] * scale_w[i / 128, j / 128].  a [m,k] and w [n,k] e4m3 row-major, 16-byte aligned; scale_a fp32 [m, ceil(k/128)] and
+ * scale_w fp32 [ceil(n/128), ceil(k/128)] as vla_op_quantize writes them with block_rows 1 and 128; k a multiple of 16.  Products
+ * are exact, each block of 128 is summed by the tensor core in fp32, scaled, and added up in fp32.  out32, out16 and act as for vla_op_linear
+ * (GeLU and SiLU to fp32 precision). */
+int vla_op_linear_scaled(const void* a, const float* scale_a, const void* w, const float* scale_w, float* out32, void* out16,
+                         int32_t m, int32_t n, int32_t k, int32_t act, void* stream);
+
+/* Linear layers grouped by expert: rows offsets[e] <= i < offsets[e + 1] of a go through expert e's matrix, y[i] = act(a[i] W_e^T).
+ * a [t,k] bf16 with its rows sorted by expert, w [experts,n,k] bf16, offsets int32 [experts + 1] DEVICE (read by the kernel, so
+ * that a router's counts never visit the host); k a multiple of 8, a and w 16-byte aligned; experts <= 1024, experts * n < 2^31.
+ * Experts may have no rows.  Rows in front of offsets[0] and from offsets[experts] on are not written.  An offset below the one
+ * before it counts as that one, one above t as t and one below 0 as 0.  out32 (fp32 [t,n]) and/or out16, act as above. */
+int vla_op_linear_grouped(const void* a, const void* w, const int32_t* offsets, float* out32, void* out16, int32_t t, int32_t n,
+                          int32_t k, int32_t experts, int32_t act, void* stream);
+
+/* The same on 8-bit operands: a [t,k], w [experts,n,k] e4m3, scale_a fp32 [t, ceil(k/128)], scale_w fp32 [experts, ceil(n/128),
+ * ceil(k/128)] (an expert's blocks start at its first row); k a multiple of 16. */
+int vla_op_linear_grouped_scaled(const void* a, const float* scale_a, const void* w, const float* scale_w, const int32_t* offsets,
+                                 float* out32, void* out16, int32_t t, int32_t n, int32_t k, int32_t experts, int32_t act,
+                                 void* stream);
+
+/* RMS norm of every query and key head and its rotation by position, in one pass (between the projection and vla_op_attention):
+ * y = x / sqrt(mean(x^2) + eps) * gain over the hd values of a head, then of its first rot values the pairs (i, i + rot/2), or
+ * (2i, 2i+1) where interleaved, turned by pos * base^(-2i/rot).  fp32 inside, angles to 2^-26 turns at any position.
+ * q [t, hq*hd] and k [t, hkv*hd], bf16 or fp32 (in_f32), rows ld_q and ld_k elements apart (views of a stacked projection);
+ * out_q, out_k bf16, rows ld_out_q and ld_out_k apart (a cache's rows); all 16-byte aligned, rows too.  The outputs may be the
+ * inputs themselves (bf16, the same rows) and overlap them in no other way.  hkv = 0: queries alone, k and out_k NULL.
+ * gain_q, gain_k fp32 [hd], NULL: ones.  pos int32 [t] DEVICE, NULL: row i is at pos0 + i.  hd and rot multiples of 16, hd <= 256,
+ * rot <= hd (0: norm only); base > 1. */
+int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld_q, int64_t ld_k, void* out_q, void* out_k,
+                        int64_t ld_out_q, int64_t ld_out_k, int32_t t, int32_t hq, int32_t hkv, int32_t hd, const float* gain_q,
+                        const float* gain_k, float eps, const int32_t* pos, int32_t pos0, int32_t rot, float base,
+                        int32_t interleaved, void* stream);
+
 /* Every device-side wait of the operators is bounded (2 s by default); a wait that runs out makes the kernel set
  * the call's error word and return, leaving garbage in the output.  vla_op_status waits for `stream` to drain and
  * reads that word back: VLA_OK, or VLA_ERR_TIMEOUT when a wait ran out.  op selects the word: VLA_OP_LINEAR (one
  * word per device, shared by all vla_op_linear calls on it: query before another call reuses it), VLA_OP_ATTENTION
- * (the word at the start of `scratch`, DEVICE) or VLA_OP_ATTENTION_STATIC (the library's fixed array). */
-enum { VLA_OP_LINEAR = 0, VLA_OP_ATTENTION = 1, VLA_OP_ATTENTION_STATIC = 2 };
+ * (the word at the start of `scratch`, DEVICE), VLA_OP_ATTENTION_STATIC (the library's fixed array), or VLA_OP_LINEAR_SCALED,
+ * VLA_OP_LINEAR_GROUPED and VLA_OP_LINEAR_GROUPED_SCALED (a word per device each, as for VLA_OP_LINEAR; vla_op_quantize and
+ * vla_op_qk_norm_rope wait for nothing). */
+enum { VLA_OP_LINEAR = 0, VLA_OP_ATTENTION = 1, VLA_OP_ATTENTION_STATIC = 2, VLA_OP_LINEAR_SCALED = 3, VLA_OP_LINEAR_GROUPED = 4,
+       VLA_OP_LINEAR_GROUPED_SCALED = 5 };
 int vla_op_status(int32_t op, const void* scratch, void* stream);
 
 /* Test hook: while drop_operand_loads is non-zero the operators' TMA producers issue no loads, so their consumers

@@ -28,7 +28,8 @@ EXPORTS = ["vla_required_arena_bytes", "vla_init", "vla_load_weights", "vla_subm
            "vla_get_counters", "vla_set_class_tags", "vla_get_class_tags", "vla_policy_probe", "vla_policy_probe_ex", "vla_debug_bump_dependency", "vla_debug_guards", "vla_last_error",
            "vla_destroy", "vla_op_status", "vla_debug_op_fault", "vla_debug_tile_linear", "vla_debug_tile_addends", "vla_debug_tile_attention",
            "vla_op_attention_scratch_bytes", "vla_op_attention", "vla_op_linear",
-           "vla_op_attention_static_capacity", "vla_op_attention_static"]
+           "vla_op_attention_static_capacity", "vla_op_attention_static", "vla_op_quantize", "vla_op_linear_scaled",
+           "vla_op_linear_grouped", "vla_op_linear_grouped_scaled", "vla_op_qk_norm_rope"]
 
 
 class vla_model_desc(C.Structure):
@@ -109,6 +110,12 @@ def load_library() -> C.CDLL:
     lib.vla_op_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 4 + [C.c_void_p]
     lib.vla_op_attention_static_capacity.argtypes = [P(C.c_size_t)]
     lib.vla_op_attention_static.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 6 + [C.c_void_p]
+    lib.vla_op_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p] + [C.c_int32] * 3 + [C.c_void_p]
+    lib.vla_op_linear_scaled.argtypes = [C.c_void_p] * 6 + [C.c_int32] * 4 + [C.c_void_p]
+    lib.vla_op_linear_grouped.argtypes = [C.c_void_p] * 5 + [C.c_int32] * 5 + [C.c_void_p]
+    lib.vla_op_linear_grouped_scaled.argtypes = [C.c_void_p] * 7 + [C.c_int32] * 5 + [C.c_void_p]
+    lib.vla_op_qk_norm_rope.argtypes = ([C.c_void_p] * 2 + [C.c_int32] + [C.c_int64] * 2 + [C.c_void_p] * 2 + [C.c_int64] * 2 + [C.c_int32] * 4 +
+                                        [C.c_void_p] * 2 + [C.c_float, C.c_void_p] + [C.c_int32] * 2 + [C.c_float, C.c_int32, C.c_void_p])
     lib.vla_last_error.argtypes = [C.c_void_p]
     lib.vla_last_error.restype = C.c_char_p
     lib.vla_destroy.argtypes = [C.c_void_p]
@@ -390,7 +397,7 @@ class Engine:
 
 
 POLICIES = {"two_phase": 0, "class_order": 1, "round_robin": 2, "two_phase_g": 3, "two_phase_r": 4}
-OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC = 0, 1, 2
+OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED = range(6)
 
 
 def policy_probe(taus, pending, feasible, cta_count, u, rr_start=0, u_max=0, policy=0, grid=None, res=None):
@@ -473,6 +480,159 @@ def op_attention_static(q, k, v, out, hq, hkv, hd, causal=False, stream=None):
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_attention_static failed")
     return out
+
+
+def _refuse(name, why):
+    raise VlaError(VLA_ERR_INVALID, f"{name}: {why}")
+
+
+def _on_current_device(name, *tensors):
+    import torch
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.get_device() == torch.cuda.current_device()):
+            _refuse(name, "tensors have to be on the current CUDA device")
+
+
+def _new(stream, shape, dtype, like):
+    """A result: memory of the stream that writes it, so that it is not handed out again while that one still runs."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    import torch
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
+
+
+def op_quantize(x, block_rows=1, stream=None):
+    """x [m,k]: CUDA bf16 or fp32, rows may lie apart.  Returns (q [m,k] float8_e4m3fn, scales fp32 [ceil(m / block_rows), ceil(k / 128)]) with
+    x ~ q * scale of its block of block_rows x 128 (see vla_op_quantize); block_rows 1 (activations) or 128 (weights)."""
+    import torch
+    _on_current_device("op_quantize", x)
+    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32) or (x.shape[1] > 1 and x.stride(1) != 1):
+        _refuse("op_quantize", "x is a bf16 or fp32 matrix with rows in one piece")
+    m, k = x.shape
+    if m < 1 or k < 16 or k % 16 or block_rows not in (1, 128):
+        _refuse("op_quantize", "at least one row, k a multiple of 16, block_rows 1 or 128")
+    q = _new(stream, (m, k), torch.float8_e4m3fn, x)
+    s = _new(stream, (-(-m // block_rows), -(-k // 128)), torch.float32, x)
+    rc = (_lib or load_library()).vla_op_quantize(x.data_ptr(), int(x.dtype == torch.float32), x.stride(0) if m > 1 else k, q.data_ptr(), s.data_ptr(),
+                                                  m, k, block_rows, _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_quantize failed")
+    return q, s
+
+
+def _matrices(name, a, w, dtype, dims):
+    if a.dim() != 2 or w.dim() != dims or a.dtype != dtype or w.dtype != dtype or not (a.is_contiguous() and w.is_contiguous()) or a.shape[1] != w.shape[-1]:
+        _refuse(name, f"a [rows,k] and w [{'experts,' if dims == 3 else ''}n,k] are contiguous {dtype}")
+
+
+def _scales(name, sa, sw, a_shape, w_shape):
+    import torch
+    blocks = -(-w_shape[-1] // 128)
+    if (tuple(sa.shape) != (a_shape[0], blocks) or tuple(sw.shape) != tuple(w_shape[:-2]) + (-(-w_shape[-2] // 128), blocks) or
+            sa.dtype != torch.float32 or sw.dtype != torch.float32 or not (sa.is_contiguous() and sw.is_contiguous())):
+        _refuse(name, "scales are contiguous fp32, one for each row (of a) or 128 rows (of w) and 128 columns")
+
+
+def _outputs(name, a, n, out_bf16, out, stream):
+    import torch
+    dtype, shape = torch.bfloat16 if out_bf16 else torch.float32, (a.shape[0], n)
+    if out is None:
+        out = _new(stream, shape, dtype, a)
+    elif tuple(out.shape) != shape or out.dtype != dtype or not out.is_contiguous():
+        _refuse(name, "out is contiguous, [rows,n], fp32 or, with out_bf16, bf16")
+    return (out, None, out.data_ptr()) if out_bf16 else (out, out.data_ptr(), None)
+
+
+def op_linear_scaled(a, scale_a, w, scale_w, act=0, out_bf16=False, stream=None):
+    """a [m,k], w [n,k]: float8_e4m3fn with the scales ``op_quantize`` gives (block_rows 1 and 128).  Returns act(A W^T) of the scaled matrices as
+    fp32 (or bf16) [m,n]."""
+    import torch
+    _on_current_device("op_linear_scaled", a, scale_a, w, scale_w)
+    _matrices("op_linear_scaled", a, w, torch.float8_e4m3fn, 2)
+    _scales("op_linear_scaled", scale_a, scale_w, a.shape, w.shape)
+    m, k = a.shape
+    n = w.shape[0]
+    out, p32, p16 = _outputs("op_linear_scaled", a, n, out_bf16, None, stream)
+    rc = (_lib or load_library()).vla_op_linear_scaled(a.data_ptr(), scale_a.data_ptr(), w.data_ptr(), scale_w.data_ptr(), p32, p16, m, n, k, act,
+                                                       _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_linear_scaled failed")
+    return out
+
+
+def _offsets_ok(name, offsets, experts):
+    import torch
+    if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.shape[0] != experts + 1 or not offsets.is_contiguous():
+        _refuse(name, "offsets is contiguous int32, [experts + 1]")
+
+
+def op_linear_grouped(a, w, offsets, act=0, out_bf16=False, out=None, stream=None):
+    """a [t,k] bf16, rows sorted by expert; w [experts,n,k] bf16; offsets int32 [experts + 1] on the GPU: rows offsets[e] .. offsets[e + 1] go through
+    expert e.  Returns act(a W_e^T) as fp32 (or bf16) [t,n]; rows outside of all experts are left as they were in ``out`` (without one: undefined)."""
+    import torch
+    _on_current_device("op_linear_grouped", a, w, offsets, out)
+    _matrices("op_linear_grouped", a, w, torch.bfloat16, 3)
+    experts, n, k = w.shape
+    _offsets_ok("op_linear_grouped", offsets, experts)
+    out, p32, p16 = _outputs("op_linear_grouped", a, n, out_bf16, out, stream)
+    rc = (_lib or load_library()).vla_op_linear_grouped(a.data_ptr(), w.data_ptr(), offsets.data_ptr(), p32, p16, a.shape[0], n, k, experts, act,
+                                                        _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_linear_grouped failed")
+    return out
+
+
+def op_linear_grouped_scaled(a, scale_a, w, scale_w, offsets, act=0, out_bf16=False, out=None, stream=None):
+    """``op_linear_grouped`` on float8_e4m3fn operands: scale_a [t, ceil(k/128)], scale_w [experts, ceil(n/128), ceil(k/128)]."""
+    import torch
+    _on_current_device("op_linear_grouped_scaled", a, scale_a, w, scale_w, offsets, out)
+    _matrices("op_linear_grouped_scaled", a, w, torch.float8_e4m3fn, 3)
+    _scales("op_linear_grouped_scaled", scale_a, scale_w, a.shape, w.shape)
+    experts, n, k = w.shape
+    _offsets_ok("op_linear_grouped_scaled", offsets, experts)
+    out, p32, p16 = _outputs("op_linear_grouped_scaled", a, n, out_bf16, out, stream)
+    rc = (_lib or load_library()).vla_op_linear_grouped_scaled(a.data_ptr(), scale_a.data_ptr(), w.data_ptr(), scale_w.data_ptr(), offsets.data_ptr(), p32, p16,
+                                                               a.shape[0], n, k, experts, act, _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_linear_grouped_scaled failed")
+    return out
+
+
+def op_qk_norm_rope(q, k, hq, hkv, hd, gq=None, gk=None, eps=1e-6, pos=None, pos0=0, base=10000.0, rot=None, interleaved=False,
+                    out_q=None, out_k=None, stream=None):
+    """RMS norm of each head of q [t, hq*hd] and k [t, hkv*hd] (CUDA bf16 or fp32, rows may lie apart; k None with hkv 0) and the rotation of the
+    first ``rot`` values of each (None: all) by position: ``pos`` int32 [t], or pos0 + row.  gq, gk: fp32 gains [hd] or None.  Returns (out_q, out_k),
+    bf16, new ones without gaps where none are given (see vla_op_qk_norm_rope)."""
+    import torch
+    name = "op_qk_norm_rope"
+    if hq < 1 or hkv < 0 or hd < 1 or (k is None) != (hkv == 0):
+        _refuse(name, "at least one query head, and k where there are key heads")
+    _on_current_device(name, q, k, gq, gk, pos, out_q, out_k)
+    t = q.shape[0]
+    for x, heads in ((q, hq), (k, hkv)):
+        if x is not None and (x.dim() != 2 or tuple(x.shape) != (t, heads * hd) or x.dtype not in (torch.bfloat16, torch.float32) or x.dtype != q.dtype or x.stride(1) != 1):
+            _refuse(name, "q [t, hq*hd] and k [t, hkv*hd] are both bf16 or both fp32, with rows in one piece")
+    for x in (gq, gk):
+        if x is not None and (tuple(x.shape) != (hd,) or x.dtype != torch.float32 or not x.is_contiguous()):
+            _refuse(name, "gains are contiguous fp32, [hd]")
+    if pos is not None and (tuple(pos.shape) != (t,) or pos.dtype != torch.int32 or not pos.is_contiguous()):
+        _refuse(name, "pos is contiguous int32, [t]")
+    if out_q is None:
+        out_q = _new(stream, (t, hq * hd), torch.bfloat16, q)
+    if out_k is None and hkv:
+        out_k = _new(stream, (t, hkv * hd), torch.bfloat16, k)
+    for x, heads in ((out_q, hq), (out_k, hkv)):
+        if (x is None) != (heads == 0) or (x is not None and (tuple(x.shape) != (t, heads * hd) or x.dtype != torch.bfloat16 or x.stride(1) != 1)):
+            _refuse(name, "outputs are bf16, of the inputs' shapes, with rows in one piece")
+    ptr = lambda x: None if x is None else x.data_ptr()                               # noqa: E731
+    ld = lambda x, heads: 0 if x is None else x.stride(0) if t > 1 else heads * hd    # noqa: E731  (one row: its stride says nothing)
+    rc = (_lib or load_library()).vla_op_qk_norm_rope(ptr(q), ptr(k), int(q.dtype == torch.float32), ld(q, hq), ld(k, hkv), ptr(out_q), ptr(out_k),
+                                                      ld(out_q, hq), ld(out_k, hkv), t, hq, hkv, hd, ptr(gq), ptr(gk), eps, ptr(pos), pos0,
+                                                      hd if rot is None else rot, base, int(bool(interleaved)), _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_qk_norm_rope failed")
+    return out_q, out_k
 
 
 def op_status(op, scratch=None, stream=None) -> int:

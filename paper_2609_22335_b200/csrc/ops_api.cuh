@@ -31,15 +31,15 @@ inline OpEncodeFn op_encoder() {
   return fn;
 }
 
-// 2-D bf16 row-major tensor, 64-column boxes, 128-byte swizzle, zero fill outside.
-inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+// 2-D row-major tensor, bf16 (or, `width` 1, bytes), boxes of 128 bytes of a row, 128-byte swizzle, zero fill outside.
+inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int width = 2) {
   OpEncodeFn enc = op_encoder();
   if (!enc) return false;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  cuuint32_t box[2] = {(cuuint32_t)GEMM_BK, (cuuint32_t)box_rows};
+  cuuint64_t strides[1] = {(cuuint64_t)ld * width};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / width), (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+  return enc(out, width == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -71,7 +71,10 @@ __device__ __forceinline__ void op_let_next_start() { asm volatile("griddepcontr
 
 #include "op_attention.cuh"
 #include "op_linear.cuh"
+#include "op_linear_blocks.cuh"
 #include "op_linear_pair.cuh"
+#include "op_qk_rope.cuh"
+#include "op_quantize.cuh"
 
 namespace vla {
 
@@ -81,10 +84,12 @@ constexpr size_t OP_ATTN_HEADER = 256;   // error word + padding (behind it: roo
 // (in a fixed device array of the library).  The kernel clears the word itself before it waits for anything, so that a call
 // that was captured into a graph reports on its latest replay like any other.
 static __device__ __align__(256) unsigned g_op_linear_error[64];
+constexpr int OP_ERROR_WORDS = 16;             // words (64 bytes) between two operators' own
 struct OpDevice {
-  unsigned* error = nullptr;
+  unsigned* error = nullptr;                   // of vla_op_linear; the others that have one: error_of
   int sms = 0;
   OpRoom room = {};
+  unsigned* error_of(int op) const { return error + OP_ERROR_WORDS * (op == VLA_OP_LINEAR ? 0 : op - VLA_OP_LINEAR_SCALED + 1); }
 };
 // The occupancy query answers one CTA per SM for a kernel that allocates tensor memory, where the hardware runs two once the first has
 // allocated; so it is asked for a kernel that does not, with the shared memory of the operators' CTAs.  What it does not answer stays 0, and
@@ -114,6 +119,14 @@ inline bool op_look_up(int dev, OpDevice* d) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LINP_SMEM) != cudaSuccess) return false;
   for (auto* kernel : {vla_op_attention_kernel<1>, vla_op_attention_kernel<2>})
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) != cudaSuccess) return false;
+  for (auto* kernel : {blocks_kernel<true, false>(32), blocks_kernel<true, false>(128), blocks_kernel<true, false>(256), blocks_kernel<true, true>(32), blocks_kernel<true, true>(128),
+                       blocks_kernel<true, true>(256), blocks_kernel<false, true>(32), blocks_kernel<false, true>(128), blocks_kernel<false, true>(256)})
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BLK_SMEM) != cudaSuccess) return false;
+  // (the widest tiles' warpgroups pass registers on: what they ask for has to be what the block was launched with)
+  for (auto* kernel : {blocks_kernel<true, false>(256), blocks_kernel<true, true>(256), blocks_kernel<false, true>(256)}) {
+    cudaFuncAttributes fa;
+    if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs * BLK_THREADS < 128 * BLK_REGS_SERVICE + 256 * BLK_REGS_SUMS) return false;
+  }
   const bool asked = cudaFuncSetAttribute(vla_op_room_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) == cudaSuccess;
   for (int s = 1; s <= OPA_MAX_SPLIT && asked; ++s) { d->room.alone[s] = op_clusters(s, OPA_MAX_SMEM); d->room.two[s] = op_clusters(s, LIN_SMEM); }
   return true;
@@ -189,6 +202,40 @@ inline int op_attention_run(const void* q, const void* k, const void* v, void* o
   return op_launch(p.terms == 2 ? vla_op_attention_kernel<2> : vla_op_attention_kernel<1>, n_tiles * p.split, OPA_THREADS, p.smem, p.split, s, a, maps, p, static_cast<unsigned*>(scratch), op_fault());
 }
 
+// The linear layers of op_linear_blocks.cuh: experts = 0 for one matrix, `width` bytes an element (1 with scales, 2 without).
+template <bool F8, bool GROUPED>
+inline int op_linear_blocks_run(int op, const void* a, const float* sa, const void* w, const float* sw, const int* offsets, float* out32, void* out16,
+                                int rows, int n, int k, int experts, int act, cudaStream_t s) {
+  constexpr int width = F8 ? 1 : 2;
+  OpDevice dev;
+  if (!op_device(&dev)) return VLA_ERR_CUDA;
+  BlocksArgs g;
+  g.rows = rows; g.n = n; g.nkb = (k - 1) / (BLK_ROW / width) + 1; g.experts = experts;
+  const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, dev.sms);
+  if (p.tiles > INT32_MAX) return VLA_ERR_INVALID;
+  g.bm = p.bm; g.bn = p.bn; g.ks = p.ks; g.tiles_n = p.tiles_n; g.stages = p.stages; g.act = act;
+  g.sa_ld = g.nkb; g.sw_ld = g.nkb; g.sw_expert = ((n - 1) / 128 + 1) * g.nkb;
+  g.offsets = offsets; g.sa = sa; g.sw = sw;
+  g.out32 = out32; g.out16 = static_cast<unsigned short*>(out16);
+  g.vec = linear_vec(n, out32, out16);
+  g.err = dev.error_of(op);
+  OpMaps maps;
+  if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
+  const int grid = (int)(p.tiles < dev.sms ? p.tiles : dev.sms);
+  return op_launch(blocks_kernel<F8, GROUPED>(p.bn), grid, BLK_THREADS, BLK_SMEM, 1, s, g, maps, op_fault());
+}
+inline bool op_linear_blocks_ok(const void* a, const void* w, const float* out32, const void* out16, int rows, int n, int k, int step, int act) {
+  return a && w && (out32 || out16) && rows >= 1 && rows <= 1 << 30 && n >= 1 && n <= 1 << 30 && k >= step && k % step == 0 && act >= 0 && act <= 2 &&
+         ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(w)) & 15) == 0 && (reinterpret_cast<uintptr_t>(out32) & 3) == 0 &&
+         (reinterpret_cast<uintptr_t>(out16) & 1) == 0;
+}
+inline bool op_experts_ok(const int* offsets, int experts, int n) {
+  return offsets && experts >= 1 && experts <= BLK_MAX_EXPERTS && (int64_t)experts * n <= INT32_MAX && (reinterpret_cast<uintptr_t>(offsets) & 3) == 0;
+}
+inline bool op_scales_ok(const float* sa, const float* sw) {
+  return sa && sw && ((reinterpret_cast<uintptr_t>(sa) | reinterpret_cast<uintptr_t>(sw)) & 3) == 0;
+}
+
 }  // namespace vla
 
 extern "C" {
@@ -235,6 +282,87 @@ int vla_op_linear(const void* a, const void* w, float* out32, void* out16, int32
   const int grid = g.ks > 1 ? g.tiles * g.ks : (g.tiles < 2 * dev.sms ? g.tiles : 2 * dev.sms);
   const auto kernel = vec == 8 ? vla_op_linear_kernel<8> : (vec == 2 ? vla_op_linear_kernel<2> : vla_op_linear_kernel<1>);
   return op_launch(kernel, grid, LIN_THREADS, linear_smem(g), g.ks, static_cast<cudaStream_t>(stream), g, maps, op_fault());
+}
+
+int vla_op_linear_scaled(const void* a, const float* scale_a, const void* w, const float* scale_w, float* out32, void* out16,
+                         int32_t m, int32_t n, int32_t k, int32_t act, void* stream) {
+  using namespace vla;
+  if (!op_linear_blocks_ok(a, w, out32, out16, m, n, k, 16, act) || !op_scales_ok(scale_a, scale_w)) return VLA_ERR_INVALID;
+  return op_linear_blocks_run<true, false>(VLA_OP_LINEAR_SCALED, a, scale_a, w, scale_w, nullptr, out32, out16, m, n, k, 0, act, static_cast<cudaStream_t>(stream));
+}
+
+int vla_op_linear_grouped(const void* a, const void* w, const int32_t* offsets, float* out32, void* out16, int32_t t, int32_t n,
+                          int32_t k, int32_t experts, int32_t act, void* stream) {
+  using namespace vla;
+  if (!op_linear_blocks_ok(a, w, out32, out16, t, n, k, 8, act) || !op_experts_ok(offsets, experts, n)) return VLA_ERR_INVALID;
+  return op_linear_blocks_run<false, true>(VLA_OP_LINEAR_GROUPED, a, nullptr, w, nullptr, offsets, out32, out16, t, n, k, experts, act, static_cast<cudaStream_t>(stream));
+}
+
+int vla_op_linear_grouped_scaled(const void* a, const float* scale_a, const void* w, const float* scale_w, const int32_t* offsets,
+                                 float* out32, void* out16, int32_t t, int32_t n, int32_t k, int32_t experts, int32_t act,
+                                 void* stream) {
+  using namespace vla;
+  if (!op_linear_blocks_ok(a, w, out32, out16, t, n, k, 16, act) || !op_scales_ok(scale_a, scale_w) || !op_experts_ok(offsets, experts, n)) return VLA_ERR_INVALID;
+  return op_linear_blocks_run<true, true>(VLA_OP_LINEAR_GROUPED_SCALED, a, scale_a, w, scale_w, offsets, out32, out16, t, n, k, experts, act, static_cast<cudaStream_t>(stream));
+}
+
+int vla_op_quantize(const void* x, int32_t x_f32, int64_t ld, void* q, float* scales, int32_t m, int32_t k, int32_t block_rows,
+                    void* stream) {
+  using namespace vla;
+  const int width = x_f32 ? 4 : 2;
+  if (!x || !q || !scales || m < 1 || k < 16 || k % 16 || (block_rows != 1 && block_rows != QUANT_BLOCK)) return VLA_ERR_INVALID;
+  if (ld < k || ld * width % 16 || (reinterpret_cast<uintptr_t>(x) & 15) || (reinterpret_cast<uintptr_t>(q) & 15) || (reinterpret_cast<uintptr_t>(scales) & 3))
+    return VLA_ERR_INVALID;
+  OpDevice dev;
+  if (!op_device(&dev)) return VLA_ERR_CUDA;
+  QuantArgs g = {x, static_cast<unsigned char*>(q), scales, m, k, (k - 1) / QUANT_BLOCK + 1, ld};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (block_rows != 1) {
+    const int64_t blocks = ((int64_t)(m - 1) / QUANT_BLOCK + 1) * g.kb;
+    if (blocks > INT32_MAX) return VLA_ERR_INVALID;
+    return op_launch(x_f32 ? vla_op_quantize_squares_kernel<true> : vla_op_quantize_squares_kernel<false>, (int)blocks, QUANT_THREADS, 0, 1, s, g);
+  }
+  // Four blocks a turn keep enough loads in flight; a call too small to fill the chip that way takes them one by one.
+  const int64_t teams = QUANT_THREADS / 16, resident = (int64_t)dev.sms * 8;
+  const bool many = (int64_t)m * g.kb > 4 * teams * resident / 8;
+  const int64_t items = (int64_t)m * (many ? (g.kb + 3) / 4 : g.kb), want = (items + teams - 1) / teams;
+  const int grid = (int)(want < resident ? want : resident);
+  if (many) return op_launch(x_f32 ? vla_op_quantize_rows_kernel<true, 4> : vla_op_quantize_rows_kernel<false, 4>, grid, QUANT_THREADS, 0, 1, s, g);
+  return op_launch(x_f32 ? vla_op_quantize_rows_kernel<true, 1> : vla_op_quantize_rows_kernel<false, 1>, grid, QUANT_THREADS, 0, 1, s, g);
+}
+
+int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld_q, int64_t ld_k, void* out_q, void* out_k,
+                        int64_t ld_out_q, int64_t ld_out_k, int32_t t, int32_t hq, int32_t hkv, int32_t hd, const float* gain_q,
+                        const float* gain_k, float eps, const int32_t* pos, int32_t pos0, int32_t rot, float base,
+                        int32_t interleaved, void* stream) {
+  using namespace vla;
+  if (!q || !out_q || t < 1 || hq < 1 || hkv < 0 || hd < 16 || hd > 256 || hd % 16 || rot < 0 || rot > hd || rot % 16) return VLA_ERR_INVALID;
+  if (hq > 65536 || hkv > 65536 || (hkv > 0 && (!k || !out_k)) || !(eps >= 0.0f) || !(eps < 1e30f) || !(base > 1.0f) || !(base < 1e30f)) return VLA_ERR_INVALID;
+  const int width = in_f32 ? 4 : 2;
+  const auto bad = [](const void* p, int64_t ld, int64_t least, int w) { return ld < least || ld * w % 16 || (reinterpret_cast<uintptr_t>(p) & 15); };
+  if (bad(q, ld_q, (int64_t)hq * hd, width) || bad(out_q, ld_out_q, (int64_t)hq * hd, 2)) return VLA_ERR_INVALID;
+  if (hkv > 0 && (bad(k, ld_k, (int64_t)hkv * hd, width) || bad(out_k, ld_out_k, (int64_t)hkv * hd, 2))) return VLA_ERR_INVALID;
+  OpDevice dev;
+  if (!op_device(&dev)) return VLA_ERR_CUDA;
+  QkArgs g;
+  g.q = q; g.k = k; g.out_q = static_cast<unsigned short*>(out_q); g.out_k = static_cast<unsigned short*>(out_k);
+  g.gain_q = gain_q; g.gain_k = gain_k; g.pos = pos;
+  g.ld_q = ld_q; g.ld_k = ld_k; g.ld_oq = ld_out_q; g.ld_ok = ld_out_k;
+  g.t = t; g.hq = hq; g.heads = hq + hkv; g.hd = hd; g.rot = rot; g.pos0 = pos0; g.eps = eps; g.inv_hd = 1.0f / (float)hd;
+  if (rot > 0) {      // (80-bit numbers; a step's error of 2^-64 grows to 2^-57 over 128 pairs)
+    const long double step = exp2l(-2.0L / rot * log2l((long double)base));
+    long double f = 2935890503282001226.0L;      // 2^64 / (2 pi)
+    for (int i = 0; i < rot / 2; ++i, f *= step) g.freq[i] = (unsigned long long)(f + 0.5L);
+  }
+  for (g.lp = 0; (16 << g.lp) < hd; ++g.lp) {}
+  // A warp per token shares the sines over its heads; where that leaves SMs without work, heads side by side instead.
+  for (g.lh = 0; g.lp + g.lh < 5 && (1 << g.lh) < g.heads; ++g.lh) {}
+  while (g.lp + g.lh < 7 && (1 << g.lh) < g.heads && ((int64_t)t << (g.lp + g.lh)) < (int64_t)dev.sms * 1024) ++g.lh;
+  const int64_t blocks = (((int64_t)t << (g.lp + g.lh)) + QK_THREADS - 1) / QK_THREADS;
+  if (blocks > INT32_MAX) return VLA_ERR_INVALID;
+  const auto kernel = in_f32 ? (interleaved ? vla_op_qk_rope_kernel<true, true> : vla_op_qk_rope_kernel<true, false>)
+                             : (interleaved ? vla_op_qk_rope_kernel<false, true> : vla_op_qk_rope_kernel<false, false>);
+  return op_launch(kernel, (int)blocks, QK_THREADS, 0, 1, static_cast<cudaStream_t>(stream), g);
 }
 
 int vla_debug_op_fault(int32_t drop_operand_loads, uint64_t wait_limit_ns) {

@@ -910,9 +910,9 @@ int vla_op_attention_static(const void* q, const void* k, const void* v, void* o
 
 int vla_op_status(int32_t op, const void* scratch, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (op == VLA_OP_LINEAR) {
+  if (op == VLA_OP_LINEAR || op == VLA_OP_LINEAR_SCALED || op == VLA_OP_LINEAR_GROUPED || op == VLA_OP_LINEAR_GROUPED_SCALED) {
     vla::OpDevice d;
-    return vla::op_device(&d) ? vla::op_status_of(d.error, s) : VLA_ERR_CUDA;
+    return vla::op_device(&d) ? vla::op_status_of(d.error_of(op), s) : VLA_ERR_CUDA;
   }
   if (op == VLA_OP_ATTENTION) {
     if (!scratch) return VLA_ERR_INVALID;
