@@ -5,8 +5,8 @@
 
 namespace vla {
 
-constexpr int BLK_SMEM = 208 * 1024;          // operand stages: an SM's shared memory less what the kernel declares beside them
-constexpr int BLK_MAX_STAGES = 24;
+constexpr int BLK_SMEM = 192 * 1024;          // operand stages: an SM's shared memory less what the kernel declares beside them
+constexpr int BLK_MAX_STAGES = 12;
 constexpr int BLK_ROW = 128;                  // bytes of a k-block's row: 64 bf16 or 128 e4m3 numbers
 constexpr int BLK_MAX_EXPERTS = 1024;
 
@@ -16,8 +16,23 @@ struct BlocksPlan {
   long long tiles;             // all of them; with experts, whose rows only the GPU knows, the most there can be
 };
 
-inline int blocks_stages(int bm, int bn) {    // (the MMA always reads 128 rows from the start of a stage)
-  const int stage = (bm + bn) * BLK_ROW, tail = stage < 16384 ? 16384 - stage : 0, s = (BLK_SMEM - tail) / stage;
+// By the width that a tile's kernel is built for (64, 128 or 256): k-blocks of a stage and of a unit, and the units whose accumulators are in use at a time
+// (op_linear_blocks.cuh).  At least `stages` stages keep the kernel's barriers in step: those of all units in flight, and of two.
+template <int WIDTH, bool F8>
+struct BlocksShape {
+  static constexpr int kps = WIDTH == 256 ? 1 : 2, unit = F8 ? kps : 2, units = WIDTH == 64 ? 4 : 2;
+  static constexpr int stages = (units > 2 ? units : 2) * unit / kps;
+  static_assert(units * (F8 ? unit : 1) * WIDTH <= 512, "accumulators fit tensor memory");
+};
+inline int blocks_width(int bn) { return bn > 128 ? 256 : (bn > 64 ? 128 : 64); }
+inline int blocks_kps(int bn) { return blocks_width(bn) == 256 ? BlocksShape<256, true>::kps : (blocks_width(bn) == 128 ? BlocksShape<128, true>::kps : BlocksShape<64, true>::kps); }
+inline int blocks_least_stages(int bn, bool f8) {
+  if (blocks_width(bn) == 256) return f8 ? BlocksShape<256, true>::stages : BlocksShape<256, false>::stages;
+  if (blocks_width(bn) == 128) return f8 ? BlocksShape<128, true>::stages : BlocksShape<128, false>::stages;
+  return f8 ? BlocksShape<64, true>::stages : BlocksShape<64, false>::stages;
+}
+inline int blocks_stages(int bm, int bn) {    // (the MMA always reads 128 rows from the start of a k-block's operands)
+  const int block = (bm + bn) * BLK_ROW, tail = block < 16384 ? 16384 - block : 0, s = (BLK_SMEM - tail) / (block * blocks_kps(bn));
   return s > BLK_MAX_STAGES ? BLK_MAX_STAGES : s;
 }
 

@@ -1,0 +1,46 @@
+"""The tile plan of the linear layers on 8-bit operands and by expert (csrc/blocks_plan.h, compiled for the host): whatever the shape, the tiles
+cover the result, the stages fit, and there are as many as the kernel's barriers need to stay in step."""
+import ctypes as C
+import os
+import random
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    out = tmp_path_factory.mktemp("plan") / "libblocks_host.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-x", "c++", os.path.join(HERE, "blocks_plan_host_shim.cc"), "-o", str(out)], check=True)
+    lib = C.CDLL(str(out))
+
+    def call(rows, n, nkb, experts=0, sms=148):
+        o = (C.c_longlong * 10)()
+        lib.blocks_plan_host(rows, n, nkb, experts, sms, o)
+        return dict(zip(("bm", "bn", "ks", "tiles_n", "stages", "tiles", "kps", "least_f8", "least_bf16", "smem"), o))
+    return call
+
+
+def shapes():
+    rnd = random.Random(3)
+    out = [(r, n, nkb, e) for r in (1, 16, 17, 127, 128, 129, 300, 100000, 1 << 30) for n in (1, 7, 64, 257, 9500, 1 << 20) for nkb in (1, 2, 3, 65, 1000)
+           for e in (0, 1, 2, 64, 1024)]
+    return out + [(int(2 ** rnd.uniform(0, 15)), int(2 ** rnd.uniform(0, 15)), int(2 ** rnd.uniform(0, 8)), rnd.choice([0, 0, 1, 3, 8, 100])) for _ in range(3000)]
+
+
+def test_every_plan_is_one_the_kernel_can_run(plan):
+    for rows, n, nkb, e in shapes():
+        for sms in (148, 132, 7):
+            p = plan(rows, n, nkb, e, sms)
+            bm, bn, kps, stages = p["bm"], p["bn"], p["kps"], p["stages"]
+            assert 16 <= bm <= 128 and bm % 16 == 0 and bn in (32, 64, 128, 256), p
+            assert p["tiles_n"] * bn >= n > (p["tiles_n"] - 1) * bn
+            assert stages >= p["least_f8"] and stages >= p["least_bf16"], p
+            block = (bm + bn) * 128
+            assert stages * kps * block <= p["smem"] and (stages * kps - 1) * block + 16384 <= p["smem"]       # (the MMA reads 128 rows of any block)
+            if e == 0:
+                assert p["tiles"] == -(-rows // bm) * p["tiles_n"]
+            else:       # however the rows are spread: every full tile but the last of each expert's has bm rows
+                assert p["tiles"] >= (rows // bm + min(rows, e) - (1 if rows % bm == 0 else 0)) * p["tiles_n"]

@@ -244,6 +244,26 @@ def test_a_wait_that_runs_out_is_reported_and_a_captured_call_works_again():
         assert all(torch.equal(p, q) for p, q in zip(graphs[0][1], want))
 
 
+@pytest.mark.parametrize("m,n", [(1, 64), (128, 64), (128, 9500), (128, 19000), (300, 19000), (700, 12900)])
+def test_long_rows_of_k(m, n):
+    """Every ring of the kernels goes round many times, at every tile width: a k-block's hand-overs must not run into the next round's."""
+    import torch
+    from paper_2609_22335_b200 import api
+    k = 8208
+    a, sa = eight_bit(1, m, k, 1)
+    w, sw = eight_bit(128, n, k, 2)
+    got = api.op_linear_scaled(a, sa, w, sw)
+    assert api.op_status(api.OP_LINEAR_SCALED) == api.VLA_OK
+    near(got, scaled(a, sa, 1), scaled(w, sw, 128), 0, True)
+    offsets, _ = sort_of([m // 2, m - m // 2])
+    x = torch.randn(m, k, device="cuda", generator=gen(3)).to(torch.bfloat16)
+    y = (0.1 * torch.randn(2, n // 2, k, device="cuda", generator=gen(4))).to(torch.bfloat16)
+    got = api.op_linear_grouped(x, y, offsets)
+    assert api.op_status(api.OP_LINEAR_GROUPED) == api.VLA_OK
+    for e, (lo, hi) in enumerate([(0, m // 2), (m // 2, m)]):
+        near(got[lo:hi], x[lo:hi].double(), y[e].double(), 0, False)
+
+
 def test_results_do_not_depend_on_the_run():
     import torch
     from paper_2609_22335_b200 import api
