@@ -8,28 +8,31 @@
 // the scales and add it to the 32-bit sums that they keep in registers, while the next accumulator is filled.  (bf16 has no scales; its sums are
 // cut as well because the tensor core's additions truncate: the error grows with their number.)
 //
-// CTA: 384 threads.  Warp 0 issues TMA loads, warps 1 and 3 MMAs, warp 2 fetches scales, and the two warpgroups behind them hold the sums (a
-// quarter of the lanes and a half of the columns a warp, a row a lane); registers move from the first warpgroup to those two.  Tile: up
-// to 128 rows (MMA M) x up to 256 features (MMA N).  Persistent, one CTA per SM.
+// CTA: 384 threads.  Warp 0 issues TMA loads, warps 1 and 3 MMAs, warp 2 fetches scales, and the eight behind them hold the sums (a
+// quarter of the lanes and a half of the columns a warp, a row a lane); of the widest tiles, registers move from the first four to those.
+// Tile: up to 128 rows (MMA M) x up to 256 features (MMA N), or 256 x 256 for two CTAs.  Persistent, one CTA per SM.
 //
 // With experts a CTA reads the offsets first and lays the tiles out in shared memory: tiles of an expert follow each other, its row tiles fastest, so
 // that neighbours share weights.  A tile's rows end with its expert's; the rows behind, which the box loads all the same, are in lanes that nobody looks at.
 #pragma once
 #include "blocks_plan.h"
-#include "op_linear.cuh"
+#include "op_linear_pair.cuh"
 
 namespace vla {
 
 constexpr int BLK_THREADS = 384;
-constexpr int BLK_REGS_SERVICE = 56, BLK_REGS_SUMS = 224;      // 128 x 56 + 256 x 224 = 384 x 168
+constexpr int BLK_REGS_SERVICE = 72, BLK_REGS_SUMS = 216;      // 128 x 72 + 256 x 216 = 384 x 168
 constexpr int BLK_TMEM_COLS = 512;
-constexpr int BLK_SCALE_SLOTS = 8;            // stages whose scales have been asked for
-constexpr int BLK_SCALE_FLOATS = 132;         // of a k-block: 128 rows' and up to two of weights
+constexpr int BLK_SPAN = 4;                   // k-blocks whose scales go together: four floats of a row
+constexpr int BLK_SCALE_SLOTS = 4;            // spans whose scales have been asked for
+constexpr int BLK_SCALE_ROWS = 131;           // 128 rows and three blocks of weight rows
 
 struct BlocksArgs {
   int rows, n, nkb, experts;                  // experts: 0 for one matrix
-  int bm, bn, ks, tiles_n, stages, act, vec;
+  int bm, bn, tiles_n, stages, units, act;
+  int vec32, vec16;                           // elements that a lane's store may cover: 4 or 1; 8, 2 or 1
   int sa_ld, sw_ld, sw_expert;                // scales: k-blocks of a row; of a block of weight rows; of an expert
+  int sa_vec, sw_vec;                         // whether four of a row lie on a 16-byte boundary
   const int* offsets;
   const float *sa, *sw;
   float* out32;
@@ -37,12 +40,20 @@ struct BlocksArgs {
   unsigned* err;
 };
 
+template <bool PAIR>
 __device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate));
+  if (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate));
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate));
 }
 // Instruction descriptor: e4m3 x e4m3 -> fp32, both K-major.
 __device__ __forceinline__ uint32_t umma_idesc_e4m3(int n, int m = 128) {
@@ -53,9 +64,16 @@ __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.a
 template <int N>
 __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// Four bytes, or zeros, into shared memory behind the thread's back; scales_landed arrives at `bar` when all of the thread's have.
-__device__ __forceinline__ void scale_fetch(uint32_t dst, const float* src, bool have) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(have ? 4 : 0) : "memory");
+// The scales of a span, `have` of four floats (zeros behind them), into shared memory behind the thread's back; scales_landed arrives at `bar` when all
+// of the thread's have.
+__device__ __forceinline__ void scales_fetch(uint32_t dst, const float* src, int have, bool vec) {
+  if (vec) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(4 * have) : "memory");
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + 4u * j), "l"(src + (j < have ? j : 0)), "r"(j < have ? 4 : 0) : "memory");
+  }
 }
 __device__ __forceinline__ void scales_landed(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
@@ -102,7 +120,7 @@ struct BlockExperts {
   int tile[BLK_MAX_EXPERTS + 1];
 };
 // One warp: rows and tiles of all experts.  An offset below the one before it counts as that one.
-__device__ __forceinline__ void blocks_lay_out(const BlocksArgs& g, BlockExperts& x, int lane) {
+__device__ __forceinline__ void blocks_lay_out(const BlocksArgs& g, BlockExperts& x, int lane, int tile_rows) {
   int row = 0, tiles = 0;                     // of the experts before
   for (int e0 = 0; e0 <= g.experts; e0 += 32) {
     const int e = e0 + lane;
@@ -116,7 +134,7 @@ __device__ __forceinline__ void blocks_lay_out(const BlocksArgs& g, BlockExperts
     // tiles of expert e - 1, which ends here
     int before = __shfl_up_sync(0xffffffffu, r, 1);
     if (lane == 0) before = row;
-    int mine = e == 0 || e > g.experts ? 0 : (r - before + g.bm - 1) / g.bm * g.tiles_n;
+    int mine = e == 0 || e > g.experts ? 0 : (r - before + tile_rows - 1) / tile_rows * g.tiles_n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int below = __shfl_up_sync(0xffffffffu, mine, o);
@@ -129,11 +147,11 @@ __device__ __forceinline__ void blocks_lay_out(const BlocksArgs& g, BlockExperts
   }
 }
 template <bool GROUPED>
-__device__ __forceinline__ BlockTile blocks_tile(const BlocksArgs& g, const BlockExperts& x, int t) {
+__device__ __forceinline__ BlockTile blocks_tile(const BlocksArgs& g, const BlockExperts& x, int t, int tile_rows) {
   BlockTile b;
   if (!GROUPED) {
-    const int tiles_m = (g.rows + g.bm - 1) / g.bm;
-    b.expert = 0; b.row0 = t % tiles_m * g.bm; b.row_end = g.rows; b.n0 = t / tiles_m * g.bn;
+    const int tiles_m = (g.rows + tile_rows - 1) / tile_rows;
+    b.expert = 0; b.row0 = t % tiles_m * tile_rows; b.row_end = g.rows; b.n0 = t / tiles_m * g.bn;
     return b;
   }
   int lo = 0, hi = g.experts;                 // the last expert whose first tile is not behind t (empty ones begin where the next does)
@@ -141,140 +159,194 @@ __device__ __forceinline__ BlockTile blocks_tile(const BlocksArgs& g, const Bloc
     const int mid = (lo + hi) >> 1;
     if (x.tile[mid] <= t) lo = mid; else hi = mid;
   }
-  const int tiles_m = (x.row[lo + 1] - x.row[lo] + g.bm - 1) / g.bm, l = t - x.tile[lo];
-  b.expert = lo; b.row0 = x.row[lo] + l % tiles_m * g.bm; b.row_end = x.row[lo + 1]; b.n0 = l / tiles_m * g.bn;
+  const int tiles_m = (x.row[lo + 1] - x.row[lo] + tile_rows - 1) / tile_rows, l = t - x.tile[lo];
+  b.expert = lo; b.row0 = x.row[lo] + l % tiles_m * tile_rows; b.row_end = x.row[lo + 1]; b.n0 = l / tiles_m * g.bn;
   return b;
 }
 
-// 32 columns of a warp's 32 lanes: a lane has a row.  (Tensor memory gives 32x32b loads 128 bytes a cycle and quarter; 16x256b, whose quads
-// would have rows ready to store, takes twice the time, and the sums are read once per k-block but stored once per tile.)
-__device__ __forceinline__ void tmem_ld_row32(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr)
-      : "memory");
+// 16 columns of a warp's 32 lanes: a lane has a row.  (Tensor memory gives 32x32b loads 128 bytes a cycle and quarter; 16x256b, whose quads
+// would have rows ready to store, takes twice the time, and the sums are read once per k-block but stored once per tile.)  tmem_ld16_nowait asks
+// for them; the wait names them, so that nothing that uses them can be moved in front of it.
+__device__ __forceinline__ void tmem_ld16_landed(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
 }
 
-// Puts 64 bytes of each of the warp's 32 rows (four 16-byte pieces `w` a lane) in order, and calls put(row, piece, value) for pieces of rows
-// so that a quad has a row's four: 2 KB of shared memory, swizzled so that neither side has conflicts.
-template <typename F>
-__device__ __forceinline__ void rows_in_order(uint4* stage, const uint4* w, int lane, F put) {
+// A warp's finished values, COLS columns (32, 64 or 128) of its 32 rows from column f of the output's row `row0` on; rows below `live` and columns below
+// n_end exist.  They pass through the warp's 4 KB of shared memory, 128 bytes of each row at a time, so that eight lanes write a row's
+// whole 128-byte line (straight from a row a lane the same stores take 4200 cycles for a 128 x 256 tile in bf16).  Pieces of 16 bytes lie
+// where neither side has conflicts.
+template <int COLS, typename F>
+__device__ __forceinline__ void rows_in_order(char* stage, int lane, int live, F put) {       // COLS: bytes of a row, in pieces of 16
+  constexpr int PIECES = COLS / 16, ROWS = 32 / PIECES;
   __syncwarp();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) stage[lane * 4 + (j ^ ((lane >> 1) & 3))] = w[j];
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 8 * i + (lane >> 2), j = lane & 3;
-    put(row, j, stage[row * 4 + (j ^ ((row >> 1) & 3))]);
+  for (int i = 0; i < 32; i += ROWS) {
+    const int row = i + lane / PIECES, j = lane % PIECES;
+    const uint4 x = *reinterpret_cast<const uint4*>(stage + row * 128 + ((j ^ (row & 7)) << 4));
+    if (row < live) put(row, j, x);
   }
+  __syncwarp();
 }
-// 32 finished columns of the warp's rows, from column f of the output's row `row0` on; rows below `live` and columns below n_end exist.
-__device__ __forceinline__ void blocks_store(const BlocksArgs& g, const float* v, uint4* stage, int lane, int row0, int live, int f, int n_end) {
-  if (g.out16) {
-    uint4 w[4];
+template <int COLS>
+__device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*sum)[8], char* stage, int lane, int row0, int live, int f, int n_end) {
+  constexpr int GROUP = COLS < 64 ? COLS : 64;                        // columns at a time: 128 bytes of bf16 (64 where there are 32), or two halves in fp32
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
-    rows_in_order(stage, w, lane, [&](int row, int j, const uint4& x) {
-      const int at = f + 8 * j;
-      if (row >= live || at >= n_end) return;
-      unsigned short* p = g.out16 + (size_t)(row0 + row) * g.n + at;
-      if (g.vec == 8) {
-        *reinterpret_cast<uint4*>(p) = x;
-      } else {
-        const uint32_t y[4] = {x.x, x.y, x.z, x.w};
+  for (int p = 0; p < COLS; p += GROUP) {
+    if (f + p >= n_end) break;
+    float v[GROUP];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (g.vec == 2) {
-            if (at + 2 * e < n_end) *reinterpret_cast<uint32_t*>(p + 2 * e) = y[e];
+    for (int j = 0; j < GROUP / 2; ++j) {
+      const float2 x = unpack2(sum[(p + 2 * j) / 16][j % 8]);
+      v[2 * j] = x.x; v[2 * j + 1] = x.y;
+    }
+    if (g.act == ACT_GELU) {
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j) v[j] = gelu_exact_f(v[j]);
+    } else if (g.act == ACT_SILU) {
+      activate<ACT_SILU, GROUP>(v);
+    }
+    if (g.out16) {
+#pragma unroll
+      for (int j = 0; j < GROUP / 8; ++j)
+        *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
+            make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+      unsigned short* const out = g.out16 + (size_t)row0 * g.n + f + p;
+      const int cols = n_end - f - p;
+      if (g.vec16 == 8) {
+        rows_in_order<GROUP * 2>(stage, lane, live, [&](int row, int j, const uint4& x) {
+          if (8 * j < cols) *reinterpret_cast<uint4*>(out + (size_t)row * g.n + 8 * j) = x;
+        });
+      } else {                                 // a row at a time, a lane two neighbouring values or one
+        __syncwarp();
+        for (int row = 0; row < live; ++row) {
+          if (g.vec16 == 2) {
+            if (2 * lane < cols && 2 * lane < GROUP) *reinterpret_cast<uint32_t*>(out + (size_t)row * g.n + 2 * lane) = *reinterpret_cast<const uint32_t*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + 4 * (lane & 3));
           } else {
-            if (at + 2 * e < n_end) p[2 * e] = (unsigned short)y[e];
-            if (at + 2 * e + 1 < n_end) p[2 * e + 1] = (unsigned short)(y[e] >> 16);
+#pragma unroll
+            for (int c = lane; c < GROUP; c += 32)
+              if (c < cols) out[(size_t)row * g.n + c] = *reinterpret_cast<const unsigned short*>(stage + row * 128 + (((c >> 3) ^ (row & 7)) << 4) + 2 * (c & 7));
           }
         }
+        __syncwarp();
       }
-    });
-  }
-  if (g.out32) {
+    }
+    if (g.out32) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint4 w[4];
+      for (int q = 0; q < GROUP; q += 32) {
+        if (f + p + q >= n_end) break;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float* u = v + 16 * h + 4 * j;
-        w[j] = make_uint4(__float_as_uint(u[0]), __float_as_uint(u[1]), __float_as_uint(u[2]), __float_as_uint(u[3]));
-      }
-      rows_in_order(stage, w, lane, [&](int row, int j, const uint4& x) {
-        const int at = f + 16 * h + 4 * j;
-        if (row >= live || at >= n_end) return;
-        float* p = g.out32 + (size_t)(row0 + row) * g.n + at;
-        if (g.vec == 8) {
-          *reinterpret_cast<uint4*>(p) = x;
-        } else if (g.vec == 2) {
-          *reinterpret_cast<uint2*>(p) = make_uint2(x.x, x.y);
-          if (at + 2 < n_end) *reinterpret_cast<uint2*>(p + 2) = make_uint2(x.z, x.w);
+        for (int j = 0; j < 8; ++j)
+          *reinterpret_cast<float4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_float4(v[q + 4 * j], v[q + 4 * j + 1], v[q + 4 * j + 2], v[q + 4 * j + 3]);
+        float* const out = g.out32 + (size_t)row0 * g.n + f + p + q;
+        const int cols = n_end - f - p - q;
+        if (g.vec32 == 4) {
+          rows_in_order<128>(stage, lane, live, [&](int row, int j, const uint4& x) {
+            if (4 * j < cols) *reinterpret_cast<uint4*>(out + (size_t)row * g.n + 4 * j) = x;
+          });
         } else {
-          const uint32_t y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (at + e < n_end) p[e] = __uint_as_float(y[e]);
+          __syncwarp();
+          for (int row = 0; row < live; ++row)
+            if (lane < cols) out[(size_t)row * g.n + lane] = *reinterpret_cast<const float*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + 4 * (lane & 3));
+          __syncwarp();
         }
-      });
+      }
     }
   }
 }
 
-// F8: e4m3 with scales, else bf16.  NG: groups of 32 columns that a warp holds sums of (a tile is up to 64 NG wide).
+// What stands between two units is branches and barriers: a branch costs a warp that has its scheduler nearly to itself some 30 cycles, a look at a
+// barrier 61 (92 with a time to sleep).  So a wait looks once before it goes to sleep, arrivals are predicated, and loops over columns have no ends of their own.
+__device__ __forceinline__ bool blocks_wait(const TileCtx& c, uint32_t bar, uint32_t parity) {
+  uint32_t there;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.b32 %0, 1, 0, p;\n\t}"
+      : "=r"(there)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return there || mbar_wait(c, bar, parity);
+}
+__device__ __forceinline__ void arrive_if(bool who, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(who ? 1u : 0u) : "memory");
+}
+// Relaxed: what has to be over is the loads from tensor memory, which were waited for; a release at cluster scope waits for the rest of the memory, too.
+__device__ __forceinline__ void arrive_far_if(bool who, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t}" ::"r"(bar), "r"(who ? 1u : 0u) : "memory");
+}
+
+// The two warps of a quarter meet; true if both say so.
+__device__ __forceinline__ bool both_sets(int bar, bool mine) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(bar), "r"(mine ? 1u : 0u) : "memory");
+  return r != 0;
+}
+
+// F8: e4m3 with scales, else bf16.  WIDTH: 64, 128 or 256, the widest tile it takes.  PAIR: two CTAs (a cluster, an SM each) share a tile of 256 rows:
+// each stages its own rows and half of the weights and keeps its own rows' sums; the first one issues the MMAs for both.  A k-block then costs
+// an SM 32 KB from L2 where a tile of its own costs 48, and that path (47 bytes a cycle) is what bounds a batch.
 //
-// A stage holds kps k-blocks: every hand-over costs its waiter about 200 cycles, which the narrower tiles' k-blocks do not last.  The sums take
-// in a unit of one or two k-blocks at a time, in an accumulator each (e4m3: they have scales of their own) or together in one (bf16).
+// Between the tensor core and the sums a hand-over takes about 1100 cycles there and back (issue 60 a MMA, a commit that is seen 300 later, a look at
+// a barrier 100 to 200), so the work is dealt to two sets, each an MMA warp, 256 columns of tensor memory (two units) and four warps of sums.  Of the widest
+// tiles each set has half of the columns: the sets' loads from tensor memory and MMAs fall between each other's.  Of narrower ones each has every
+// other unit, and the sums of both meet at the tile's end.  A unit is one or two k-blocks, in an accumulator each (e4m3: they have scales of
+// their own) or together in one (bf16); a stage holds kps k-blocks.
 //
-// Barriers: full[s] -- stage s holds its operands; done[s] -- the MMAs that read it are complete: the stage is free, and where it is its unit's last the
-// accumulators are full (one commit says both: a commit costs the issuing thread 150 cycles); freed[u] -- the sums have taken unit u in; landed[i],
-// taken[i] -- slot i holds a stage's scales, has been read.
-// Whoever waits for a phase has to know that the one before is over and that the one after cannot be before it looks.  done[s]: the phase
-// after belongs to a unit that needs this one's accumulators back, as long as there are at least as many stages as units in flight have.
-// full[s]: an MMA warp looks up to two units ahead of what it knows to have landed, so there have to be two units' stages.  BlocksShape has both.
-template <bool F8, bool GROUPED, int NG>
+// Barriers: full[s] -- stage s holds its operands; done[s] -- the MMAs that read it are complete (of the widest tiles, one of each set's): the stage is free,
+// and where it is its unit's last the accumulators are full; freed[h][u] -- set h's sums have taken its unit u in; landed[i], taken[i] -- slot i
+// holds a span's scales, has been read.  Of a pair, full and freed are the first CTA's, done is signalled in both.
+// Whoever waits for a phase has to know that the one before is over and that the one after cannot be before it looks.  done: the phase after is that of
+// the unit a ring of stages later; it is the same set's (that ring is even where units are dealt) and needs the accumulators of this unit back, as long as
+// there are the stages of the units in flight.  full: an MMA warp has seen every stage of its units, so also the one a ring before.
+template <bool F8, bool GROUPED, int WIDTH, bool PAIR>
 __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(const __grid_constant__ BlocksArgs g, const __grid_constant__ OpMaps maps,
                                                                               OpFault fault) {
-  typedef BlocksShape<64 * NG, F8> Shape;
-  constexpr int KPS = Shape::kps, UNIT = Shape::unit, SPU = UNIT / KPS, UNITS = Shape::units;         // k-blocks of a stage and a unit, stages of a unit
-  constexpr int PER_UNIT = F8 ? UNIT : 1, ACC_COLS = 64 * NG;                                         // accumulators of a unit
+  typedef BlocksShape<WIDTH, F8, PAIR> Shape;
+  constexpr bool HALVES = WIDTH == 256;                               // the sets share a tile's columns, else its units
+  constexpr int KPS = Shape::kps, UNIT = Shape::unit, SPU = UNIT / KPS, UNITS = Shape::units;         // k-blocks of a stage and a unit, stages of a unit, units of a set at most
+  constexpr int ACC_COLS = HALVES ? 128 : WIDTH, PER_UNIT = F8 ? UNIT : 1;                            // an accumulator's columns, accumulators of a unit
+  constexpr int GROUPS = ACC_COLS / 16, OWN = HALVES ? GROUPS : GROUPS / 2;                          // groups of 16 columns that a warp holds sums of, and that it finishes
   constexpr int KB = F8 ? 128 : 64;                                   // elements of a k-block
-  constexpr int N_BARS = 2 * BLK_MAX_STAGES + UNITS + 2 * BLK_SCALE_SLOTS;
-  static_assert(UNITS * PER_UNIT * ACC_COLS <= BLK_TMEM_COLS, "accumulators");
+  constexpr int DONE = HALVES ? 2 : 1, N_BARS = (1 + DONE) * BLK_MAX_STAGES + 2 * UNITS + 2 * BLK_SCALE_SLOTS;
+  static_assert(HALVES || SPU == 1, "units are dealt by stages");
   extern __shared__ __align__(1024) char smem_raw[];
   __shared__ uint32_t tmem_base_s;
   __shared__ __align__(8) uint64_t bars[N_BARS];
-  __shared__ __align__(16) float scales_s[F8 ? BLK_SCALE_SLOTS * KPS * BLK_SCALE_FLOATS : 1];
-  __shared__ __align__(16) uint4 rows_s[8][128];
+  __shared__ __align__(16) float4 scales_s[F8 ? BLK_SCALE_SLOTS * BLK_SCALE_ROWS : 1];
   __shared__ unsigned failed_s;
   __shared__ __align__(8) char experts_s[GROUPED ? sizeof(BlockExperts) : 8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = g.stages;
-  const uint32_t full0 = smem_u32(bars), done0 = full0 + 8u * BLK_MAX_STAGES, freed0 = done0 + 8u * BLK_MAX_STAGES;
-  const uint32_t landed0 = freed0 + 8u * UNITS, taken0 = landed0 + 8u * BLK_SCALE_SLOTS;
-  const uint32_t a_bytes = (uint32_t)(g.bm * BLK_ROW), kb_bytes = (uint32_t)((g.bm + g.bn) * BLK_ROW), stage_bytes = KPS * kb_bytes, stage0 = smem_u32(smem_raw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = g.stages, rank = PAIR ? (int)blockIdx.x & 1 : 0;
+  const int first = PAIR ? (int)blockIdx.x >> 1 : (int)blockIdx.x, step = PAIR ? (int)gridDim.x >> 1 : (int)gridDim.x;
+  const uint32_t full0 = smem_u32(bars), done0 = full0 + 8u * BLK_MAX_STAGES, freed0 = done0 + 8u * DONE * BLK_MAX_STAGES;
+  const uint32_t landed0 = freed0 + 8u * 2 * UNITS, taken0 = landed0 + 8u * BLK_SCALE_SLOTS;
+  const uint32_t units = WIDTH == 64 ? (uint32_t)g.units : UNITS;
+  const int w_rows = PAIR ? 128 : g.bn;                               // weight rows that this CTA stages
+  const uint32_t a_bytes = (uint32_t)(g.bm * BLK_ROW), kb_bytes = (uint32_t)((g.bm + w_rows) * BLK_ROW), stage_bytes = KPS * kb_bytes, stage0 = smem_u32(smem_raw);
   BlockExperts& experts = *reinterpret_cast<BlockExperts*>(experts_s);
   if (warp == 0) {
     for (int i = lane; i < N_BARS; i += 32) {
-      const int j = i - 2 * BLK_MAX_STAGES, l = j - UNITS;            // (freed and taken: a warp's arrival each; landed: a lane's each)
-      mbar_init(full0 + 8u * i, j < 0 ? 1 : (l < 0 ? 8 : (l < BLK_SCALE_SLOTS ? 32 : 8)));
+      const int j = i - (1 + DONE) * BLK_MAX_STAGES, l = j - 2 * UNITS;              // (freed: a set's warps; taken: all warps; landed: a lane's arrival each)
+      mbar_init(full0 + 8u * i, j < 0 ? 1 : (l < 0 ? (PAIR ? 8 : 4) : (l < BLK_SCALE_SLOTS ? 32 : 8)));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (lane == 0) failed_s = 0;
   } else if (warp == 1) {
-    tmem_alloc(&tmem_base_s, BLK_TMEM_COLS);
+    if (PAIR) tmem_alloc_pair(&tmem_base_s, BLK_TMEM_COLS);
+    else tmem_alloc(&tmem_base_s, BLK_TMEM_COLS);
+  }
+  if (PAIR) {
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                            // both CTAs' barriers and tensor memory are there
+    tc_fence_after();
   }
   op_wait_previous(maps, 2);
   if (threadIdx.x == 0 && blockIdx.x == 0) *g.err = 0u;
-  if (GROUPED && warp == 2) blocks_lay_out(g, experts, lane);
+  if (GROUPED && warp == 2) blocks_lay_out(g, experts, lane, PAIR ? 2 * g.bm : g.bm);
   TileCtx c;                                   // (what the bounded waits look at)
   c.error = &failed_s;
   c.deadline = gtimer() + fault.wait_limit_ns;
@@ -283,94 +355,110 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   op_let_next_start();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
-  const int tiles = GROUPED ? experts.tile[g.experts] : ((g.rows + g.bm - 1) / g.bm) * g.tiles_n, nkb = g.nkb;
+  const int tile_rows = PAIR ? 2 * g.bm : g.bm;
+  const int tiles = GROUPED ? experts.tile[g.experts] : ((g.rows + tile_rows - 1) / tile_rows) * g.tiles_n, nkb = g.nkb;
   bool ok = true;
   if (warp < 4) {
-    if (NG == 4) regs_dec<BLK_REGS_SERVICE>();
+    if (ACC_COLS == 128) regs_dec<BLK_REGS_SERVICE>();
     if (warp == 0) {
       uint32_t s = 0, ph = 1u;
-      for (int t = fault.drop_loads ? tiles : (int)blockIdx.x; t < tiles && ok; t += (int)gridDim.x) {
-        const BlockTile b = blocks_tile<GROUPED>(g, experts, t);
-        const int wrow = b.expert * g.n + b.n0;
+      const uint32_t full_first = PAIR ? cluster_addr(full0, 0u) : full0;
+      const int n_right = PAIR ? (g.bn - 128) / 2 : 0;                // a CTA's weight rows of the right half
+      for (int t = fault.drop_loads ? tiles : first; t < tiles && ok; t += step) {
+        const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
+        const int wrow = b.expert * g.n + b.n0, arow = b.row0 + rank * g.bm;
 #pragma unroll 1
         for (int kb = 0; kb < nkb; kb += KPS) {
-          const uint32_t full = full0 + 8u * s, dst = stage0 + s * stage_bytes;
-          if (!(ok = mbar_wait(c, done0 + 8u * s, ph))) break;
+          const uint32_t full = full_first + 8u * s, dst = stage0 + s * stage_bytes;
+          ok = blocks_wait(c, done0 + 8u * s, ph) && (!HALVES || blocks_wait(c, done0 + 8u * (BLK_MAX_STAGES + s), ph));
+          if (!ok) break;
           if (elect_one()) {
-            mbar_expect_tx(full, (KPS == 1 || kb + 1 < nkb ? KPS : 1) * kb_bytes);
+            if (rank == 0) mbar_expect_tx(full0 + 8u * s, (PAIR ? 2 : 1) * (KPS == 1 || kb + 1 < nkb ? KPS : 1) * kb_bytes);
 #pragma unroll
             for (int j = 0; j < KPS; ++j)
               if (j == 0 || kb + j < nkb) {
-                tma_load_2d(dst + j * kb_bytes + a_bytes, &maps.m[0], full, (kb + j) * KB, wrow);
-                tma_load_2d(dst + j * kb_bytes, &maps.m[1], full, (kb + j) * KB, b.row0);
+                const uint32_t to = dst + j * kb_bytes;
+                if (PAIR) {                    // of each half of the columns, this CTA's half
+                  tma_load_2d_pair(to + a_bytes, &maps.m[0], full, (kb + j) * KB, wrow + rank * 64);
+                  tma_load_2d_pair(to + a_bytes + 64 * BLK_ROW, &maps.m[0], full, (kb + j) * KB, wrow + 128 + rank * n_right);
+                  tma_load_2d_pair(to, &maps.m[1], full, (kb + j) * KB, arow);
+                } else {
+                  tma_load_2d(to + a_bytes, &maps.m[0], full, (kb + j) * KB, wrow);
+                  tma_load_2d(to, &maps.m[1], full, (kb + j) * KB, arow);
+                }
               }
           }
           __syncwarp();
           if (++s == (uint32_t)S) { s = 0; ph ^= 1u; }
         }
       }
+      if (PAIR)                                // every commit that the other CTA sends has come before this one ends
+        for (int i = 0; i < S && ok; ++i) {
+          ok = mbar_wait(c, done0 + 8u * s, ph) && mbar_wait(c, done0 + 8u * (BLK_MAX_STAGES + s), ph);
+          if (++s == (uint32_t)S) { s = 0; ph ^= 1u; }
+        }
     } else if (warp != 2) {
-      // two warps issue, a unit each in turn: a k-block costs its issuing thread more than half of the 512 cycles that the tensor core
-      // needs for the widest one, and more than all it needs for the others
-      const uint32_t idesc = F8 ? umma_idesc_e4m3(g.bn) : umma_idesc_bf16(g.bn);
-      const uint64_t desc0 = umma_desc_sw128(stage0);
-      uint32_t s = 0, ph = 0u, unit = 0, uph = 1u;
-      int turn = warp == 1 ? 0 : 1;                                   // units until this warp's next one
-      for (int t = (int)blockIdx.x; t < tiles && ok; t += (int)gridDim.x) {
+      const int h = warp == 1 ? 0 : 1, n = HALVES ? (h ? g.bn - 128 : 128) : g.bn;                    // the set, its MMAs' columns
+      if (rank == 0) {
+        const uint32_t idesc = F8 ? umma_idesc_e4m3(n, PAIR ? 256 : 128) : umma_idesc_bf16(n, PAIR ? 256 : 128);
+        const uint64_t desc0 = umma_desc_sw128(stage0);
+        const uint32_t to_w = (a_bytes + (HALVES && h ? (PAIR ? 64u : 128u) * BLK_ROW : 0u)) >> 4, my_done = done0 + (HALVES ? 8u * BLK_MAX_STAGES * (uint32_t)h : 0u);
+        const uint32_t my_freed = freed0 + 8u * UNITS * (uint32_t)h, my_acc = tmem + 256u * (uint32_t)h;
+        uint32_t s = HALVES ? 0u : (uint32_t)h, ph = 0u, unit = 0, uph = 1u;       // (where units are dealt, a set's are in every other stage)
+        int dealt = h;                                                // k-block units of the tile before this set's first one
+        for (int t = first; t < tiles && ok; t += step) {
 #pragma unroll 1
-        for (int kb = 0; kb < nkb && ok; kb += UNIT) {
-          if (turn == 0) {
-            const uint32_t acc = tmem + ACC_COLS * PER_UNIT * unit;
-            if (!(ok = mbar_wait(c, freed0 + 8u * unit, uph))) break;
-#pragma unroll 1
-            for (int i = 0; i < SPU && kb + i * KPS < nkb; ++i) {
-              if (!(ok = mbar_wait(c, full0 + 8u * s, ph))) break;
+          for (int kb = HALVES ? 0 : dealt * UNIT; kb < nkb; kb += HALVES ? UNIT : 2 * UNIT) {
+            const uint32_t acc = my_acc + ACC_COLS * PER_UNIT * unit;
+#pragma unroll
+            for (int i = 0; i < SPU; ++i) {
+              if (i > 0 && kb + i * KPS >= nkb) break;
+              if (!(ok = blocks_wait(c, full0 + 8u * s, ph))) break;
+              if (i == 0 && !(ok = blocks_wait(c, my_freed + 8u * unit, uph))) break;
               tc_fence_after();
+              const bool second = KPS > 1 && kb + 1 < nkb;
               if (elect_one()) {
+                const uint64_t ad = desc0 + ((s * stage_bytes) >> 4), wd = ad + to_w;
 #pragma unroll
                 for (int j = 0; j < KPS; ++j) {
-                  if (j > 0 && kb + i * KPS + j >= nkb) break;
-                  const uint64_t ad = desc0 + ((s * stage_bytes + j * kb_bytes) >> 4), wd = ad + (a_bytes >> 4);
+                  if (j > 0 && !second) break;
 #pragma unroll
                   for (int k = 0; k < 4; ++k) {                       // 32 bytes of K at a time
-                    if (F8) umma_e4m3(acc + ACC_COLS * j, ad + 2u * k, wd + 2u * k, idesc, k != 0 ? 1u : 0u);
-                    else umma_bf16(acc, ad + 2u * k, wd + 2u * k, idesc, (i | j | k) != 0 ? 1u : 0u);
+                    const uint64_t at = (uint64_t)((uint32_t)j * (kb_bytes >> 4) + 2u * k);
+                    if (F8) umma_e4m3<PAIR>(acc + ACC_COLS * j, ad + at, wd + at, idesc, k != 0 ? 1u : 0u);
+                    else if (PAIR) umma_bf16_pair(acc, ad + at, wd + at, idesc, (i | j | k) != 0 ? 1u : 0u);
+                    else umma_bf16(acc, ad + at, wd + at, idesc, (i | j | k) != 0 ? 1u : 0u);
                   }
                 }
-                umma_commit(done0 + 8u * s);
+                if (PAIR) umma_commit_pair(my_done + 8u * s);
+                else umma_commit(my_done + 8u * s);
               }
               __syncwarp();
-              if (++s == (uint32_t)S) { s = 0; ph ^= 1u; }
+              s += HALVES ? 1u : 2u;
+              if (s >= (uint32_t)S) { s -= (uint32_t)S; ph ^= 1u; }
             }
-          } else {
-            s += (uint32_t)min(SPU, (nkb - kb + KPS - 1) / KPS);
-            if (s >= (uint32_t)S) { s -= (uint32_t)S; ph ^= 1u; }
+            if (!ok) break;
+            if (++unit == units) { unit = 0; uph ^= 1u; }
           }
-          turn ^= 1;
-          if (++unit == UNITS) { unit = 0; uph ^= 1u; }
+          if (!HALVES) dealt ^= ((nkb + UNIT - 1) / UNIT) & 1;
         }
       }
     } else if (F8) {
       uint32_t slot = 0, ph = 1u;
-      for (int t = (int)blockIdx.x; t < tiles && ok; t += (int)gridDim.x) {
-        const BlockTile b = blocks_tile<GROUPED>(g, experts, t);
-        const int live = min(g.bm, b.row_end - b.row0);
-        const float* sa = g.sa + (size_t)(b.row0 + min(lane, live - 1)) * g.sa_ld;
-        const float* sw = g.sw + (size_t)b.expert * g.sw_expert + (size_t)min(b.n0 / 128 + (lane & 1), (g.n - 1) / 128) * g.sw_ld;
+      for (int t = first; t < tiles && ok; t += step) {
+        const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
+        const int arow = b.row0 + rank * g.bm, live = min(g.bm, b.row_end - arow);                    // (a pair's second CTA may have no rows)
+        const float* sa = g.sa + (size_t)(live > 0 ? arow : 0) * g.sa_ld;
+        const float* sw = g.sw + (size_t)b.expert * g.sw_expert + (size_t)min(b.n0 / 128 + min(lane, 2), (g.n - 1) / 128) * g.sw_ld;
 #pragma unroll 1
-        for (int kb = 0; kb < nkb; kb += KPS) {
+        for (int kb = 0; kb < nkb; kb += BLK_SPAN) {
           if (!(ok = mbar_wait(c, taken0 + 8u * slot, ph))) break;
           __syncwarp();
-          const uint32_t dst = smem_u32(scales_s) + slot * (KPS * BLK_SCALE_FLOATS * 4u) + 4u * (uint32_t)lane;
-#pragma unroll
-          for (int j = 0; j < KPS; ++j) {
-            if (j > 0 && kb + j >= nkb) break;
-            const uint32_t to = dst + j * (BLK_SCALE_FLOATS * 4u);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (32 * r < live) scale_fetch(to + 128u * r, sa + (lane + 32 * r < live ? (size_t)(32 * r) * g.sa_ld : 0) + kb + j, lane + 32 * r < live);
-            if (lane < 2) scale_fetch(to + 512u, sw + kb + j, true);
-          }
+          const uint32_t dst = smem_u32(scales_s) + 16u * (slot * BLK_SCALE_ROWS + (uint32_t)lane);
+          const int have = min(BLK_SPAN, nkb - kb);
+#pragma unroll 1
+          for (int r = lane; r < live; r += 32) scales_fetch(dst + 16u * (uint32_t)(r - lane), sa + (size_t)r * g.sa_ld + kb, have, g.sa_vec != 0);
+          if (lane < 3) scales_fetch(dst + 16u * 128u, sw + kb, have, g.sw_vec != 0);
           scales_landed(landed0 + 8u * slot);
           if (++slot == BLK_SCALE_SLOTS) { slot = 0; ph ^= 1u; }
         }
@@ -379,95 +467,125 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
     }
     if (!ok && warp != 2) for (int i = 0; i < 100; ++i) __nanosleep(1000);       // gave up: copies and MMAs in flight end before the CTA does
   } else {
-    if (NG == 4) regs_inc<BLK_REGS_SUMS>();
-    const int quarter = warp & 3, half = warp >= 8 ? 1 : 0, groups = g.bn / 32, mine = groups < 2 * NG ? (half ? groups / 2 : (groups + 1) / 2) : NG;
-    const int c0 = half ? (groups + 1) / 2 : 0;                       // this warp's columns: groups [c0, c0 + mine)
-    const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + 32u * (uint32_t)c0;
-    const float* const my_scale = scales_s + 32 * quarter + lane;
-    uint32_t unit = 0, s = 0, ph = 0u, slot = 0, lph = 0u;
-    for (int t = (int)blockIdx.x; t < tiles && ok; t += (int)gridDim.x) {
-      const BlockTile b = blocks_tile<GROUPED>(g, experts, t);
-      const int row0 = b.row0 + 32 * quarter, live = min(g.bm, b.row_end - b.row0) - 32 * quarter;      // rows of this warp
-      f32x2 sum[NG][16];
+    if (ACC_COLS == 128) regs_inc<BLK_REGS_SUMS>();
+    const int quarter = warp & 3, h = (warp >> 2) - 1, col0 = HALVES ? 128 * h : 0;          // this set's first column
+    const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + 256u * (uint32_t)h, my_done = done0 + (HALVES ? 8u * BLK_MAX_STAGES * (uint32_t)h : 0u);
+    const uint32_t my_freed = (PAIR ? cluster_addr(freed0, 0u) : freed0) + 8u * UNITS * (uint32_t)h;
+    const bool speaks = lane == 0;
+    uint32_t unit = 0, s = HALVES ? 0u : (uint32_t)h, ph = 0u, slot = 0, lph = 0u;
+    int dealt = h;
+    for (int t = first; t < tiles && ok; t += step) {
+      const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
+      const int arow = b.row0 + rank * g.bm, row0 = arow + 32 * quarter, live = min(32, min(g.bm, b.row_end - arow) - 32 * quarter);          // rows of this warp
+      // The weights' scale changes every 128 of their rows: from group `turn` on it is that of the next block.
+      const int w0 = b.n0 % 128 + col0, turn = 8 - w0 % 128 / 16;
+      const float* const scales = reinterpret_cast<const float*>(scales_s);
+      const int at_row = 4 * (32 * quarter + lane), at_w = 4 * (128 + w0 / 128), at_next = 4 * (128 + min(w0 / 128 + 1, 2));
+      f32x2 sum[GROUPS][8];
 #pragma unroll
-      for (int c1 = 0; c1 < NG; ++c1)
+      for (int c1 = 0; c1 < GROUPS; ++c1)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum[c1][j] = 0ull;
+        for (int j = 0; j < 8; ++j) sum[c1][j] = 0ull;
 #pragma unroll 1
-      for (int kb = 0; kb < nkb; kb += UNIT) {
-        float f[KPS];
-        if (F8) {
-          if (!(ok = mbar_wait(c, landed0 + 8u * slot, lph))) break;
-#pragma unroll
-          for (int j = 0; j < KPS; ++j) {
-            const int at = ((int)slot * KPS + j) * BLK_SCALE_FLOATS;
-            f[j] = my_scale[at] * scales_s[at + 128 + (NG == 4 ? half : 0)];
-          }
-        }
-        if (SPU > 1 && kb + KPS < nkb && ++s == (uint32_t)S) { s = 0; ph ^= 1u; }      // (the unit's last stage)
-        if (!(ok = mbar_wait(c, done0 + 8u * s, ph))) break;
-        if (++s == (uint32_t)S) { s = 0; ph ^= 1u; }
-        __syncwarp();
-        tc_fence_after();
-        if (live > 0 && mine > 0) {
+      for (int kb0 = 0; kb0 < nkb; kb0 += BLK_SPAN) {
+        const float* const sc = scales + slot * (4 * BLK_SCALE_ROWS);
+        if (F8 && !(ok = blocks_wait(c, landed0 + 8u * slot, lph))) break;
+#pragma unroll 1
+        for (int kb = kb0 + (HALVES ? 0 : dealt * UNIT); kb < min(kb0 + BLK_SPAN, nkb); kb += HALVES ? UNIT : 2 * UNIT) {
+          float f[PER_UNIT], f_next[PER_UNIT];                        // the row's scale times the weights', in front of `turn` and behind it
 #pragma unroll
           for (int j = 0; j < PER_UNIT; ++j) {
-            if (j > 0 && kb + j >= nkb) break;
-            const uint32_t acc = from + ACC_COLS * (PER_UNIT * unit + j);
-            const f32x2 fj = F8 ? pack2(__float_as_uint(f[j % KPS]), __float_as_uint(f[j % KPS])) : 0;
-            uint32_t v[NG > 1 ? 2 : 1][32];
-            tmem_ld_row32(acc, v[0]);
+            const int u = kb - kb0 + j;
+            f[j] = F8 ? sc[at_row + u] * sc[at_w + u] : 1.0f;
+            f_next[j] = F8 ? sc[at_row + u] * sc[at_next + u] : 1.0f;
+          }
+          if (SPU > 1 && kb + KPS < nkb && ++s == (uint32_t)S) { s = 0; ph ^= 1u; }    // (the unit's last stage)
+          if (!(ok = blocks_wait(c, my_done + 8u * s, ph))) break;
+          __syncwarp();
+          tc_fence_after();
+          if (live > 0) {
 #pragma unroll
-            for (int c1 = 0; c1 < NG; ++c1) {
-              if (c1 >= mine) break;
-              tmem_ld_wait();
-              if (c1 + 1 < NG && c1 + 1 < mine) tmem_ld_row32(acc + 32u * (c1 + 1), v[(c1 + 1) & 1]);
+            for (int j = 0; j < PER_UNIT; ++j) {
+              if (j > 0 && kb + j >= nkb) break;
+              const uint32_t acc = from + ACC_COLS * (PER_UNIT * unit + j);
+              uint32_t v[2][16];
+              tmem_ld16_nowait(acc, v[0]);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const f32x2 p = pack2(v[c1 & 1][2 * i], v[c1 & 1][2 * i + 1]);
-                sum[c1][i] = F8 ? fma2(p, fj, sum[c1][i]) : add2(p, sum[c1][i]);
+              for (int c1 = 0; c1 < GROUPS; ++c1) {                   // the next columns are on their way while these are added (those behind the tile's width for nothing)
+                uint32_t* const w = v[c1 & 1];
+                tmem_ld16_landed(w);
+                if (c1 + 1 < GROUPS) tmem_ld16_nowait(acc + 16u * (c1 + 1), v[(c1 + 1) & 1]);
+                const uint32_t fc = __float_as_uint(c1 < turn ? f[j] : f_next[j]);
+                const f32x2 fj = pack2(fc, fc);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  const f32x2 x = pack2(w[2 * i], w[2 * i + 1]);
+                  sum[c1][i] = F8 ? fma2(x, fj, sum[c1][i]) : add2(x, sum[c1][i]);
+                }
               }
             }
           }
+          tc_fence_before();
+          __syncwarp();
+          if (PAIR && rank != 0) arrive_far_if(speaks, my_freed + 8u * unit);
+          else arrive_if(speaks, freed0 + 8u * (UNITS * (uint32_t)h + unit));
+          if (++unit == units) unit = 0;
+          s += HALVES ? 1u : 2u;
+          if (s >= (uint32_t)S) { s -= (uint32_t)S; ph ^= 1u; }
         }
-        tc_fence_before();
-        arrive_warp(freed0 + 8u * unit, lane);
+        if (!ok) break;
         if (F8) {
-          arrive_warp(taken0 + 8u * slot, lane);
+          __syncwarp();
+          arrive_if(speaks, taken0 + 8u * slot);
           if (++slot == BLK_SCALE_SLOTS) { slot = 0; lph ^= 1u; }
         }
-        if (++unit == UNITS) unit = 0;
       }
+      if (!HALVES) dealt ^= ((nkb + UNIT - 1) / UNIT) & 1;
+      if (!HALVES) ok = both_sets(1 + quarter, ok);                   // (from here on the two warps of a quarter go together, or leave together)
       if (!ok || live <= 0) continue;
+      char* const stage = smem_raw + BLK_SMEM + 4096 * (warp - 4);      // this warp's rows on their way out, or its sums on their way to the other set
+      if (!HALVES) {
+        // The sets' sums meet: each finishes its half of the columns and gives the other one the rest, through its own 4 KB.
+        float* const mine_out = reinterpret_cast<float*>(stage) + lane;
+        const float* const theirs = reinterpret_cast<const float*>(smem_raw + BLK_SMEM + 4096 * ((warp - 4) ^ 4)) + lane;
 #pragma unroll
-      for (int c1 = 0; c1 < NG; ++c1) {
-        if (c1 >= mine) break;
-        float v[32];
+        for (int c1 = 0; c1 < OWN; c1 += 2) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float2 p = unpack2(sum[c1][j]);
-          v[2 * j] = p.x; v[2 * j + 1] = p.y;
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float2 x = unpack2(h ? sum[c1 + e][j] : sum[OWN + c1 + e][j]);
+              mine_out[512 * e + 64 * j] = x.x; mine_out[512 * e + 64 * j + 32] = x.y;
+            }
+          both_sets(1 + quarter, true);
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              sum[c1 + e][j] = add2(h ? sum[OWN + c1 + e][j] : sum[c1 + e][j], pack2(__float_as_uint(theirs[512 * e + 64 * j]), __float_as_uint(theirs[512 * e + 64 * j + 32])));
+          both_sets(1 + quarter, true);
         }
-        if (g.act == ACT_GELU) {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = gelu_exact_f(v[j]);
-        } else if (g.act == ACT_SILU) {
-          activate<ACT_SILU, 32>(v);
-        }
-        blocks_store(g, v, rows_s[warp - 4], lane, row0, live, b.n0 + 32 * (c0 + c1), min(g.n, b.n0 + g.bn));
       }
+      blocks_store<OWN * 16>(g, sum, stage, lane, row0, live, b.n0 + (HALVES ? col0 : OWN * 16 * h), min(g.n, b.n0 + g.bn));
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 1) tmem_dealloc(tmem, BLK_TMEM_COLS);
+  if (PAIR) {
+    cluster_sync();                            // nobody reads or signals the other CTA any more
+    if (warp == 1) tmem_dealloc_pair(tmem, BLK_TMEM_COLS);
+  } else if (warp == 1) {
+    tmem_dealloc(tmem, BLK_TMEM_COLS);
+  }
   if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(&failed_s) != 0u) *g.err = (unsigned)DEV_ERR_WAIT_MBAR;
+  if (PAIR) cluster_sync();                    // (both have given their columns back)
 }
 
 typedef void (*BlocksKernel)(const BlocksArgs, const OpMaps, OpFault);
 template <bool F8, bool GROUPED>
-inline BlocksKernel blocks_kernel(int bn) {   // for tiles of that width
-  return bn > 128 ? vla_op_linear_blocks_kernel<F8, GROUPED, 4> : (bn > 64 ? vla_op_linear_blocks_kernel<F8, GROUPED, 2> : vla_op_linear_blocks_kernel<F8, GROUPED, 1>);
+inline BlocksKernel blocks_kernel(int bn, bool pair) {                // for tiles of that width
+  if (pair) return vla_op_linear_blocks_kernel<F8, GROUPED, 256, true>;
+  return bn > 128 ? vla_op_linear_blocks_kernel<F8, GROUPED, 256, false> : (bn > 64 ? vla_op_linear_blocks_kernel<F8, GROUPED, 128, false> : vla_op_linear_blocks_kernel<F8, GROUPED, 64, false>);
 }
 
 }  // namespace vla

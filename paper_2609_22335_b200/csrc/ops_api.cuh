@@ -119,13 +119,12 @@ inline bool op_look_up(int dev, OpDevice* d) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LINP_SMEM) != cudaSuccess) return false;
   for (auto* kernel : {vla_op_attention_kernel<1>, vla_op_attention_kernel<2>})
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) != cudaSuccess) return false;
-  for (auto* kernel : {blocks_kernel<true, false>(32), blocks_kernel<true, false>(128), blocks_kernel<true, false>(256), blocks_kernel<true, true>(32), blocks_kernel<true, true>(128),
-                       blocks_kernel<true, true>(256), blocks_kernel<false, true>(32), blocks_kernel<false, true>(128), blocks_kernel<false, true>(256)})
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BLK_SMEM) != cudaSuccess) return false;
-  // (the widest tiles' warpgroups pass registers on: what they ask for has to be what the block was launched with)
-  for (auto* kernel : {blocks_kernel<true, false>(256), blocks_kernel<true, true>(256), blocks_kernel<false, true>(256)}) {
-    cudaFuncAttributes fa;
-    if (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs * BLK_THREADS < 128 * BLK_REGS_SERVICE + 256 * BLK_REGS_SUMS) return false;
+  for (int width : {64, 128, 256, 512}) {     // (512: a pair's; of all but the narrowest the warpgroups pass registers on, and what they ask for has to be there)
+    for (auto* kernel : {blocks_kernel<true, false>(width, width > 256), blocks_kernel<true, true>(width, width > 256), blocks_kernel<false, true>(width, width > 256)}) {
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BLK_SMEM_ALL) != cudaSuccess) return false;
+      cudaFuncAttributes fa;
+      if (width > 64 && (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs * BLK_THREADS < 128 * BLK_REGS_SERVICE + 256 * BLK_REGS_SUMS)) return false;
+    }
   }
   const bool asked = cudaFuncSetAttribute(vla_op_room_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) == cudaSuccess;
   for (int s = 1; s <= OPA_MAX_SPLIT && asked; ++s) { d->room.alone[s] = op_clusters(s, OPA_MAX_SMEM); d->room.two[s] = op_clusters(s, LIN_SMEM); }
@@ -211,18 +210,21 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   if (!op_device(&dev)) return VLA_ERR_CUDA;
   BlocksArgs g;
   g.rows = rows; g.n = n; g.nkb = (k - 1) / (BLK_ROW / width) + 1; g.experts = experts;
-  const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, dev.sms);
+  const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, F8, dev.sms);
   if (p.tiles > INT32_MAX) return VLA_ERR_INVALID;
-  g.bm = p.bm; g.bn = p.bn; g.ks = p.ks; g.tiles_n = p.tiles_n; g.stages = p.stages; g.act = act;
+  g.bm = p.bm; g.bn = p.bn; g.tiles_n = p.tiles_n; g.stages = p.stages; g.units = p.units; g.act = act;
   g.sa_ld = g.nkb; g.sw_ld = g.nkb; g.sw_expert = ((n - 1) / 128 + 1) * g.nkb;
   g.offsets = offsets; g.sa = sa; g.sw = sw;
+  g.sa_vec = g.nkb % 4 == 0 && (reinterpret_cast<uintptr_t>(sa) & 15) == 0;
+  g.sw_vec = g.nkb % 4 == 0 && (reinterpret_cast<uintptr_t>(sw) & 15) == 0;
   g.out32 = out32; g.out16 = static_cast<unsigned short*>(out16);
-  g.vec = linear_vec(n, out32, out16);
+  g.vec32 = n % 4 == 0 && (reinterpret_cast<uintptr_t>(out32) & 15) == 0 ? 4 : 1;
+  g.vec16 = n % 8 == 0 && (reinterpret_cast<uintptr_t>(out16) & 15) == 0 ? 8 : (n % 2 == 0 && (reinterpret_cast<uintptr_t>(out16) & 3) == 0 ? 2 : 1);
   g.err = dev.error_of(op);
   OpMaps maps;
-  if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
-  const int grid = (int)(p.tiles < dev.sms ? p.tiles : dev.sms);
-  return op_launch(blocks_kernel<F8, GROUPED>(p.bn), grid, BLK_THREADS, BLK_SMEM, 1, s, g, maps, op_fault());
+  if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.pair ? 64 : p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
+  const int ctas = p.pair ? 2 : 1, room = dev.sms / ctas, grid = ctas * (int)(p.tiles < room ? p.tiles : room);
+  return op_launch(blocks_kernel<F8, GROUPED>(p.bn, p.pair != 0), grid, BLK_THREADS, BLK_SMEM_ALL, ctas, s, g, maps, op_fault());
 }
 inline bool op_linear_blocks_ok(const void* a, const void* w, const float* out32, const void* out16, int rows, int n, int k, int step, int act) {
   return a && w && (out32 || out16) && rows >= 1 && rows <= 1 << 30 && n >= 1 && n <= 1 << 30 && k >= step && k % step == 0 && act >= 0 && act <= 2 &&

@@ -16,10 +16,10 @@ def plan(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-x", "c++", os.path.join(HERE, "blocks_plan_host_shim.cc"), "-o", str(out)], check=True)
     lib = C.CDLL(str(out))
 
-    def call(rows, n, nkb, experts=0, sms=148):
-        o = (C.c_longlong * 10)()
-        lib.blocks_plan_host(rows, n, nkb, experts, sms, o)
-        return dict(zip(("bm", "bn", "ks", "tiles_n", "stages", "tiles", "kps", "least_f8", "least_bf16", "smem"), o))
+    def call(rows, n, nkb, experts=0, f8=True, sms=148):
+        o = (C.c_longlong * 12)()
+        lib.blocks_plan_host(rows, n, nkb, experts, int(f8), sms, o)
+        return dict(zip(("bm", "bn", "pair", "tiles_n", "stages", "tiles", "kps", "unit_stages", "smem", "turns", "units", "most_units"), o))
     return call
 
 
@@ -32,15 +32,19 @@ def shapes():
 
 def test_every_plan_is_one_the_kernel_can_run(plan):
     for rows, n, nkb, e in shapes():
-        for sms in (148, 132, 7):
-            p = plan(rows, n, nkb, e, sms)
-            bm, bn, kps, stages = p["bm"], p["bn"], p["kps"], p["stages"]
-            assert 16 <= bm <= 128 and bm % 16 == 0 and bn in (32, 64, 128, 256), p
+        for sms, f8 in ((148, True), (148, False), (132, True), (7, False)):
+            if not f8 and e == 0:
+                continue
+            p = plan(rows, n, nkb, e, f8, sms)
+            bm, bn, kps, stages, pair = p["bm"], p["bn"], p["kps"], p["stages"], p["pair"]
+            assert 16 <= bm <= 128 and bm % 16 == 0 and 16 <= bn <= 256 and bn % 16 == 0 and (not pair or bn % 32 == 0 and bn > 128), p
             assert p["tiles_n"] * bn >= n > (p["tiles_n"] - 1) * bn
-            assert stages >= p["least_f8"] and stages >= p["least_bf16"], p
-            block = (bm + bn) * 128
+            assert 1 <= p["units"] <= p["most_units"] and p["units"] * p["unit_stages"] <= stages <= 12 and not (p["turns"] and stages % 2), p
+            assert p["units"] == 2 or bn <= 64, p                    # (the wider tiles' kernels count on two)
+            block = (bm + (128 if pair else bn)) * 128
             assert stages * kps * block <= p["smem"] and (stages * kps - 1) * block + 16384 <= p["smem"]       # (the MMA reads 128 rows of any block)
+            tile = bm * (2 if pair else 1)
             if e == 0:
-                assert p["tiles"] == -(-rows // bm) * p["tiles_n"]
-            else:       # however the rows are spread: every full tile but the last of each expert's has bm rows
-                assert p["tiles"] >= (rows // bm + min(rows, e) - (1 if rows % bm == 0 else 0)) * p["tiles_n"]
+                assert p["tiles"] == -(-rows // tile) * p["tiles_n"]
+            else:       # however the rows are spread over the experts
+                assert p["tiles"] >= (rows // tile + min(rows, e) - (1 if rows % tile == 0 else 0)) * p["tiles_n"]
