@@ -23,8 +23,6 @@ namespace vla {
 constexpr int BLK_THREADS = 384;
 constexpr int BLK_REGS_SERVICE = 72, BLK_REGS_SUMS = 216;      // 128 x 72 + 256 x 216 = 384 x 168
 constexpr int BLK_TMEM_COLS = 512;
-constexpr int BLK_SPAN = 4;                   // k-blocks whose scales go together: four floats of a row
-constexpr int BLK_SCALE_SLOTS = 4;            // spans whose scales have been asked for
 constexpr int BLK_SCALE_ROWS = 131;           // 128 rows and three blocks of weight rows
 
 struct BlocksArgs {
@@ -179,15 +177,20 @@ __device__ __forceinline__ void tmem_ld16_landed(uint32_t* r) {
 // n_end exist.  They pass through the warp's 4 KB of shared memory, 128 bytes of each row at a time, so that eight lanes write a row's
 // whole 128-byte line (straight from a row a lane the same stores take 4200 cycles for a 128 x 256 tile in bf16).  Pieces of 16 bytes lie
 // where neither side has conflicts.
-template <int COLS, typename F>
-__device__ __forceinline__ void rows_in_order(char* stage, int lane, int live, F put) {       // COLS: bytes of a row, in pieces of 16
-  constexpr int PIECES = COLS / 16, ROWS = 32 / PIECES;
+template <int BYTES>                              // of a row
+__device__ __forceinline__ void rows_in_order(const char* stage, int lane, int live, int left, void* out, size_t pitch) {       // left: bytes of a row that exist
+  constexpr int PIECES = BYTES / 16, ROWS = 32 / PIECES;
+  const int row0 = lane / PIECES, j = lane % PIECES;
+  char* p = static_cast<char*>(out) + (size_t)row0 * pitch + 16 * j;
   __syncwarp();
+  if (live == 32 && left >= BYTES) {
 #pragma unroll
-  for (int i = 0; i < 32; i += ROWS) {
-    const int row = i + lane / PIECES, j = lane % PIECES;
-    const uint4 x = *reinterpret_cast<const uint4*>(stage + row * 128 + ((j ^ (row & 7)) << 4));
-    if (row < live) put(row, j, x);
+    for (int i = 0; i < 32; i += ROWS, p += ROWS * pitch)
+      *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(stage + (row0 + i) * 128 + ((j ^ ((row0 + i) & 7)) << 4));
+  } else {
+#pragma unroll 1
+    for (int row = row0; row < live; row += ROWS, p += ROWS * pitch)
+      if (16 * j < left) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(stage + row * 128 + ((j ^ (row & 7)) << 4));
   }
   __syncwarp();
 }
@@ -217,9 +220,7 @@ __device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*
       unsigned short* const out = g.out16 + (size_t)row0 * g.n + f + p;
       const int cols = n_end - f - p;
       if (g.vec16 == 8) {
-        rows_in_order<GROUP * 2>(stage, lane, live, [&](int row, int j, const uint4& x) {
-          if (8 * j < cols) *reinterpret_cast<uint4*>(out + (size_t)row * g.n + 8 * j) = x;
-        });
+        rows_in_order<GROUP * 2>(stage, lane, live, 2 * cols, out, 2 * (size_t)g.n);
       } else {                                 // a row at a time, a lane two neighbouring values or one
         __syncwarp();
         for (int row = 0; row < live; ++row) {
@@ -244,9 +245,7 @@ __device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*
         float* const out = g.out32 + (size_t)row0 * g.n + f + p + q;
         const int cols = n_end - f - p - q;
         if (g.vec32 == 4) {
-          rows_in_order<128>(stage, lane, live, [&](int row, int j, const uint4& x) {
-            if (4 * j < cols) *reinterpret_cast<uint4*>(out + (size_t)row * g.n + 4 * j) = x;
-          });
+          rows_in_order<128>(stage, lane, live, 4 * cols, out, 4 * (size_t)g.n);
         } else {
           __syncwarp();
           for (int row = 0; row < live; ++row)
@@ -311,18 +310,19 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   constexpr int ACC_COLS = HALVES ? 128 : WIDTH, PER_UNIT = F8 ? UNIT : 1;                            // an accumulator's columns, accumulators of a unit
   constexpr int GROUPS = ACC_COLS / 16, OWN = HALVES ? GROUPS : GROUPS / 2;                          // groups of 16 columns that a warp holds sums of, and that it finishes
   constexpr int KB = F8 ? 128 : 64;                                   // elements of a k-block
-  constexpr int DONE = HALVES ? 2 : 1, N_BARS = (1 + DONE) * BLK_MAX_STAGES + 2 * UNITS + 2 * BLK_SCALE_SLOTS;
+  constexpr int SPAN = HALVES ? 8 : 4, SLOTS = HALVES ? 2 : 4;        // k-blocks whose scales go together, and the spans of them that have been asked for
+  constexpr int DONE = HALVES ? 2 : 1, N_BARS = (1 + DONE) * BLK_MAX_STAGES + 2 * UNITS + 2 * SLOTS;
   static_assert(HALVES || SPU == 1, "units are dealt by stages");
   extern __shared__ __align__(1024) char smem_raw[];
   __shared__ uint32_t tmem_base_s;
   __shared__ __align__(8) uint64_t bars[N_BARS];
-  __shared__ __align__(16) float4 scales_s[F8 ? BLK_SCALE_SLOTS * BLK_SCALE_ROWS : 1];
+  __shared__ __align__(16) float4 scales_s[F8 ? SLOTS * SPAN / 4 * BLK_SCALE_ROWS : 1];
   __shared__ unsigned failed_s;
   __shared__ __align__(8) char experts_s[GROUPED ? sizeof(BlockExperts) : 8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = g.stages, rank = PAIR ? (int)blockIdx.x & 1 : 0;
   const int first = PAIR ? (int)blockIdx.x >> 1 : (int)blockIdx.x, step = PAIR ? (int)gridDim.x >> 1 : (int)gridDim.x;
   const uint32_t full0 = smem_u32(bars), done0 = full0 + 8u * BLK_MAX_STAGES, freed0 = done0 + 8u * DONE * BLK_MAX_STAGES;
-  const uint32_t landed0 = freed0 + 8u * 2 * UNITS, taken0 = landed0 + 8u * BLK_SCALE_SLOTS;
+  const uint32_t landed0 = freed0 + 8u * 2 * UNITS, taken0 = landed0 + 8u * SLOTS;
   const uint32_t units = WIDTH == 64 ? (uint32_t)g.units : UNITS;
   const int w_rows = PAIR ? 128 : g.bn;                               // weight rows that this CTA stages
   const uint32_t a_bytes = (uint32_t)(g.bm * BLK_ROW), kb_bytes = (uint32_t)((g.bm + w_rows) * BLK_ROW), stage_bytes = KPS * kb_bytes, stage0 = smem_u32(smem_raw);
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   if (warp == 0) {
     for (int i = lane; i < N_BARS; i += 32) {
       const int j = i - (1 + DONE) * BLK_MAX_STAGES, l = j - 2 * UNITS;              // (freed: a set's warps; taken: all warps; landed: a lane's arrival each)
-      mbar_init(full0 + 8u * i, j < 0 ? 1 : (l < 0 ? (PAIR ? 8 : 4) : (l < BLK_SCALE_SLOTS ? 32 : 8)));
+      mbar_init(full0 + 8u * i, j < 0 ? 1 : (l < 0 ? (PAIR ? 8 : 4) : (l < SLOTS ? 32 : 8)));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (lane == 0) failed_s = 0;
@@ -447,20 +447,27 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
       uint32_t slot = 0, ph = 1u;
       for (int t = first; t < tiles && ok; t += step) {
         const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
-        const int arow = b.row0 + rank * g.bm, live = min(g.bm, b.row_end - arow);                    // (a pair's second CTA may have no rows)
+        const int arow = b.row0 + rank * g.bm, live = max(min(g.bm, b.row_end - arow), 0);            // (a pair's second CTA may have no rows)
         const float* sa = g.sa + (size_t)(live > 0 ? arow : 0) * g.sa_ld;
-        const float* sw = g.sw + (size_t)b.expert * g.sw_expert + (size_t)min(b.n0 / 128 + min(lane, 2), (g.n - 1) / 128) * g.sw_ld;
+        const float* sw = g.sw + (size_t)b.expert * g.sw_expert;
 #pragma unroll 1
-        for (int kb = 0; kb < nkb; kb += BLK_SPAN) {
+        for (int kb = 0; kb < nkb; kb += SPAN) {
           if (!(ok = mbar_wait(c, taken0 + 8u * slot, ph))) break;
           __syncwarp();
-          const uint32_t dst = smem_u32(scales_s) + 16u * (slot * BLK_SCALE_ROWS + (uint32_t)lane);
-          const int have = min(BLK_SPAN, nkb - kb);
+          const uint32_t dst = smem_u32(scales_s) + 4u * SPAN * slot * BLK_SCALE_ROWS;
 #pragma unroll 1
-          for (int r = lane; r < live; r += 32) scales_fetch(dst + 16u * (uint32_t)(r - lane), sa + (size_t)r * g.sa_ld + kb, have, g.sa_vec != 0);
-          if (lane < 3) scales_fetch(dst + 16u * 128u, sw + kb, have, g.sw_vec != 0);
+          for (int i = lane; i < live + 3; i += 32) {                 // the rows, then the blocks of weights
+            const bool is_w = i >= live;
+            const float* const src = (is_w ? sw + (size_t)min(b.n0 / 128 + i - live, (g.n - 1) / 128) * g.sw_ld : sa + (size_t)i * g.sa_ld) + kb;
+            const uint32_t to = dst + 4u * SPAN * (uint32_t)(is_w ? 128 + i - live : i);
+#pragma unroll
+            for (int q = 0; q < SPAN; q += 4) {
+              const int have = min(4, max(nkb - kb - q, 0));
+              scales_fetch(to + 4u * q, src + (have ? q : 0), have, is_w ? g.sw_vec != 0 : g.sa_vec != 0);
+            }
+          }
           scales_landed(landed0 + 8u * slot);
-          if (++slot == BLK_SCALE_SLOTS) { slot = 0; ph ^= 1u; }
+          if (++slot == SLOTS) { slot = 0; ph ^= 1u; }
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");                // (nothing is on its way into shared memory when the CTA ends)
@@ -477,21 +484,21 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
     for (int t = first; t < tiles && ok; t += step) {
       const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
       const int arow = b.row0 + rank * g.bm, row0 = arow + 32 * quarter, live = min(32, min(g.bm, b.row_end - arow) - 32 * quarter);          // rows of this warp
-      // The weights' scale changes every 128 of their rows: from group `turn` on it is that of the next block.
+      // The weights' scale changes every 128 of their rows: from group `turn` on it is that of the next block (the widest tiles' halves are whole blocks).
       const int w0 = b.n0 % 128 + col0, turn = 8 - w0 % 128 / 16;
       const float* const scales = reinterpret_cast<const float*>(scales_s);
-      const int at_row = 4 * (32 * quarter + lane), at_w = 4 * (128 + w0 / 128), at_next = 4 * (128 + min(w0 / 128 + 1, 2));
+      const int at_row = SPAN * (32 * quarter + lane), at_w = SPAN * (128 + w0 / 128), at_next = SPAN * (128 + min(w0 / 128 + 1, 2));
       f32x2 sum[GROUPS][8];
 #pragma unroll
       for (int c1 = 0; c1 < GROUPS; ++c1)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[c1][j] = 0ull;
 #pragma unroll 1
-      for (int kb0 = 0; kb0 < nkb; kb0 += BLK_SPAN) {
-        const float* const sc = scales + slot * (4 * BLK_SCALE_ROWS);
+      for (int kb0 = 0; kb0 < nkb; kb0 += SPAN) {
+        const float* const sc = scales + slot * (SPAN * BLK_SCALE_ROWS);
         if (F8 && !(ok = blocks_wait(c, landed0 + 8u * slot, lph))) break;
 #pragma unroll 1
-        for (int kb = kb0 + (HALVES ? 0 : dealt * UNIT); kb < min(kb0 + BLK_SPAN, nkb); kb += HALVES ? UNIT : 2 * UNIT) {
+        for (int kb = kb0 + (HALVES ? 0 : dealt * UNIT); kb < min(kb0 + SPAN, nkb); kb += HALVES ? UNIT : 2 * UNIT) {
           float f[PER_UNIT], f_next[PER_UNIT];                        // the row's scale times the weights', in front of `turn` and behind it
 #pragma unroll
           for (int j = 0; j < PER_UNIT; ++j) {
@@ -515,7 +522,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
                 uint32_t* const w = v[c1 & 1];
                 tmem_ld16_landed(w);
                 if (c1 + 1 < GROUPS) tmem_ld16_nowait(acc + 16u * (c1 + 1), v[(c1 + 1) & 1]);
-                const uint32_t fc = __float_as_uint(c1 < turn ? f[j] : f_next[j]);
+                const uint32_t fc = __float_as_uint(HALVES || c1 < turn ? f[j] : f_next[j]);
                 const f32x2 fj = pack2(fc, fc);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -537,7 +544,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
         if (F8) {
           __syncwarp();
           arrive_if(speaks, taken0 + 8u * slot);
-          if (++slot == BLK_SCALE_SLOTS) { slot = 0; lph ^= 1u; }
+          if (++slot == SLOTS) { slot = 0; lph ^= 1u; }
         }
       }
       if (!HALVES) dealt ^= ((nkb + UNIT - 1) / UNIT) & 1;
