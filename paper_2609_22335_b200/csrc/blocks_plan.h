@@ -11,7 +11,7 @@ constexpr int BLK_ROW = 128;                  // bytes of a k-block's row: 64 bf
 constexpr int BLK_MAX_EXPERTS = 1024;
 
 struct BlocksPlan {
-  int bm, bn, pair;            // rows of a CTA and features of a tile; whether two CTAs share it
+  int bm, bn, pair, ks;        // rows of a CTA and features of a tile; whether two CTAs share it; how many share its K (tiles up to 64 wide)
   int tiles_n, stages, units;  // units: that a set has in flight
   long long tiles;             // all of them; with experts, whose rows only the GPU knows, the most there can be
 };
@@ -58,6 +58,7 @@ inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, in
   while (p.bn > 32 && likely_m * ((n - 1) / p.bn + 1) < sms) p.bn /= 2;
   p.pair = per_expert >= 2 && p.bn == 256 ? 1 : 0;
   const int tile_rows = p.pair ? 2 * p.bm : p.bm;
+  p.ks = 1;
   p.tiles_n = (n - 1) / p.bn + 1;
   p.tiles = (experts > 0 ? (long long)(rows / tile_rows) + (rows < experts ? rows : experts) : (rows - 1) / tile_rows + 1) * p.tiles_n;
   const BlocksRings r = blocks_rings(p.bn, p.pair != 0, f8);

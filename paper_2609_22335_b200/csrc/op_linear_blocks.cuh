@@ -27,7 +27,7 @@ constexpr int BLK_SCALE_ROWS = 131;           // 128 rows and three blocks of we
 
 struct BlocksArgs {
   int rows, n, nkb, experts;                  // experts: 0 for one matrix
-  int bm, bn, tiles_n, stages, units, act;
+  int bm, bn, ks, tiles_n, stages, units, act;      // ks: CTAs (a cluster) that share the K of a tile up to 64 wide
   int vec32, vec16;                           // elements that a lane's store may cover: 4 or 1; 8, 2 or 1
   int sa_ld, sw_ld, sw_expert;                // scales: k-blocks of a row; of a block of weight rows; of an expert
   int sa_vec, sw_vec;                         // whether four of a row lie on a 16-byte boundary
@@ -108,6 +108,8 @@ __device__ __forceinline__ float gelu_exact_f(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
   return x * r;
 }
+
+__device__ __forceinline__ void st_cluster_f1(uint32_t a, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(x) : "memory"); }
 
 // Where a tile is: `row_end` is the end of its expert's rows.
 struct BlockTile { int expert, row0, row_end, n0; };
@@ -320,7 +322,9 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   __shared__ unsigned failed_s;
   __shared__ __align__(8) char experts_s[GROUPED ? sizeof(BlockExperts) : 8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = g.stages, rank = PAIR ? (int)blockIdx.x & 1 : 0;
-  const int first = PAIR ? (int)blockIdx.x >> 1 : (int)blockIdx.x, step = PAIR ? (int)gridDim.x >> 1 : (int)gridDim.x;
+  constexpr bool SPLITS = WIDTH == 64;
+  const int ks = SPLITS ? g.ks : 1, part = SPLITS ? (int)blockIdx.x % ks : 0;
+  const int first = PAIR ? (int)blockIdx.x >> 1 : (SPLITS ? (int)blockIdx.x / ks : (int)blockIdx.x), step = PAIR ? (int)gridDim.x >> 1 : (SPLITS ? (int)gridDim.x / ks : (int)gridDim.x);
   const uint32_t full0 = smem_u32(bars), done0 = full0 + 8u * BLK_MAX_STAGES, freed0 = done0 + 8u * DONE * BLK_MAX_STAGES;
   const uint32_t landed0 = freed0 + 8u * 2 * UNITS, taken0 = landed0 + 8u * SLOTS;
   const uint32_t units = WIDTH == 64 ? (uint32_t)g.units : UNITS;
@@ -356,8 +360,12 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   tc_fence_after();
   const uint32_t tmem = tmem_base_s;
   const int tile_rows = PAIR ? 2 * g.bm : g.bm;
-  const int tiles = GROUPED ? experts.tile[g.experts] : ((g.rows + tile_rows - 1) / tile_rows) * g.tiles_n, nkb = g.nkb;
-  bool ok = true;
+  const int tiles = GROUPED ? experts.tile[g.experts] : ((g.rows + tile_rows - 1) / tile_rows) * g.tiles_n;
+  // this CTA's k-blocks: whole spans
+  const int spans = (g.nkb + SPAN - 1) / SPAN, k0 = SPLITS ? spans * part / ks * SPAN : 0, nkb = SPLITS ? min(spans * (part + 1) / ks * SPAN, g.nkb) - k0 : g.nkb;
+  bool ok = true, keep = false;                // (a tile whose K is split: what a warp of sums keeps for its end)
+  int keep_row0 = 0, keep_live = 0, keep_f = 0, keep_end = 0;
+  f32x2 kept[SPLITS ? OWN : 1][8];
   if (warp < 4) {
     if (ACC_COLS == 128) regs_dec<BLK_REGS_SERVICE>();
     if (warp == 0) {
@@ -379,12 +387,12 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
               if (j == 0 || kb + j < nkb) {
                 const uint32_t to = dst + j * kb_bytes;
                 if (PAIR) {                    // of each half of the columns, this CTA's half
-                  tma_load_2d_pair(to + a_bytes, &maps.m[0], full, (kb + j) * KB, wrow + rank * 64);
-                  tma_load_2d_pair(to + a_bytes + 64 * BLK_ROW, &maps.m[0], full, (kb + j) * KB, wrow + 128 + rank * n_right);
-                  tma_load_2d_pair(to, &maps.m[1], full, (kb + j) * KB, arow);
+                  tma_load_2d_pair(to + a_bytes, &maps.m[0], full, (k0 + kb + j) * KB, wrow + rank * 64);
+                  tma_load_2d_pair(to + a_bytes + 64 * BLK_ROW, &maps.m[0], full, (k0 + kb + j) * KB, wrow + 128 + rank * n_right);
+                  tma_load_2d_pair(to, &maps.m[1], full, (k0 + kb + j) * KB, arow);
                 } else {
-                  tma_load_2d(to + a_bytes, &maps.m[0], full, (kb + j) * KB, wrow);
-                  tma_load_2d(to, &maps.m[1], full, (kb + j) * KB, arow);
+                  tma_load_2d(to + a_bytes, &maps.m[0], full, (k0 + kb + j) * KB, wrow);
+                  tma_load_2d(to, &maps.m[1], full, (k0 + kb + j) * KB, arow);
                 }
               }
           }
@@ -458,7 +466,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
 #pragma unroll 1
           for (int i = lane; i < live + 3; i += 32) {                 // the rows, then the blocks of weights
             const bool is_w = i >= live;
-            const float* const src = (is_w ? sw + (size_t)min(b.n0 / 128 + i - live, (g.n - 1) / 128) * g.sw_ld : sa + (size_t)i * g.sa_ld) + kb;
+            const float* const src = (is_w ? sw + (size_t)min(b.n0 / 128 + i - live, (g.n - 1) / 128) * g.sw_ld : sa + (size_t)i * g.sa_ld) + k0 + kb;
             const uint32_t to = dst + 4u * SPAN * (uint32_t)(is_w ? 128 + i - live : i);
 #pragma unroll
             for (int q = 0; q < SPAN; q += 4) {
@@ -573,7 +581,47 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
           both_sets(1 + quarter, true);
         }
       }
+      if (SPLITS && ks > 1) {                  // one tile a cluster: what is left to do needs the others
+        keep = true;
+        keep_row0 = row0; keep_live = live; keep_f = b.n0 + OWN * 16 * h; keep_end = min(g.n, b.n0 + g.bn);
+#pragma unroll
+        for (int c1 = 0; c1 < OWN; ++c1)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) kept[SPLITS ? c1 : 0][j] = sum[c1][j];
+        break;
+      }
       blocks_store<OWN * 16>(g, sum, stage, lane, row0, live, b.n0 + (HALVES ? col0 : OWN * 16 * h), min(g.n, b.n0 + g.bn));
+    }
+  }
+  if (SPLITS && ks > 1) {
+    // The first CTA adds up: the others' sums come into its stages, which are free once every CTA has come to the first of these barriers, and lie
+    // there in the order of the warps that hold the same place.
+    constexpr uint32_t SENT = 8u * OWN * 2048u;                       // bytes of a CTA
+    const uint32_t at = (uint32_t)((warp - 4) * OWN) * 2048u + 4u * (uint32_t)lane;
+    __syncwarp();
+    cluster_sync();
+    if (keep && part > 0) {
+      const uint32_t to = cluster_addr(stage0 + SENT * (uint32_t)(part - 1) + at, 0u);
+#pragma unroll
+      for (int c1 = 0; c1 < OWN; ++c1)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 x = unpack2(kept[c1][j]);
+          st_cluster_f1(to + 2048u * c1 + 256u * j, x.x);
+          st_cluster_f1(to + 2048u * c1 + 256u * j + 128u, x.y);
+        }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (keep && part == 0) {
+      const float* from = reinterpret_cast<const float*>(smem_raw + at);
+#pragma unroll 1
+      for (int r = 1; r < ks; ++r, from += SENT / 4)
+#pragma unroll
+        for (int c1 = 0; c1 < OWN; ++c1)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) kept[c1][j] = add2(kept[c1][j], pack2(__float_as_uint(from[512 * c1 + 64 * j]), __float_as_uint(from[512 * c1 + 64 * j + 32])));
+      blocks_store<OWN * 16>(g, kept, smem_raw + BLK_SMEM + 4096 * (warp - 4), lane, keep_row0, keep_live, keep_f, keep_end);
     }
   }
   tc_fence_before();

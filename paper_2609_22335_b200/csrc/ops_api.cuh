@@ -212,7 +212,7 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   g.rows = rows; g.n = n; g.nkb = (k - 1) / (BLK_ROW / width) + 1; g.experts = experts;
   const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, F8, dev.sms);
   if (p.tiles > INT32_MAX) return VLA_ERR_INVALID;
-  g.bm = p.bm; g.bn = p.bn; g.tiles_n = p.tiles_n; g.stages = p.stages; g.units = p.units; g.act = act;
+  g.bm = p.bm; g.bn = p.bn; g.ks = p.ks; g.tiles_n = p.tiles_n; g.stages = p.stages; g.units = p.units; g.act = act;
   g.sa_ld = g.nkb; g.sw_ld = g.nkb; g.sw_expert = ((n - 1) / 128 + 1) * g.nkb;
   g.offsets = offsets; g.sa = sa; g.sw = sw;
   g.sa_vec = g.nkb % 4 == 0 && (reinterpret_cast<uintptr_t>(sa) & 15) == 0;
@@ -223,7 +223,8 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   g.err = dev.error_of(op);
   OpMaps maps;
   if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.pair ? 64 : p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
-  const int ctas = p.pair ? 2 : 1, room = dev.sms / ctas, grid = ctas * (int)(p.tiles < room ? p.tiles : room);
+  if (p.ks > 1 && p.tiles > INT32_MAX / p.ks) return VLA_ERR_INVALID;
+  const int ctas = p.pair ? 2 : p.ks, room = dev.sms / ctas, grid = ctas * (int)(p.ks > 1 || p.tiles < room ? p.tiles : room);      // (a tile whose K is split is a cluster of its own)
   return op_launch(blocks_kernel<F8, GROUPED>(p.bn, p.pair != 0), grid, BLK_THREADS, BLK_SMEM_ALL, ctas, s, g, maps, op_fault());
 }
 inline bool op_linear_blocks_ok(const void* a, const void* w, const float* out32, const void* out16, int rows, int n, int k, int step, int act) {
