@@ -42,29 +42,55 @@ inline int blocks_stages(int bm, int bn, bool pair, const BlocksRings& r) {     
   return r.turns ? s & ~1 : s;
 }
 
-// rows x n outputs, nkb k-blocks; experts = 0: one matrix for all rows.
-inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, int sms) {
-  BlocksPlan p;
-  const int share = experts > 0 ? (rows - 1) / experts + 1 : rows;        // rows of an expert, if they had equally many
+// rows x n outputs, nkb k-blocks; experts = 0: one matrix for all rows.  fours: CTAs in clusters of four that run at once.
+//
+// The choice with the least estimated time: a tile's k-blocks at `kb` us each -- what the hand-overs between tensor core and sums leave of a kernel's
+// width, or its operands at 85 bytes a ns -- and its end, in as many rounds as the tiles take on the chip; a K that is shared, its exchange.  Of experts only
+// the number is known: an expert's rows end in the middle of a tile, so each is taken to have half a tile more than its share, and a tile to
+// be twice as high as an expert's share is, 128 rows at most (of four heights tried per shape 1.2 % behind the best one on average).
+// Fitted to 260 shapes of 1..16384 x 7..16384 x 64..16384 and up to 64 experts, with every width, height and split timed: 2.1 % behind the best choice
+// on average, more than 10 % in 13, up to 1.4 times where an odd width makes the stores the longest part or the experts' rows fall
+// otherwise.  (The widest tile that gives every SM one, alone: 13 %, 1.9 times.)
+inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, int sms, int fours) {
+  static const double kKb[2][4] = {{0.10, 0.26, 0.43, 0.49}, {0.18, 0.33, 0.51, 0.46}}, kEnd[4] = {0.94, 0.88, 1.24, 1.96};        // [e4m3][width 64, 128, 256, pair]
+  BlocksPlan p = {};
+  const int share = experts > 0 ? (rows - 1) / experts + 1 : rows, busy = rows < experts ? rows : experts;      // rows of an expert, if they had equally many; experts with any
+  int bm;
   if (experts > 0) {
-    for (p.bm = 16; p.bm < share && p.bm < 128; p.bm *= 2) {}
+    for (bm = 16; bm < 128 && bm < 2 * (long long)share; bm *= 2) {}
   } else {
     const int tiles_m = (rows - 1) / 128 + 1;
-    p.bm = ((rows - 1) / tiles_m / 16 + 1) * 16;
+    bm = ((rows - 1) / tiles_m / 16 + 1) * 16;
   }
-  const int per_expert = (share - 1) / p.bm + 1;
-  const long long likely_m = experts > 0 ? (long long)per_expert * (rows < experts ? rows : experts) : per_expert;
-  p.bn = 256;
-  while (p.bn > 32 && likely_m * ((n - 1) / p.bn + 1) < sms) p.bn /= 2;
-  p.pair = per_expert >= 2 && p.bn == 256 ? 1 : 0;
+  double best = 1e300;
+  const int spans = (nkb + 3) / 4;
+  for (int bn = 256; bn >= 16; bn -= bn == 256 ? 128 : 16) {
+    if (bn > 16 && bn >= n + 16 && !(bn == 256 && n > 128)) continue;
+    const long long tiles_n = (n - 1) / bn + 1;
+    for (int kind = 0; kind < 3; ++kind) {    // as it is; a pair's; K shared by two, then four
+      const bool pair = bn == 256 && kind == 1;
+      const int ks = bn <= 64 ? 1 << kind : 1, w = pair ? 3 : (bn > 128 ? 2 : (bn > 64 ? 1 : 0)), tile_rows = pair ? 256 : bm;
+      if (kind > 0 && !(pair && (experts == 0 ? rows > 128 : bm == 128) && sms >= 2) && !(ks > 1 && nkb >= 8 * ks)) continue;
+      const int own_bm = pair && experts == 0 ? ((rows - 1) / (2 * ((rows - 1) / 256 + 1)) / 16 + 1) * 16 : bm;
+      const long long full = (rows - 1) / (pair ? 2 * own_bm : tile_rows) + 1;
+      const long long tiles_m = experts == 0 ? full : (rows + tile_rows * (long long)busy / 2 - 1) / tile_rows + 1;
+      const long long likely = (experts > 0 && tiles_m < busy ? busy : tiles_m) * tiles_n;
+      const long long slots = pair ? sms / 2 : (ks == 4 ? fours / 4 : (ks == 2 ? sms / 2 : sms));
+      if (slots < 1) continue;
+      const double rounds = (double)((likely - 1) / slots + 1), bytes = (own_bm + (pair ? 128 : bn)) * BLK_ROW;
+      double kb = kKb[f8][w] + (w < 2 ? 0.04 * own_bm / 128 : 0.0);
+      if (bytes / 85e3 > kb) kb = bytes / 85e3;
+      const int steps = ks > 1 ? ((spans - 1) / ks + 1) * 4 : nkb;
+      const double t = rounds * (steps * kb + kEnd[w]) + (ks > 1 ? 0.56 : 0.0) + (ks > 2 ? 0.12 : 0.0);
+      if (t < best) { best = t; p.bm = own_bm; p.bn = bn; p.pair = pair ? 1 : 0; p.ks = ks; }
+    }
+  }
   const int tile_rows = p.pair ? 2 * p.bm : p.bm;
-  p.ks = 1;
   p.tiles_n = (n - 1) / p.bn + 1;
-  p.tiles = (experts > 0 ? (long long)(rows / tile_rows) + (rows < experts ? rows : experts) : (rows - 1) / tile_rows + 1) * p.tiles_n;
+  p.tiles = (experts > 0 ? (long long)(rows / tile_rows) + busy : (rows - 1) / tile_rows + 1) * p.tiles_n;
   const BlocksRings r = blocks_rings(p.bn, p.pair != 0, f8);
   p.stages = blocks_stages(p.bm, p.bn, p.pair != 0, r);
   p.units = p.stages / r.stages < r.units ? p.stages / r.stages : r.units;
-  (void)nkb;
   return p;
 }
 

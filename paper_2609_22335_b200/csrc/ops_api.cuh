@@ -210,7 +210,7 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   if (!op_device(&dev)) return VLA_ERR_CUDA;
   BlocksArgs g;
   g.rows = rows; g.n = n; g.nkb = (k - 1) / (BLK_ROW / width) + 1; g.experts = experts;
-  const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, F8, dev.sms);
+  const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, F8, dev.sms, dev.room.alone[4] > 0 ? 4 * dev.room.alone[4] : dev.sms);
   if (p.tiles > INT32_MAX) return VLA_ERR_INVALID;
   g.bm = p.bm; g.bn = p.bn; g.ks = p.ks; g.tiles_n = p.tiles_n; g.stages = p.stages; g.units = p.units; g.act = act;
   g.sa_ld = g.nkb; g.sw_ld = g.nkb; g.sw_expert = ((n - 1) / 128 + 1) * g.nkb;

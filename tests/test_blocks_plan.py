@@ -17,9 +17,9 @@ def plan(tmp_path_factory):
     lib = C.CDLL(str(out))
 
     def call(rows, n, nkb, experts=0, f8=True, sms=148):
-        o = (C.c_longlong * 12)()
+        o = (C.c_longlong * 13)()
         lib.blocks_plan_host(rows, n, nkb, experts, int(f8), sms, o)
-        return dict(zip(("bm", "bn", "pair", "tiles_n", "stages", "tiles", "kps", "unit_stages", "smem", "turns", "units", "most_units"), o))
+        return dict(zip(("bm", "bn", "pair", "tiles_n", "stages", "tiles", "kps", "unit_stages", "smem", "turns", "units", "most_units", "ks"), o))
     return call
 
 
@@ -44,6 +44,8 @@ def test_every_plan_is_one_the_kernel_can_run(plan):
             block = (bm + (128 if pair else bn)) * 128
             assert stages * kps * block <= p["smem"] and (stages * kps - 1) * block + 16384 <= p["smem"]       # (the MMA reads 128 rows of any block)
             tile = bm * (2 if pair else 1)
+            # a shared K: narrow tiles, work for each CTA, and the others' sums fit the first one's stages
+            assert p["ks"] in (1, 2, 4) and (p["ks"] == 1 or bn <= 64 and nkb >= 8 * p["ks"] and (p["ks"] - 1) * 32768 <= p["smem"]), p
             if e == 0:
                 assert p["tiles"] == -(-rows // tile) * p["tiles_n"]
             else:       # however the rows are spread over the experts
