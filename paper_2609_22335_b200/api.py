@@ -486,11 +486,16 @@ def _refuse(name, why):
     raise VlaError(VLA_ERR_INVALID, f"{name}: {why}")
 
 
-def _on_current_device(name, *tensors):
+def _elsewhere(first, *others):
+    """Whether any of the tensors (None: not given) is not on the current CUDA device.  (The calls below cost their host time: one question each.)"""
     import torch
-    for t in tensors:
-        if t is not None and not (t.is_cuda and t.get_device() == torch.cuda.current_device()):
-            _refuse(name, "tensors have to be on the current CUDA device")
+    dev = first.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        return True
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            return True
+    return False
 
 
 def _new(stream, shape, dtype, like):
@@ -506,78 +511,64 @@ def op_quantize(x, block_rows=1, stream=None):
     """x [m,k]: CUDA bf16 or fp32, rows may lie apart.  Returns (q [m,k] float8_e4m3fn, scales fp32 [ceil(m / block_rows), ceil(k / 128)]) with
     x ~ q * scale of its block of block_rows x 128 (see vla_op_quantize); block_rows 1 (activations) or 128 (weights)."""
     import torch
-    _on_current_device("op_quantize", x)
-    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32) or (x.shape[1] > 1 and x.stride(1) != 1):
-        _refuse("op_quantize", "x is a bf16 or fp32 matrix with rows in one piece")
+    f32 = x.dtype == torch.float32
+    if x.dim() != 2 or not (f32 or x.dtype == torch.bfloat16) or _elsewhere(x):
+        _refuse("op_quantize", "x is a bf16 or fp32 matrix on the current CUDA device")
     m, k = x.shape
-    if m < 1 or k < 16 or k % 16 or block_rows not in (1, 128):
-        _refuse("op_quantize", "at least one row, k a multiple of 16, block_rows 1 or 128")
+    ld, step = x.stride()
+    if m < 1 or k < 16 or k % 16 or step != 1 or (block_rows != 1 and block_rows != 128):
+        _refuse("op_quantize", "rows in one piece, at least one, k a multiple of 16, block_rows 1 or 128")
     q = _new(stream, (m, k), torch.float8_e4m3fn, x)
-    s = _new(stream, (-(-m // block_rows), -(-k // 128)), torch.float32, x)
-    rc = (_lib or load_library()).vla_op_quantize(x.data_ptr(), int(x.dtype == torch.float32), x.stride(0) if m > 1 else k, q.data_ptr(), s.data_ptr(),
-                                                  m, k, block_rows, _stream_ptr(stream))
+    s = _new(stream, (m if block_rows == 1 else (m + 127) // 128, (k + 127) // 128), torch.float32, x)
+    rc = (_lib or load_library()).vla_op_quantize(x.data_ptr(), int(f32), ld if m > 1 else k, q.data_ptr(), s.data_ptr(), m, k, block_rows,
+                                                  None if stream is None else stream.cuda_stream)
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_quantize failed")
     return q, s
 
 
-def _matrices(name, a, w, dtype, dims):
-    if a.dim() != 2 or w.dim() != dims or a.dtype != dtype or w.dtype != dtype or not (a.is_contiguous() and w.is_contiguous()) or a.shape[1] != w.shape[-1]:
-        _refuse(name, f"a [rows,k] and w [{'experts,' if dims == 3 else ''}n,k] are contiguous {dtype}")
-
-
-def _scales(name, sa, sw, a_shape, w_shape):
+def _blocks(name, a, scale_a, w, scale_w, offsets, out, act, out_bf16, stream):
+    """What the linear layers below have in common: their arguments looked at, the result made, and the C arguments in front of the sizes."""
     import torch
-    blocks = -(-w_shape[-1] // 128)
-    if (tuple(sa.shape) != (a_shape[0], blocks) or tuple(sw.shape) != tuple(w_shape[:-2]) + (-(-w_shape[-2] // 128), blocks) or
-            sa.dtype != torch.float32 or sw.dtype != torch.float32 or not (sa.is_contiguous() and sw.is_contiguous())):
-        _refuse(name, "scales are contiguous fp32, one for each row (of a) or 128 rows (of w) and 128 columns")
-
-
-def _outputs(name, a, n, out_bf16, out, stream):
-    import torch
-    dtype, shape = torch.bfloat16 if out_bf16 else torch.float32, (a.shape[0], n)
+    dtype = torch.bfloat16 if scale_a is None else torch.float8_e4m3fn
+    grouped = offsets is not None
+    if a.dtype != dtype or w.dtype != dtype or a.dim() != 2 or w.dim() != (3 if grouped else 2) or _elsewhere(a, w, scale_a, scale_w, offsets, out):
+        _refuse(name, f"a [rows,k] and w [{'experts,' if grouped else ''}n,k] are {dtype} on the current CUDA device")
+    m, k = a.shape
+    shape = w.shape
+    n = shape[-2]
+    if shape[-1] != k or not a.is_contiguous() or not w.is_contiguous():
+        _refuse(name, "a and w are contiguous, rows of the same k")
+    if scale_a is not None:
+        kb, nb = (k + 127) // 128, (n + 127) // 128
+        if (scale_a.shape != (m, kb) or scale_w.shape != ((shape[0], nb, kb) if grouped else (nb, kb)) or scale_a.dtype != torch.float32 or
+                scale_w.dtype != torch.float32 or not scale_a.is_contiguous() or not scale_w.is_contiguous()):
+            _refuse(name, "scales are contiguous fp32, one for each row (of a) or 128 rows (of w) and 128 columns")
+    if grouped and (offsets.shape != (shape[0] + 1,) or offsets.dtype != torch.int32 or not offsets.is_contiguous()):
+        _refuse(name, "offsets is contiguous int32, [experts + 1]")
+    result = torch.bfloat16 if out_bf16 else torch.float32
     if out is None:
-        out = _new(stream, shape, dtype, a)
-    elif tuple(out.shape) != shape or out.dtype != dtype or not out.is_contiguous():
+        out = _new(stream, (m, n), result, a)
+    elif out.shape != (m, n) or out.dtype != result or not out.is_contiguous():
         _refuse(name, "out is contiguous, [rows,n], fp32 or, with out_bf16, bf16")
-    return (out, None, out.data_ptr()) if out_bf16 else (out, out.data_ptr(), None)
+    return m, n, k, out, (None, out.data_ptr()) if out_bf16 else (out.data_ptr(), None), None if stream is None else stream.cuda_stream
 
 
 def op_linear_scaled(a, scale_a, w, scale_w, act=0, out_bf16=False, stream=None):
     """a [m,k], w [n,k]: float8_e4m3fn with the scales ``op_quantize`` gives (block_rows 1 and 128).  Returns act(A W^T) of the scaled matrices as
     fp32 (or bf16) [m,n]."""
-    import torch
-    _on_current_device("op_linear_scaled", a, scale_a, w, scale_w)
-    _matrices("op_linear_scaled", a, w, torch.float8_e4m3fn, 2)
-    _scales("op_linear_scaled", scale_a, scale_w, a.shape, w.shape)
-    m, k = a.shape
-    n = w.shape[0]
-    out, p32, p16 = _outputs("op_linear_scaled", a, n, out_bf16, None, stream)
-    rc = (_lib or load_library()).vla_op_linear_scaled(a.data_ptr(), scale_a.data_ptr(), w.data_ptr(), scale_w.data_ptr(), p32, p16, m, n, k, act,
-                                                       _stream_ptr(stream))
+    m, n, k, out, (p32, p16), s = _blocks("op_linear_scaled", a, scale_a, w, scale_w, None, None, act, out_bf16, stream)
+    rc = (_lib or load_library()).vla_op_linear_scaled(a.data_ptr(), scale_a.data_ptr(), w.data_ptr(), scale_w.data_ptr(), p32, p16, m, n, k, act, s)
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_linear_scaled failed")
     return out
 
 
-def _offsets_ok(name, offsets, experts):
-    import torch
-    if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.shape[0] != experts + 1 or not offsets.is_contiguous():
-        _refuse(name, "offsets is contiguous int32, [experts + 1]")
-
-
 def op_linear_grouped(a, w, offsets, act=0, out_bf16=False, out=None, stream=None):
     """a [t,k] bf16, rows sorted by expert; w [experts,n,k] bf16; offsets int32 [experts + 1] on the GPU: rows offsets[e] .. offsets[e + 1] go through
     expert e.  Returns act(a W_e^T) as fp32 (or bf16) [t,n]; rows outside of all experts are left as they were in ``out`` (without one: undefined)."""
-    import torch
-    _on_current_device("op_linear_grouped", a, w, offsets, out)
-    _matrices("op_linear_grouped", a, w, torch.bfloat16, 3)
-    experts, n, k = w.shape
-    _offsets_ok("op_linear_grouped", offsets, experts)
-    out, p32, p16 = _outputs("op_linear_grouped", a, n, out_bf16, out, stream)
-    rc = (_lib or load_library()).vla_op_linear_grouped(a.data_ptr(), w.data_ptr(), offsets.data_ptr(), p32, p16, a.shape[0], n, k, experts, act,
-                                                        _stream_ptr(stream))
+    m, n, k, out, (p32, p16), s = _blocks("op_linear_grouped", a, None, w, None, offsets, out, act, out_bf16, stream)
+    rc = (_lib or load_library()).vla_op_linear_grouped(a.data_ptr(), w.data_ptr(), offsets.data_ptr(), p32, p16, m, n, k, w.shape[0], act, s)
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_linear_grouped failed")
     return out
@@ -585,15 +576,9 @@ def op_linear_grouped(a, w, offsets, act=0, out_bf16=False, out=None, stream=Non
 
 def op_linear_grouped_scaled(a, scale_a, w, scale_w, offsets, act=0, out_bf16=False, out=None, stream=None):
     """``op_linear_grouped`` on float8_e4m3fn operands: scale_a [t, ceil(k/128)], scale_w [experts, ceil(n/128), ceil(k/128)]."""
-    import torch
-    _on_current_device("op_linear_grouped_scaled", a, scale_a, w, scale_w, offsets, out)
-    _matrices("op_linear_grouped_scaled", a, w, torch.float8_e4m3fn, 3)
-    _scales("op_linear_grouped_scaled", scale_a, scale_w, a.shape, w.shape)
-    experts, n, k = w.shape
-    _offsets_ok("op_linear_grouped_scaled", offsets, experts)
-    out, p32, p16 = _outputs("op_linear_grouped_scaled", a, n, out_bf16, out, stream)
+    m, n, k, out, (p32, p16), s = _blocks("op_linear_grouped_scaled", a, scale_a, w, scale_w, offsets, out, act, out_bf16, stream)
     rc = (_lib or load_library()).vla_op_linear_grouped_scaled(a.data_ptr(), scale_a.data_ptr(), w.data_ptr(), scale_w.data_ptr(), offsets.data_ptr(), p32, p16,
-                                                               a.shape[0], n, k, experts, act, _stream_ptr(stream))
+                                                               m, n, k, w.shape[0], act, s)
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_linear_grouped_scaled failed")
     return out
@@ -605,31 +590,48 @@ def op_qk_norm_rope(q, k, hq, hkv, hd, gq=None, gk=None, eps=1e-6, pos=None, pos
     first ``rot`` values of each (None: all) by position: ``pos`` int32 [t], or pos0 + row.  gq, gk: fp32 gains [hd] or None.  Returns (out_q, out_k),
     bf16, new ones without gaps where none are given (see vla_op_qk_norm_rope)."""
     import torch
-    name = "op_qk_norm_rope"
-    if hq < 1 or hkv < 0 or hd < 1 or (k is None) != (hkv == 0):
-        _refuse(name, "at least one query head, and k where there are key heads")
-    _on_current_device(name, q, k, gq, gk, pos, out_q, out_k)
-    t = q.shape[0]
-    for x, heads in ((q, hq), (k, hkv)):
-        if x is not None and (x.dim() != 2 or tuple(x.shape) != (t, heads * hd) or x.dtype not in (torch.bfloat16, torch.float32) or x.dtype != q.dtype or x.stride(1) != 1):
-            _refuse(name, "q [t, hq*hd] and k [t, hkv*hd] are both bf16 or both fp32, with rows in one piece")
+    name, f32, bf16 = "op_qk_norm_rope", torch.float32, torch.bfloat16
+    dt = q.dtype
+    if (dt != bf16 and dt != f32) or q.dim() != 2 or hq < 1 or hkv < 0 or (k is None) != (hkv == 0) or _elsewhere(q, k, gq, gk, pos, out_q, out_k):
+        _refuse(name, "q, and k where there are key heads, are bf16 or fp32 matrices on the current CUDA device, like all else")
+    t, wq = q.shape
+    ld_q, step = q.stride()
+    wk, ld_k, ptr_k, ld_ok, ptr_ok = hkv * hd, 0, None, 0, None
+    if wq != hq * hd or step != 1 or t < 1:
+        _refuse(name, "q is [t, hq*hd], rows in one piece, at least one")
+    if k is not None:
+        if k.dtype != dt or k.shape != (t, wk) or k.stride(1) != 1:
+            _refuse(name, "k is [t, hkv*hd], of q's type, rows in one piece")
+        ld_k, ptr_k = k.stride(0), k.data_ptr()
     for x in (gq, gk):
-        if x is not None and (tuple(x.shape) != (hd,) or x.dtype != torch.float32 or not x.is_contiguous()):
+        if x is not None and (x.shape != (hd,) or x.dtype != f32 or not x.is_contiguous()):
             _refuse(name, "gains are contiguous fp32, [hd]")
-    if pos is not None and (tuple(pos.shape) != (t,) or pos.dtype != torch.int32 or not pos.is_contiguous()):
+    if pos is not None and (pos.shape != (t,) or pos.dtype != torch.int32 or not pos.is_contiguous()):
         _refuse(name, "pos is contiguous int32, [t]")
     if out_q is None:
-        out_q = _new(stream, (t, hq * hd), torch.bfloat16, q)
-    if out_k is None and hkv:
-        out_k = _new(stream, (t, hkv * hd), torch.bfloat16, k)
-    for x, heads in ((out_q, hq), (out_k, hkv)):
-        if (x is None) != (heads == 0) or (x is not None and (tuple(x.shape) != (t, heads * hd) or x.dtype != torch.bfloat16 or x.stride(1) != 1)):
-            _refuse(name, "outputs are bf16, of the inputs' shapes, with rows in one piece")
-    ptr = lambda x: None if x is None else x.data_ptr()                               # noqa: E731
-    ld = lambda x, heads: 0 if x is None else x.stride(0) if t > 1 else heads * hd    # noqa: E731  (one row: its stride says nothing)
-    rc = (_lib or load_library()).vla_op_qk_norm_rope(ptr(q), ptr(k), int(q.dtype == torch.float32), ld(q, hq), ld(k, hkv), ptr(out_q), ptr(out_k),
-                                                      ld(out_q, hq), ld(out_k, hkv), t, hq, hkv, hd, ptr(gq), ptr(gk), eps, ptr(pos), pos0,
-                                                      hd if rot is None else rot, base, int(bool(interleaved)), _stream_ptr(stream))
+        out_q, ld_oq = _new(stream, (t, wq), bf16, q), wq
+    else:
+        if out_q.dtype != bf16 or out_q.shape != (t, wq) or out_q.stride(1) != 1:
+            _refuse(name, "out_q is bf16 [t, hq*hd], rows in one piece")
+        ld_oq = out_q.stride(0)
+    if hkv == 0:
+        if out_k is not None:
+            _refuse(name, "out_k goes with k")
+    elif out_k is None:
+        out_k, ld_ok = _new(stream, (t, wk), bf16, q), wk
+    else:
+        if out_k.dtype != bf16 or out_k.shape != (t, wk) or out_k.stride(1) != 1:
+            _refuse(name, "out_k is bf16 [t, hkv*hd], rows in one piece")
+        ld_ok = out_k.stride(0)
+    if out_k is not None:
+        ptr_ok = out_k.data_ptr()
+    if t == 1:                                 # (the stride of one row says nothing)
+        ld_q = ld_oq = wq
+        ld_k = ld_ok = wk
+    rc = (_lib or load_library()).vla_op_qk_norm_rope(q.data_ptr(), ptr_k, int(dt == f32), ld_q, ld_k, out_q.data_ptr(), ptr_ok, ld_oq, ld_ok, t, hq, hkv, hd,
+                                                      None if gq is None else gq.data_ptr(), None if gk is None else gk.data_ptr(), eps,
+                                                      None if pos is None else pos.data_ptr(), pos0, hd if rot is None else rot, base, int(interleaved),
+                                                      None if stream is None else stream.cuda_stream)
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_qk_norm_rope failed")
     return out_q, out_k

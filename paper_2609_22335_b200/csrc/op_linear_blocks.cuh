@@ -17,6 +17,7 @@
 #pragma once
 #include "blocks_plan.h"
 #include "op_linear_pair.cuh"
+#include "packed_f32.cuh"
 
 namespace vla {
 
@@ -75,29 +76,6 @@ __device__ __forceinline__ void scales_fetch(uint32_t dst, const float* src, int
 }
 __device__ __forceinline__ void scales_landed(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
-
-// Two sums at a time (the packed forms: half the instructions of a loop that is bound by them).
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(uint32_t x, uint32_t y) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(x), "r"(y));
-  return r;
-}
-__device__ __forceinline__ float2 unpack2(f32x2 v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-  f32x2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
 }
 
 // 0.5 x (1 + tanh(u)) = x / (1 + e^-2u): to fp32 precision at the price of a SiLU (tanh.approx is off by 2^-11, which shows in fp32 results).

@@ -8,11 +8,12 @@
 // Bound by memory (x in, y out).  A thread has sixteen values of a head, both halves of eight pairs (P threads a head), and keeps their
 // sines over the heads it takes in turn, so that they cost little; sixteen-byte loads and stores.
 #pragma once
+#include "packed_f32.cuh"
 #include "tiles_common.cuh"
 
 namespace vla {
 
-constexpr int QK_THREADS = 128;
+constexpr int QK_THREADS = 128, QK_CTAS = 7;    // threads of a CTA, CTAs an SM has room for (six 23.3, eight 22.8 us)
 
 struct QkArgs {
   const void *q, *k;
@@ -26,81 +27,118 @@ struct QkArgs {
   unsigned long long freq[128];
 };
 
-__device__ __forceinline__ void qk_load(const void* p, size_t at, bool f32, float* v) {
-  if (f32) {
-    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-    const float4 a = f[0], b = f[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-    unpack8(*reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p) + at), v);
+template <bool F32>
+struct QkRaw { uint4 w[F32 ? 4 : 2]; };        // a thread's two runs of eight, as they lie
+template <bool F32>
+__device__ __forceinline__ void qk_load(QkRaw<F32>& r, const char* p, int apart) {
+  constexpr int H = F32 ? 2 : 1;
+  const uint4 *a = reinterpret_cast<const uint4*>(p), *b = reinterpret_cast<const uint4*>(p + apart);
+#pragma unroll
+  for (int i = 0; i < H; ++i) { r.w[i] = a[i]; r.w[H + i] = b[i]; }
+}
+template <bool F32>
+__device__ __forceinline__ void qk_values(const QkRaw<F32>& r, float* v) {
+#pragma unroll
+  for (int i = 0; i < (F32 ? 4 : 2); ++i) {
+    if (F32) {
+      v[4 * i] = __uint_as_float(r.w[i].x); v[4 * i + 1] = __uint_as_float(r.w[i].y); v[4 * i + 2] = __uint_as_float(r.w[i].z); v[4 * i + 3] = __uint_as_float(r.w[i].w);
+    } else {
+      unpack8(r.w[i], v + 8 * i);
+    }
   }
 }
-__device__ __forceinline__ void qk_store(unsigned short* p, const float* v) {
+__device__ __forceinline__ void qk_store(char* p, const float* v) {
   *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
+// A team of 1 << (lp + lh) threads a row.
 template <bool F32, bool INTERLEAVED>
-__global__ void __launch_bounds__(QK_THREADS) vla_op_qk_rope_kernel(const __grid_constant__ QkArgs g) {
+__global__ void __launch_bounds__(QK_THREADS, QK_CTAS) vla_op_qk_rope_kernel(const __grid_constant__ QkArgs g) {
+  // (a lane's own frequencies: from the arguments themselves, one address at a time, they took a third of the kernel)
+  __shared__ unsigned long long freq[8][16];   // [j][c]: of pair 8 c + j
+  for (int i = threadIdx.x; i < g.rot / 2; i += QK_THREADS) freq[i & 7][i >> 3] = g.freq[i];
+  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int P = 1 << g.lp, c = threadIdx.x & (P - 1), h0 = (int)(threadIdx.x >> g.lp) & ((1 << g.lh) - 1);
+  constexpr int W = F32 ? 4 : 2;
+  const int P = 1 << g.lp, c = threadIdx.x & (P - 1), aside = 1 << g.lh, h0 = (int)(threadIdx.x >> g.lp) & (aside - 1);
   const long long row = ((long long)blockIdx.x * QK_THREADS + threadIdx.x) >> (g.lp + g.lh);
   const bool live = row < g.t && 16 * c < g.hd, turned = 16 * c < g.rot;
   // the sixteen values: two runs of eight
-  const int lo = INTERLEAVED || !turned ? 16 * c : 8 * c, hi = INTERLEAVED || !turned ? lo + 8 : g.rot / 2 + 8 * c;
-  float cs[8], sn[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) { cs[j] = 1.0f; sn[j] = 0.0f; }
+  const int lo = INTERLEAVED || !turned ? 16 * c : 8 * c, run = INTERLEAVED || !turned ? 8 : g.rot / 2;
+  // Where head h's lie: a whole number of heads behind the queries' or the keys' start.
+  const char* const q = static_cast<const char*>(g.q) + (row * g.ld_q + lo) * W;
+  const char* const k = static_cast<const char*>(g.k) + (row * g.ld_k + lo - (long long)g.hq * g.hd) * W;
+  char* const oq = reinterpret_cast<char*>(g.out_q) + (row * g.ld_oq + lo) * 2;
+  char* const ok = reinterpret_cast<char*>(g.out_k) + (row * g.ld_ok + lo - (long long)g.hq * g.hd) * 2;
+  // A head is asked for while the one before is worked on (in place, too: a thread writes what it alone has read).  Two ahead cost more threads than
+  // they were worth (8192 rows of 24 heads of 128: 23.2 us for 20.9).
+  QkRaw<F32> next = {};
+  auto fetch = [&](QkRaw<F32>& to, int h) {
+    if (live && h < g.heads) qk_load<F32>(to, (h >= g.hq ? k : q) + (long long)h * (g.hd * W), run * W);
+  };
+  fetch(next, h0);
+  // Everything from here on two values at a time: the rows' own pairs (j, j + 1) of each run, or, interleaved, the first and second values of two pairs.
+  auto two = [](float x, float y) { return pack2(__float_as_uint(x), __float_as_uint(y)); };
+  auto at = [](int i) { return INTERLEAVED ? (i < 4 ? 4 * i : 4 * (i - 4) + 1) : 2 * i; };              // the first of pair i; the second is `apart` further on
+  constexpr int apart = INTERLEAVED ? 2 : 1;
+  f32x2 gain[8], c2[4], s2[4], n2[4];
   if (live && turned) {
     const long long pos = g.pos ? (long long)g.pos[row] : (long long)g.pos0 + row;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const unsigned long long turn = (unsigned long long)pos * g.freq[8 * c + j];
-      sincospif((float)(int)(turn >> 32) * 0x1p-31f, &sn[j], &cs[j]);       // half turns
+    for (int j = 0; j < 4; ++j) {
+      float sn[2], cs[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const unsigned long long turn = (unsigned long long)pos * freq[2 * j + e][c];
+        __sincosf((float)(int)(turn >> 32) * 1.4629180792671596e-9f, &sn[e], &cs[e]);          // 2 pi / 2^32: between -pi and pi these are off by 2^-21
+      }
+      c2[j] = two(cs[0], cs[1]); s2[j] = two(sn[0], sn[1]); n2[j] = two(-sn[0], -sn[1]);
     }
   }
-  float gain[16];
   int gained = -1;                             // whose gains these are: 0 queries', 1 keys'
-  for (int h = h0; h - h0 < g.heads; h += 1 << g.lh) {       // (the same number of times for all threads of a warp)
+#pragma unroll 1
+  for (int h = h0; h - h0 < g.heads; h += aside) {       // (the same number of times for all threads of a warp)
     const bool have = live && h < g.heads, is_k = h >= g.hq;
     float v[16];
+    qk_values<F32>(next, v);
+    fetch(next, h + aside);
+    f32x2 x[8], s4 = 0;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = 0.0f;
-    if (have) {
-      const size_t at = is_k ? (size_t)row * g.ld_k + (size_t)(h - g.hq) * g.hd : (size_t)row * g.ld_q + (size_t)h * g.hd;
-      qk_load(is_k ? g.k : g.q, at + lo, F32, v);
-      qk_load(is_k ? g.k : g.q, at + hi, F32, v + 8);
-    }
-    float ss = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) ss = fmaf(v[j], v[j], ss);
+    for (int i = 0; i < 8; ++i) { x[i] = two(v[at(i)], v[at(i) + apart]); s4 = fma2(x[i], x[i], s4); }
+    const float2 halves = unpack2(s4);
+    float ss = have ? halves.x + halves.y : 0.0f;
     for (int o = P >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
     if (!have) continue;
     if (gained != (int)is_k) {
       gained = (int)is_k;
       const float* p = is_k ? g.gain_k : g.gain_q;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { gain[j] = p ? p[lo + j] : 1.0f; gain[8 + j] = p ? p[hi + j] : 1.0f; }
+      for (int i = 0; i < 8; ++i) {
+        const int a = at(i) < 8 ? lo + at(i) : lo + run + at(i) - 8, b = at(i) + apart < 8 ? lo + at(i) + apart : lo + run + at(i) + apart - 8;
+        gain[i] = p ? two(p[a], p[b]) : two(1.0f, 1.0f);
+      }
     }
     const float r = rsqrtf(fmaf(ss, g.inv_hd, g.eps));
+    const f32x2 r2 = two(r, r);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = v[j] * r * gain[j];
-    if (INTERLEAVED && turned) {
+    for (int i = 0; i < 8; ++i) x[i] = mul2(mul2(x[i], r2), gain[i]);
+    if (turned) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = v[2 * j], y = v[2 * j + 1];
-        v[2 * j] = fmaf(x, cs[j], -y * sn[j]); v[2 * j + 1] = fmaf(y, cs[j], x * sn[j]);
-      }
-    } else if (turned) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = v[j], y = v[8 + j];
-        v[j] = fmaf(x, cs[j], -y * sn[j]); v[8 + j] = fmaf(y, cs[j], x * sn[j]);
+      for (int j = 0; j < 4; ++j) {            // x[j] and x[4 + j] are turned into each other
+        const f32x2 u = x[j], w = x[4 + j];
+        x[j] = fma2(u, c2[j], mul2(w, n2[j]));
+        x[4 + j] = fma2(w, c2[j], mul2(u, s2[j]));
       }
     }
-    unsigned short* o = is_k ? g.out_k + (size_t)row * g.ld_ok + (size_t)(h - g.hq) * g.hd : g.out_q + (size_t)row * g.ld_oq + (size_t)h * g.hd;
-    qk_store(o + lo, v);
-    qk_store(o + hi, v + 8);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float2 y = unpack2(x[i]);
+      v[at(i)] = y.x; v[at(i) + apart] = y.y;
+    }
+    char* const o = (is_k ? ok : oq) + (long long)h * (g.hd * 2);
+    qk_store(o, v);
+    qk_store(o + run * 2, v + 8);
   }
 }
 

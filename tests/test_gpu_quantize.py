@@ -34,7 +34,8 @@ def check(x, rows, api, view=None):
     want_q, want_s = formula(x, rows)
     assert q.shape == x.shape and s.shape == want_s.shape
     assert np.array_equal(s.cpu().numpy(), want_s, equal_nan=True)
-    assert np.array_equal(q.float().cpu().numpy(), want_q, equal_nan=True)
+    got = q.float().cpu().numpy()
+    assert np.array_equal(got, want_q, equal_nan=True)
     return q, s
 
 
@@ -50,6 +51,22 @@ def test_bytes_and_scales_are_the_formulas(m, k, f32, rows):
         x = torch.from_numpy(x).to(torch.bfloat16).float().numpy()
     view = torch.from_numpy(x).cuda()
     check(x, rows, api, view if f32 else view.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("seed", range(4))
+def test_quotients_round_as_a_division_does(f32, seed):
+    """Millions of quotients, many of them near ties of e4m3 (bf16 values over bf16 maxima), scales of every fraction, ones of nothing but ones among them."""
+    import torch
+    from paper_2609_22335_b200 import api
+    rng = np.random.default_rng(seed)
+    x = (rng.standard_normal((8192, 512)) * np.exp2(rng.integers(-60, 60, (8192, 1)))).astype(np.float32)
+    ones = np.float32(np.uint32(0x3FFFFFFF).view(np.float32)) * np.float32(448)          # amax / 448 has a fraction of ones, or nearly
+    x[:64, ::128] = ones * np.exp2(rng.integers(-20, 20, (64, 4))).astype(np.float32)
+    if not f32:
+        x = torch.from_numpy(x).to(torch.bfloat16).float().numpy()
+    view = torch.from_numpy(x).cuda()
+    check(x, 1, api, view if f32 else view.to(torch.bfloat16))
 
 
 def test_many_rows_take_the_same_values_as_few():
