@@ -72,6 +72,7 @@ __device__ __forceinline__ void op_let_next_start() { asm volatile("griddepcontr
 #include "op_attention.cuh"
 #include "op_linear.cuh"
 #include "op_linear_blocks.cuh"
+#include "op_linear_few.cuh"
 #include "op_linear_pair.cuh"
 #include "op_qk_rope.cuh"
 #include "op_quantize.cuh"
@@ -119,6 +120,9 @@ inline bool op_look_up(int dev, OpDevice* d) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LINP_SMEM) != cudaSuccess) return false;
   for (auto* kernel : {vla_op_attention_kernel<1>, vla_op_attention_kernel<2>})
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) != cudaSuccess) return false;
+  for (int rows : {16, 32, 64})
+    for (auto* kernel : {few_kernel<true, false>(rows), few_kernel<true, true>(rows), few_kernel<false, true>(rows)})
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM) != cudaSuccess) return false;
   for (int width : {64, 128, 256, 512}) {     // (512: a pair's; of all but the narrowest the warpgroups pass registers on, and what they ask for has to be there)
     for (auto* kernel : {blocks_kernel<true, false>(width, width > 256), blocks_kernel<true, true>(width, width > 256), blocks_kernel<false, true>(width, width > 256)}) {
       if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BLK_SMEM_ALL) != cudaSuccess) return false;
@@ -224,6 +228,10 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   OpMaps maps;
   if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.pair ? 64 : p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
   if (p.ks > 1 && p.tiles > INT32_MAX / p.ks) return VLA_ERR_INVALID;
+  if (p.few) {
+    const int room = 2 * dev.sms, grid = p.ks * (int)(p.ks > 1 || p.tiles < room ? p.tiles : room);
+    return op_launch(few_kernel<F8, GROUPED>(p.bm), grid, FEW_THREADS, FEW_SMEM, p.ks, s, g, maps, op_fault());
+  }
   const int ctas = p.pair ? 2 : p.ks, room = dev.sms / ctas, grid = ctas * (int)(p.ks > 1 || p.tiles < room ? p.tiles : room);      // (a tile whose K is split is a cluster of its own)
   return op_launch(blocks_kernel<F8, GROUPED>(p.bn, p.pair != 0), grid, BLK_THREADS, BLK_SMEM_ALL, ctas, s, g, maps, op_fault());
 }

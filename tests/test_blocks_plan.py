@@ -17,15 +17,15 @@ def plan(tmp_path_factory):
     lib = C.CDLL(str(out))
 
     def call(rows, n, nkb, experts=0, f8=True, sms=148):
-        o = (C.c_longlong * 13)()
+        o = (C.c_longlong * 15)()
         lib.blocks_plan_host(rows, n, nkb, experts, int(f8), sms, o)
-        return dict(zip(("bm", "bn", "pair", "tiles_n", "stages", "tiles", "kps", "unit_stages", "smem", "turns", "units", "most_units", "ks"), o))
+        return dict(zip(("bm", "bn", "pair", "tiles_n", "stages", "tiles", "kps", "unit_stages", "smem", "turns", "units", "most_units", "ks", "few", "few_smem"), o))
     return call
 
 
 def shapes():
     rnd = random.Random(3)
-    out = [(r, n, nkb, e) for r in (1, 16, 17, 127, 128, 129, 300, 100000, 1 << 30) for n in (1, 7, 64, 257, 9500, 1 << 20) for nkb in (1, 2, 3, 65, 1000)
+    out = [(r, n, nkb, e) for r in (1, 8, 40, 64, 65, 16, 17, 127, 128, 129, 300, 100000, 1 << 30) for n in (1, 7, 64, 257, 9500, 1 << 20) for nkb in (1, 2, 3, 65, 1000)
            for e in (0, 1, 2, 64, 1024)]
     return out + [(int(2 ** rnd.uniform(0, 15)), int(2 ** rnd.uniform(0, 15)), int(2 ** rnd.uniform(0, 8)), rnd.choice([0, 0, 1, 3, 8, 100])) for _ in range(3000)]
 
@@ -39,13 +39,19 @@ def test_every_plan_is_one_the_kernel_can_run(plan):
             bm, bn, kps, stages, pair = p["bm"], p["bn"], p["kps"], p["stages"], p["pair"]
             assert 16 <= bm <= 128 and bm % 16 == 0 and 16 <= bn <= 256 and bn % 16 == 0 and (not pair or bn % 32 == 0 and bn > 128), p
             assert p["tiles_n"] * bn >= n > (p["tiles_n"] - 1) * bn
-            assert 1 <= p["units"] <= p["most_units"] and p["units"] * p["unit_stages"] <= stages <= 12 and not (p["turns"] and stages % 2), p
-            assert p["units"] == 2 or bn <= 64, p                    # (the wider tiles' kernels count on two)
-            block = (bm + (128 if pair else bn)) * 128
-            assert stages * kps * block <= p["smem"] and (stages * kps - 1) * block + 16384 <= p["smem"]       # (the MMA reads 128 rows of any block)
             tile = bm * (2 if pair else 1)
-            # a shared K: narrow tiles, work for each CTA, and the others' sums fit the first one's stages
-            assert p["ks"] in (1, 2, 4) and (p["ks"] == 1 or bn <= 64 and nkb >= 8 * p["ks"] and (p["ks"] - 1) * 32768 <= p["smem"]), p
+            if p["few"]:        # operands exchanged: half an SM's shared and tensor memory, a stage's accumulator each, the others' sums in the first CTA's stages
+                block = (bm + bn) * 128
+                assert bm in (16, 32, 64) and bn <= 128 and not pair and p["ks"] in (1, 2, 4, 8) and nkb >= p["ks"], p
+                assert 1 <= stages <= 8 and stages * bm <= 256 and stages * block <= p["few_smem"] and (stages - 1) * block + 16384 <= p["few_smem"], p
+                assert (p["ks"] - 1) * bm * 512 <= p["few_smem"], p
+            else:
+                assert 1 <= p["units"] <= p["most_units"] and p["units"] * p["unit_stages"] <= stages <= 12 and not (p["turns"] and stages % 2), p
+                assert p["units"] == 2 or bn <= 64, p                # (the wider tiles' kernels count on two)
+                block = (bm + (128 if pair else bn)) * 128
+                assert stages * kps * block <= p["smem"] and (stages * kps - 1) * block + 16384 <= p["smem"]   # (the MMA reads 128 rows of any block)
+                # a shared K: narrow tiles, work for each CTA, and the others' sums fit the first one's stages
+                assert p["ks"] in (1, 2, 4) and (p["ks"] == 1 or bn <= 64 and nkb >= 8 * p["ks"] and (p["ks"] - 1) * 32768 <= p["smem"]), p
             if e == 0:
                 assert p["tiles"] == -(-rows // tile) * p["tiles_n"]
             else:       # however the rows are spread over the experts
