@@ -58,12 +58,12 @@ inline int few_stages(int rows, int bn) {
 // and never less than the weights take from memory.  Of experts only the number is known: an expert's rows end in the middle of a tile, so each
 // is taken to have half a tile more than its share, and a tile (operands not exchanged) to be twice as high as an expert's share is, 128 rows at most
 // (of four heights tried per shape 1.2 % behind the best one on average).
-// Fitted to 634 shapes of 1..16384 x 7..16384 x 64..16384 and up to 64 experts, with every width, height, split and both orders of the operands timed: 2.3 %
-// behind the best choice on average, more than 10 % in 34, up to 1.6 times where an odd width makes the stores the longest part or the experts'
+// Fitted to 1008 shapes of 1..16384 x 7..16384 x 64..16384 and up to 64 experts, with every width, height, split and both orders of the operands timed: 2.6 %
+// behind the best choice on average, more than 10 % in 72, up to 1.6 times where an odd width makes the stores the longest part or the experts'
 // rows fall otherwise.  (The widest tile that gives every SM one, operands not exchanged: 13 % on the larger shapes, up to 2.3 times.)
 inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, int sms, int fours) {
-  static const double kKb[2][4] = {{0.10, 0.26, 0.43, 0.49}, {0.18, 0.33, 0.51, 0.46}}, kEnd[4] = {0.94, 0.88, 1.24, 1.96};        // [e4m3][width 64, 128, 256, pair]
-  static const double kFewKb[3] = {0.111, 0.156, 0.383}, kFewEnd[3] = {0.37, 0.60, 0.82}, kLog[9] = {0, 0, 0.39, 0, 0.78, 0, 0, 0, 1.17};
+  static const double kKb[2][4] = {{0.10, 0.26, 0.43, 0.49}, {0.18, 0.33, 0.51, 0.46}}, kEnd[4] = {0.89, 0.78, 1.09, 1.70};        // [e4m3][width 64, 128, 256, pair]
+  static const double kFewKb[3] = {0.129, 0.330, 0.427}, kFewEnd[3] = {0.29, 0.51, 0.77}, kLog[9] = {0, 0, 0.40, 0, 0.80, 0, 0, 0, 1.20};
   BlocksPlan p = {};
   const int share = experts > 0 ? (rows - 1) / experts + 1 : rows, busy = experts == 0 ? 1 : (rows < experts ? rows : experts);         // rows of an expert, if they had equally many; experts with any
   const double weights = (double)busy * n * nkb * BLK_ROW;
@@ -73,7 +73,7 @@ inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, in
     const int height = 16 << r;
     if (height >= 32 && height >= 2 * rows) break;
     const long long tiles_m = experts == 0 ? (rows - 1) / height + 1 : ((long long)rows + (long long)height * busy / 2 - 1) / height + 1, m = tiles_m < busy ? busy : tiles_m;
-    const double least = 4.66 + weights / 11.2e6;
+    const double least = 4.57 + weights / 10.9e6;
     for (int bn = 128; bn >= 16 && least < best; bn -= 16) {
       if (bn > 16 && bn >= 2 * (long long)n + 16) continue;
       const long long tiles = m * ((n - 1) / bn + 1);
@@ -83,10 +83,10 @@ inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, in
         const long long slots = ks <= 2 ? 2 * sms / ks : 2 * fours / ks, ctas = tiles * ks;
         if (slots < 1) break;
         const int rounds = tiles <= slots ? 1 : (int)((tiles - 1) / slots) + 1, active = (int)(ctas < 2 * sms ? ctas : 2 * sms);
-        double kb = kFewKb[r], bytes = (height + bn) * BLK_ROW / (active > sms ? 34.8e3 : 115e3), memory = (double)active * bn * BLK_ROW * busy / (m * 11.2e6);
+        double kb = kFewKb[r], bytes = (height + bn) * BLK_ROW / (active > sms ? 31.6e3 : 115e3), memory = (double)active * bn * BLK_ROW * busy / (m * 10.9e6);
         kb = bytes > kb ? bytes : kb;
         kb = memory > kb ? memory : kb;
-        double t = 4.24 + rounds * ((nkb + ks - 1) / ks * kb + kFewEnd[r]) + kLog[ks];
+        double t = 4.28 + rounds * ((nkb + ks - 1) / ks * kb + kFewEnd[r]) + kLog[ks];
         t = least > t ? least : t;
         if (t < best) { best = t; p.few = 1; p.bm = height; p.bn = bn; p.ks = ks; }
       }
@@ -101,7 +101,7 @@ inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, in
     bm = ((rows - 1) / tiles_m / 16 + 1) * 16;
   }
   const int spans = (nkb + 3) / 4;
-  const double least = 5.13 + weights / 6.2e6;
+  const double least = 5.17 + weights / 6.2e6;
   for (int bn = 256; bn >= 16 && least < best; bn -= bn == 256 ? 128 : 16) {
     if (bn > 16 && bn >= n + 16 && !(bn == 256 && n > 128)) continue;
     const long long tiles_n = (n - 1) / bn + 1;
@@ -116,10 +116,10 @@ inline BlocksPlan blocks_plan(int rows, int n, int nkb, int experts, bool f8, in
       const long long slots = pair ? sms / 2 : (ks == 4 ? fours / 4 : (ks == 2 ? sms / 2 : sms));
       if (slots < 1) continue;
       const double rounds = likely <= slots ? 1.0 : (double)((likely - 1) / slots + 1), bytes = (own_bm + (pair ? 128 : bn)) * BLK_ROW;
-      double kb = kKb[f8][w] + (w < 2 ? 0.04 * own_bm / 128 : 0.0);
+      double kb = kKb[f8][w] + (w < 2 ? 0.03 * own_bm / 128 : 0.0);
       if (bytes / 85e3 > kb) kb = bytes / 85e3;
       const int steps = ks > 1 ? ((spans - 1) / ks + 1) * 4 : nkb;
-      double t = 3.96 + rounds * (steps * kb + kEnd[w]) + (ks > 1 ? 0.56 : 0.0) + (ks > 2 ? 0.12 : 0.0);
+      double t = 3.96 + rounds * (steps * kb + kEnd[w]) + (ks > 1 ? 0.52 : 0.0) + (ks > 2 ? 0.12 : 0.0);
       t = least > t ? least : t;
       if (t < best) { best = t; p.few = 0; p.bm = own_bm; p.bn = bn; p.pair = pair ? 1 : 0; p.ks = ks; }
     }
