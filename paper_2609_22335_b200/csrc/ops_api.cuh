@@ -120,16 +120,6 @@ inline bool op_look_up(int dev, OpDevice* d) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LINP_SMEM) != cudaSuccess) return false;
   for (auto* kernel : {vla_op_attention_kernel<1>, vla_op_attention_kernel<2>})
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) != cudaSuccess) return false;
-  for (int rows : {16, 32, 64})
-    for (auto* kernel : {few_kernel<true, false>(rows), few_kernel<true, true>(rows), few_kernel<false, true>(rows)})
-      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM) != cudaSuccess) return false;
-  for (int width : {64, 128, 256, 512}) {     // (512: a pair's; of all but the narrowest the warpgroups pass registers on, and what they ask for has to be there)
-    for (auto* kernel : {blocks_kernel<true, false>(width, width > 256), blocks_kernel<true, true>(width, width > 256), blocks_kernel<false, true>(width, width > 256)}) {
-      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BLK_SMEM_ALL) != cudaSuccess) return false;
-      cudaFuncAttributes fa;
-      if (width > 64 && (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs * BLK_THREADS < 128 * BLK_REGS_SERVICE + 256 * BLK_REGS_SUMS)) return false;
-    }
-  }
   const bool asked = cudaFuncSetAttribute(vla_op_room_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, OPA_MAX_SMEM) == cudaSuccess;
   for (int s = 1; s <= OPA_MAX_SPLIT && asked; ++s) { d->room.alone[s] = op_clusters(s, OPA_MAX_SMEM); d->room.two[s] = op_clusters(s, LIN_SMEM); }
   return true;
@@ -205,13 +195,36 @@ inline int op_attention_run(const void* q, const void* k, const void* v, void* o
   return op_launch(p.terms == 2 ? vla_op_attention_kernel<2> : vla_op_attention_kernel<1>, n_tiles * p.split, OPA_THREADS, p.smem, p.split, s, a, maps, p, static_cast<unsigned*>(scratch), op_fault());
 }
 
+// What the linear layers by blocks need beside that, looked up on the first call of one of them (so that nobody else waits for their kernels to be loaded).
+struct OpBlocksDevice { bool ready = false; };
+inline bool op_blocks_look_up(OpBlocksDevice* d) {
+  for (int rows : {16, 32, 64})
+    for (auto* kernel : {few_kernel<true, false>(rows), few_kernel<true, true>(rows), few_kernel<false, true>(rows)})
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM) != cudaSuccess) return false;
+  for (int width : {64, 128, 256, 512}) {     // (512: a pair's; of all but the narrowest the warpgroups pass registers on, and what they ask for has to be there)
+    for (auto* kernel : {blocks_kernel<true, false>(width, width > 256), blocks_kernel<true, true>(width, width > 256), blocks_kernel<false, true>(width, width > 256)}) {
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BLK_SMEM_ALL) != cudaSuccess) return false;
+      cudaFuncAttributes fa;
+      if (width > 64 && (cudaFuncGetAttributes(&fa, kernel) != cudaSuccess || fa.numRegs * BLK_THREADS < 128 * BLK_REGS_SERVICE + 256 * BLK_REGS_SUMS)) return false;
+    }
+  }
+  d->ready = true;
+  return true;
+}
+inline bool op_blocks_device() {
+  static PerDevice<OpBlocksDevice> devices;
+  int dev = -1;
+  OpBlocksDevice d;
+  return cudaGetDevice(&dev) == cudaSuccess && devices.get(dev, &d, op_blocks_look_up) && d.ready;
+}
+
 // The linear layers of op_linear_blocks.cuh: experts = 0 for one matrix, `width` bytes an element (1 with scales, 2 without).
 template <bool F8, bool GROUPED>
 inline int op_linear_blocks_run(int op, const void* a, const float* sa, const void* w, const float* sw, const int* offsets, float* out32, void* out16,
                                 int rows, int n, int k, int experts, int act, cudaStream_t s) {
   constexpr int width = F8 ? 1 : 2;
   OpDevice dev;
-  if (!op_device(&dev)) return VLA_ERR_CUDA;
+  if (!op_device(&dev) || !op_blocks_device()) return VLA_ERR_CUDA;
   BlocksArgs g;
   g.rows = rows; g.n = n; g.nkb = (k - 1) / (BLK_ROW / width) + 1; g.experts = experts;
   const BlocksPlan p = blocks_plan(rows, n, g.nkb, experts, F8, dev.sms, dev.room.alone[4] > 0 ? 4 * dev.room.alone[4] : dev.sms);

@@ -56,3 +56,22 @@ def test_every_plan_is_one_the_kernel_can_run(plan):
                 assert p["tiles"] == -(-rows // tile) * p["tiles_n"]
             else:       # however the rows are spread over the experts
                 assert p["tiles"] >= (rows // tile + min(rows, e) - (1 if rows % tile == 0 else 0)) * p["tiles_n"]
+
+
+def kernel_of(p):
+    return ("few", p["bm"], p["ks"]) if p["few"] else (("pair",) if p["pair"] else ("wide",) if p["bn"] > 128 else ("middle",) if p["bn"] > 64 else ("narrow", p["ks"]))
+
+
+def test_the_gpu_tests_reach_every_kernel(plan):
+    """Over the shapes of test_gpu_linear_blocks.py: operands exchanged at every height, alone and with a shared K, and every width of the others."""
+    import test_gpu_linear_blocks as T
+    seen = {(True,) + kernel_of(plan(m, n, -(-k // 128))) for m, n, k in T.SCALED} | {(True,) + kernel_of(plan(m, n, 65)) for m, n in T.LONG_K}
+    shapes = [(c, n, k) for c in T.COUNTS for n, k in ((96, 136), (257, 1040), (2048, 64))] + T.EVERY
+    for counts, n, k in shapes:
+        seen.add((False,) + kernel_of(plan(sum(counts), n, -(-k // 64), len(counts), False)))
+        seen.add((True,) + kernel_of(plan(sum(counts), n, -(-k // 128), len(counts), True)))
+    seen |= {(False,) + kernel_of(plan(m, n // 2, 129, 2, False)) for m, n in T.LONG_K}
+    missing = [(f8,) + k for f8 in (False, True) for k in
+               [("pair",), ("wide",), ("middle",)] + [("narrow", ks) for ks in (1, 2, 4)] + [("few", h, ks) for h in (16, 32, 64) for ks in (1, 2, 4)] + [("few", 16, 8)]
+               if (f8,) + k not in seen]
+    assert not missing

@@ -54,8 +54,14 @@ def near(got, a, w, act, f8):
     assert bool(torch.isfinite(got).all()) and bool((d <= tol + 1e-30).all()), float((d / (tol + 1e-30)).max())
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 1, 16), (1, 7, 128), (1, 2048, 1024), (3, 33, 144), (16, 64, 256), (17, 130, 400), (33, 128, 1040), (64, 257, 512), (100, 520, 128),
-                                   (128, 256, 2048), (129, 96, 64), (300, 1000, 384), (513, 2050, 272), (1000, 4304, 1152), (40, 11008, 512)])
+# (between them they reach every kernel, width, height and split there is: test_blocks_plan.py)
+SCALED = [(1, 1, 16), (1, 7, 128), (1, 2048, 1024), (3, 33, 144), (16, 64, 256), (17, 130, 400), (33, 128, 1040), (64, 257, 512), (100, 520, 128),
+          (128, 256, 2048), (129, 96, 64), (300, 1000, 384), (513, 2050, 272), (1000, 4304, 1152), (40, 11008, 512),
+          (20, 16000, 256), (20, 11008, 1024), (20, 11008, 512), (33, 8000, 512), (33, 11008, 2048), (33, 2000, 8192), (33, 4000, 8192), (51, 6000, 8192),
+          (200, 11008, 256), (200, 11008, 1024)]
+
+
+@pytest.mark.parametrize("m,n,k", SCALED)
 @pytest.mark.parametrize("act,bf16", [(0, False), (1, False), (2, True)])
 def test_scaled_matches_the_formula(m, n, k, act, bf16):
     import torch
@@ -122,6 +128,16 @@ def test_grouped_scaled_matches_the_formula(counts, n, k, act, bf16):
     ends = offsets.tolist()
     for e, (lo, hi) in enumerate(zip(ends, ends[1:])):
         near(got[lo:hi], scaled(a[lo:hi], sa[lo:hi], 1), scaled(w[e], sw[e], 128), act, True)
+
+
+EVERY = [([32], 8000, 128), ([150, 0, 200, 250], 130, 4224), ([10, 10], 8000, 1024), ([150, 0, 200, 250], 130, 2112), ([17, 16], 16000, 128), ([80], 4000, 512), ([80], 2000, 4096), ([80], 11008, 512), ([16], 11008, 256),
+         ([80], 11008, 256), ([16], 11008, 4160), ([16], 11008, 4096), ([16], 1500, 4096), ([51], 6000, 8192), ([33], 11008, 2048), ([20], 11008, 1024)]
+
+
+@pytest.mark.parametrize("counts,n,k", EVERY)
+def test_grouped_by_every_kernel(counts, n, k):
+    test_grouped_matches_the_formula(counts, n, k, 0, True)
+    test_grouped_scaled_matches_the_formula(counts, n, k, 0, False)
 
 
 def test_grouped_over_many_experts():
@@ -244,7 +260,10 @@ def test_a_wait_that_runs_out_is_reported_and_a_captured_call_works_again():
         assert all(torch.equal(p, q) for p, q in zip(graphs[0][1], want))
 
 
-@pytest.mark.parametrize("m,n", [(1, 64), (128, 64), (128, 9500), (128, 19000), (300, 19000), (700, 12900)])
+LONG_K = [(1, 64), (128, 64), (128, 9500), (128, 19000), (300, 19000), (700, 12900)]
+
+
+@pytest.mark.parametrize("m,n", LONG_K)
 def test_long_rows_of_k(m, n):
     """Every ring of the kernels goes round many times, at every tile width: a k-block's hand-overs must not run into the next round's."""
     import torch
