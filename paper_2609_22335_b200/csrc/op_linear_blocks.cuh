@@ -29,6 +29,7 @@ constexpr int BLK_SCALE_ROWS = 131;           // 128 rows and three blocks of we
 struct BlocksArgs {
   int rows, n, nkb, experts;                  // experts: 0 for one matrix
   int bm, bn, ks, tiles_n, stages, units, act;      // ks: CTAs (a cluster) that share the K of a tile up to 64 wide
+  int boxes;                                  // whether whole tiles go out as boxes (maps 2 and 3: out16, out32)
   int vec32, vec16;                           // elements that a lane's store may cover: 4 or 1; 8, 2 or 1
   int sa_ld, sw_ld, sw_expert;                // scales: k-blocks of a row; of a block of weight rows; of an expert
   int sa_vec, sw_vec;                         // whether four of a row lie on a 16-byte boundary
@@ -90,7 +91,8 @@ __device__ __forceinline__ float gelu_exact_f(float x) {
 __device__ __forceinline__ void st_cluster_f1(uint32_t a, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(x) : "memory"); }
 
 // Where a tile is: `row_end` is the end of its expert's rows.
-struct BlockTile { int expert, row0, row_end, n0; };
+struct __align__(16) BlockTile { int expert, row0, row_end, n0; };
+constexpr int BLK_TOLD = 4;                   // tiles that the sums' warps are told of ahead, of experts (32 of them: 1 %; without any, a single tile's start takes longer by 2 %)
 
 // What the CTA knows about the experts (shared memory): first row of each, and the first of its tiles.
 struct BlockExperts {
@@ -174,6 +176,21 @@ __device__ __forceinline__ void rows_in_order(const char* stage, int lane, int l
   }
   __syncwarp();
 }
+// N columns, finished, as they lie in the row.
+template <int N>
+__device__ __forceinline__ void finished(int act, const f32x2 (*sum)[8], float* v) {
+#pragma unroll
+  for (int j = 0; j < N / 2; ++j) {
+    const float2 x = unpack2(sum[j / 8][j % 8]);
+    v[2 * j] = x.x; v[2 * j + 1] = x.y;
+  }
+  if (act == ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = gelu_exact_f(v[j]);
+  } else if (act == ACT_SILU) {
+    activate<ACT_SILU, N>(v);
+  }
+}
 template <int COLS>
 __device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*sum)[8], char* stage, int lane, int row0, int live, int f, int n_end) {
   constexpr int GROUP = COLS < 64 ? COLS : 64;                        // columns at a time: 128 bytes of bf16 (64 where there are 32), or two halves in fp32
@@ -181,17 +198,7 @@ __device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*
   for (int p = 0; p < COLS; p += GROUP) {
     if (f + p >= n_end) break;
     float v[GROUP];
-#pragma unroll
-    for (int j = 0; j < GROUP / 2; ++j) {
-      const float2 x = unpack2(sum[(p + 2 * j) / 16][j % 8]);
-      v[2 * j] = x.x; v[2 * j + 1] = x.y;
-    }
-    if (g.act == ACT_GELU) {
-#pragma unroll
-      for (int j = 0; j < GROUP; ++j) v[j] = gelu_exact_f(v[j]);
-    } else if (g.act == ACT_SILU) {
-      activate<ACT_SILU, GROUP>(v);
-    }
+    finished<GROUP>(g.act, sum + p / 16, v);
     if (g.out16) {
 #pragma unroll
       for (int j = 0; j < GROUP / 8; ++j)
@@ -232,6 +239,49 @@ __device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*
             if (lane < cols) out[(size_t)row * g.n + lane] = *reinterpret_cast<const float*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + 4 * (lane & 3));
           __syncwarp();
         }
+      }
+    }
+  }
+}
+// The same for 128 columns of 32 rows that all exist, as boxes of 32 rows x 128 bytes that the copy engine takes from the stage on its own, the last one
+// while the warp is at the next tile's sums.  (Columns behind the width are not written.)  All CTAs' tiles end at about the same time, and a warp that
+// stores itself waits for memory then.  Of several tiles a CTA: 8192 x 8192 x 2048 in 8 bits to bf16 136 -> 132 us, bf16 8192 x 4096 x 2048 by eight
+// experts to fp32 133 -> 125, 8-bit 16384 x 4096 x 2048 by 32 186 -> 178.
+__device__ __forceinline__ void box_out(const void* tmap, const char* stage, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(smem_u32(stage)), "r"(x), "r"(y) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void boxes_read(bool who) {                // the stage is free again
+  if (who) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  __syncwarp();
+}
+__device__ __forceinline__ void blocks_store_boxes(const BlocksArgs& g, const OpMaps& maps, const f32x2 (*sum)[8], char* stage, int lane, int row0, int f0) {
+  const bool who = lane == 0;
+  char* const my_row = stage + lane * 128;
+  auto send = [&](const void* tmap, int f) {                          // what all lanes have written
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (who && f < g.n) box_out(tmap, stage, f, row0);
+  };
+#pragma unroll
+  for (int p = 0; p < 128; p += 64) {
+    float v[64];
+    finished<64>(g.act, sum + p / 16, v);
+    if (g.out16) {
+      boxes_read(who);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<uint4*>(my_row + ((j ^ (lane & 7)) << 4)) =
+            make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+      send(&maps.m[2], f0 + p);
+    }
+    if (g.out32) {
+#pragma unroll
+      for (int q = 0; q < 64; q += 32) {
+        boxes_read(who);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(my_row + ((j ^ (lane & 7)) << 4)) = make_float4(v[q + 4 * j], v[q + 4 * j + 1], v[q + 4 * j + 2], v[q + 4 * j + 3]);
+        send(&maps.m[3], f0 + p + q);
       }
     }
   }
@@ -299,12 +349,13 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   constexpr int GROUPS = ACC_COLS / 16, OWN = HALVES ? GROUPS : GROUPS / 2;                          // groups of 16 columns that a warp holds sums of, and that it finishes
   constexpr int KB = F8 ? 128 : 64;                                   // elements of a k-block
   constexpr int SPAN = HALVES ? 8 : 4, SLOTS = HALVES ? 2 : 4;        // k-blocks whose scales go together, and the spans of them that have been asked for
-  constexpr int DONE = HALVES ? 2 : 1, N_BARS = (1 + DONE) * BLK_MAX_STAGES + 2 * UNITS + 2 * SLOTS;
+  constexpr int DONE = HALVES ? 2 : 1, N_BARS = (1 + DONE) * BLK_MAX_STAGES + 2 * UNITS + 2 * SLOTS + 2 * BLK_TOLD;
   static_assert(HALVES || SPU == 1, "units are dealt by stages");
   extern __shared__ __align__(1024) char smem_raw[];
   __shared__ uint32_t tmem_base_s;
   __shared__ __align__(8) uint64_t bars[N_BARS];
   __shared__ __align__(16) float4 scales_s[F8 ? SLOTS * SPAN / 4 * BLK_SCALE_ROWS : 1];
+  __shared__ BlockTile tiles_s[GROUPED ? BLK_TOLD : 1];
   __shared__ unsigned failed_s;
   __shared__ __align__(8) char experts_s[GROUPED ? sizeof(BlockExperts) : 8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = g.stages, rank = PAIR ? (int)blockIdx.x & 1 : 0;
@@ -312,15 +363,15 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   const int ks = SPLITS ? g.ks : 1, part = SPLITS ? (int)blockIdx.x % ks : 0;
   const int first = PAIR ? (int)blockIdx.x >> 1 : (SPLITS ? (int)blockIdx.x / ks : (int)blockIdx.x), step = PAIR ? (int)gridDim.x >> 1 : (SPLITS ? (int)gridDim.x / ks : (int)gridDim.x);
   const uint32_t full0 = smem_u32(bars), done0 = full0 + 8u * BLK_MAX_STAGES, freed0 = done0 + 8u * DONE * BLK_MAX_STAGES;
-  const uint32_t landed0 = freed0 + 8u * 2 * UNITS, taken0 = landed0 + 8u * SLOTS;
+  const uint32_t landed0 = freed0 + 8u * 2 * UNITS, taken0 = landed0 + 8u * SLOTS, told0 = taken0 + 8u * SLOTS, heard0 = told0 + 8u * BLK_TOLD;
   const uint32_t units = WIDTH == 64 ? (uint32_t)g.units : UNITS;
   const int w_rows = PAIR ? 128 : g.bn;                               // weight rows that this CTA stages
   const uint32_t a_bytes = (uint32_t)(g.bm * BLK_ROW), kb_bytes = (uint32_t)((g.bm + w_rows) * BLK_ROW), stage_bytes = KPS * kb_bytes, stage0 = smem_u32(smem_raw);
   BlockExperts& experts = *reinterpret_cast<BlockExperts*>(experts_s);
   if (warp == 0) {
     for (int i = lane; i < N_BARS; i += 32) {
-      const int j = i - (1 + DONE) * BLK_MAX_STAGES, l = j - 2 * UNITS;              // (freed: a set's warps; taken: all warps; landed: a lane's arrival each)
-      mbar_init(full0 + 8u * i, j < 0 ? 1 : (l < 0 ? (PAIR ? 8 : 4) : (l < SLOTS ? 32 : 8)));
+      const int j = i - (1 + DONE) * BLK_MAX_STAGES, l = j - 2 * UNITS;              // (freed: a set's warps; taken and heard: all warps; landed: a lane's arrival each)
+      mbar_init(full0 + 8u * i, j < 0 ? 1 : (l < 0 ? (PAIR ? 8 : 4) : (l < SLOTS ? 32 : (l < 2 * SLOTS ? 8 : (l < 2 * SLOTS + BLK_TOLD ? 1 : 8)))));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (lane == 0) failed_s = 0;
@@ -437,10 +488,21 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
           if (!HALVES) dealt ^= ((nkb + UNIT - 1) / UNIT) & 1;
         }
       }
-    } else if (F8) {
-      uint32_t slot = 0, ph = 1u;
+    } else if (GROUPED || F8) {
+      // of experts, the sums' warps are told where their tiles are (a search, which would stand between two tiles), and the scales are fetched
+      uint32_t slot = 0, ph = 1u, told = 0, tph = 1u;
       for (int t = first; t < tiles && ok; t += step) {
         const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
+        if (GROUPED) {
+          if (!(ok = blocks_wait(c, heard0 + 8u * told, tph))) break;
+          __syncwarp();
+          if (lane == 0) {
+            tiles_s[told] = b;
+            asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(told0 + 8u * told) : "memory");
+          }
+          if (++told == BLK_TOLD) { told = 0; tph ^= 1u; }
+        }
+        if (!F8) continue;
         const int arow = b.row0 + rank * g.bm, live = max(min(g.bm, b.row_end - arow), 0);            // (a pair's second CTA may have no rows)
         const float* sa = g.sa + (size_t)(live > 0 ? arow : 0) * g.sa_ld;
         const float* sw = g.sw + (size_t)b.expert * g.sw_expert;
@@ -473,10 +535,19 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
     const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + 256u * (uint32_t)h, my_done = done0 + (HALVES ? 8u * BLK_MAX_STAGES * (uint32_t)h : 0u);
     const uint32_t my_freed = (PAIR ? cluster_addr(freed0, 0u) : freed0) + 8u * UNITS * (uint32_t)h;
     const bool speaks = lane == 0;
-    uint32_t unit = 0, s = HALVES ? 0u : (uint32_t)h, ph = 0u, slot = 0, lph = 0u;
+    uint32_t unit = 0, s = HALVES ? 0u : (uint32_t)h, ph = 0u, slot = 0, lph = 0u, told = 0, tph = 0u;
     int dealt = h;
     for (int t = first; t < tiles && ok; t += step) {
-      const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
+      BlockTile b;
+      if (GROUPED) {
+        if (!(ok = blocks_wait(c, told0 + 8u * told, tph))) break;
+        b = tiles_s[told];
+        __syncwarp();
+        arrive_if(speaks, heard0 + 8u * told);
+        if (++told == BLK_TOLD) { told = 0; tph ^= 1u; }
+      } else {
+        b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
+      }
       const int arow = b.row0 + rank * g.bm, row0 = arow + 32 * quarter, live = min(32, min(g.bm, b.row_end - arow) - 32 * quarter);          // rows of this warp
       // The weights' scale changes every 128 of their rows: from group `turn` on it is that of the next block (the widest tiles' halves are whole blocks).
       const int w0 = b.n0 % 128 + col0, turn = 8 - w0 % 128 / 16;
@@ -579,8 +650,14 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
           for (int j = 0; j < 8; ++j) kept[SPLITS ? c1 : 0][j] = sum[c1][j];
         break;
       }
-      blocks_store<OWN * 16>(g, sum, stage, lane, row0, live, b.n0 + (HALVES ? col0 : OWN * 16 * h), min(g.n, b.n0 + g.bn));
+      if (HALVES && live == 32 && g.boxes) {
+        if constexpr (HALVES) blocks_store_boxes(g, maps, sum, stage, lane, row0, b.n0 + col0);
+      } else {
+        if (HALVES) boxes_read(speaks);
+        blocks_store<OWN * 16>(g, sum, stage, lane, row0, live, b.n0 + (HALVES ? col0 : OWN * 16 * h), min(g.n, b.n0 + g.bn));
+      }
     }
+    if (HALVES && speaks) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   if (SPLITS && ks > 1) {
     // The first CTA adds up: the others' sums come into its stages, which are free once every CTA has come to the first of these barriers, and lie

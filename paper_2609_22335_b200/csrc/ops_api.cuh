@@ -31,7 +31,7 @@ inline OpEncodeFn op_encoder() {
   return fn;
 }
 
-// 2-D row-major tensor, bf16 (or, `width` 1, bytes), boxes of 128 bytes of a row, 128-byte swizzle, zero fill outside.
+// 2-D row-major tensor, bf16 (or, by `width`, bytes or fp32), boxes of 128 bytes of a row, 128-byte swizzle, zero fill outside.
 inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int width = 2) {
   OpEncodeFn enc = op_encoder();
   if (!enc) return false;
@@ -39,7 +39,7 @@ inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t 
   cuuint64_t strides[1] = {(cuuint64_t)ld * width};
   cuuint32_t box[2] = {(cuuint32_t)(128 / width), (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  return enc(out, width == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+  return enc(out, width == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : (width == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16), 2, const_cast<void*>(base), dims, strides, box, estr,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -239,13 +239,15 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   g.vec16 = n % 8 == 0 && (reinterpret_cast<uintptr_t>(out16) & 15) == 0 ? 8 : (n % 2 == 0 && (reinterpret_cast<uintptr_t>(out16) & 3) == 0 ? 2 : 1);
   g.err = dev.error_of(op);
   OpMaps maps;
+  const int ctas = p.few || !p.pair ? p.ks : 2, room = (p.few ? 2 : 1) * dev.sms / ctas;            // CTAs that share a tile, and such groups at once
+  // (With one tile a CTA nothing goes on while boxes are taken: 817 x 4304 x 1152 with GELU 12.5 us from the warps' own stores, 13.0 as boxes.)
+  g.boxes = p.bn == 256 && p.tiles > room && (!out16 || g.vec16 == 8) && (!out32 || g.vec32 == 4);
+  if (g.boxes && out16 && !op_encode(&maps.m[2], out16, rows, n, n, 32)) return VLA_ERR_CUDA;
+  if (g.boxes && out32 && !op_encode(&maps.m[3], out32, rows, n, n, 32, 4)) return VLA_ERR_CUDA;
   if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.pair ? 64 : p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
   if (p.ks > 1 && p.tiles > INT32_MAX / p.ks) return VLA_ERR_INVALID;
-  if (p.few) {
-    const int room = 2 * dev.sms, grid = p.ks * (int)(p.ks > 1 || p.tiles < room ? p.tiles : room);
-    return op_launch(few_kernel<F8, GROUPED>(p.bm), grid, FEW_THREADS, FEW_SMEM, p.ks, s, g, maps, op_fault());
-  }
-  const int ctas = p.pair ? 2 : p.ks, room = dev.sms / ctas, grid = ctas * (int)(p.ks > 1 || p.tiles < room ? p.tiles : room);      // (a tile whose K is split is a cluster of its own)
+  const int grid = ctas * (int)(p.ks > 1 || p.tiles < room ? p.tiles : room);        // (a tile whose K is split is a cluster of its own)
+  if (p.few) return op_launch(few_kernel<F8, GROUPED>(p.bm), grid, FEW_THREADS, FEW_SMEM, ctas, s, g, maps, op_fault());
   return op_launch(blocks_kernel<F8, GROUPED>(p.bn, p.pair != 0), grid, BLK_THREADS, BLK_SMEM_ALL, ctas, s, g, maps, op_fault());
 }
 inline bool op_linear_blocks_ok(const void* a, const void* w, const float* out32, const void* out16, int rows, int n, int k, int step, int act) {

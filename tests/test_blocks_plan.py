@@ -75,3 +75,10 @@ def test_the_gpu_tests_reach_every_kernel(plan):
                [("pair",), ("wide",), ("middle",)] + [("narrow", ks) for ks in (1, 2, 4)] + [("few", h, ks) for h in (16, 32, 64) for ks in (1, 2, 4)] + [("few", 16, 8)]
                if (f8,) + k not in seen]
     assert not missing
+
+
+def test_the_boxes_tests_have_several_wide_tiles_a_block(plan):
+    import test_gpu_linear_blocks as T
+    for m, n, k in T.BOXES:
+        for p in (plan(m, n, -(-k // 128)), plan(m - 33, n, -(-k // 64), 3, False)):
+            assert p["bn"] == 256 and p["tiles"] > 148 // (2 if p["pair"] else 1), (m, n, k, p)

@@ -73,6 +73,45 @@ def test_scaled_matches_the_formula(m, n, k, act, bf16):
     near(got, scaled(a, sa, 1), scaled(w, sw, 128), act, True)
 
 
+# Several 256-wide tiles a CTA: whole blocks of rows go out as boxes of 64 (bf16) or 32 (fp32) columns, of which the last tile has none, some or a part.
+BOXES = [(2600, 4360, 256), (2600, 4384, 144), (2600, 4396, 256), (2600, 4424, 128), (4100, 4352, 400), (2600, 4363, 256)]
+
+
+@pytest.mark.parametrize("m,n,k", BOXES)
+@pytest.mark.parametrize("act", [0, 2])
+def test_rows_that_go_out_as_boxes(m, n, k, act):
+    """Both results at once, between guard values; then by expert, where rows end inside of boxes."""
+    import torch
+    from paper_2609_22335_b200 import api
+    a, sa = eight_bit(1, m, k, m + k)
+    w, sw = eight_bit(128, n, k, n + k + 1)
+    want = scaled(a, sa, 1), scaled(w, sw, 128)
+    buf32, buf16 = torch.full((m * n + 64,), 7.0, device="cuda"), torch.full((m * n + 64,), 7.0, device="cuda", dtype=torch.bfloat16)
+    o32, o16 = buf32[32:32 + m * n].view(m, n), buf16[32:32 + m * n].view(m, n)
+    for p32, p16 in ((o32, o16), (o32, None), (None, o16)):
+        o32.fill_(float("nan"))
+        o16.fill_(float("nan"))
+        rc = api.load_library().vla_op_linear_scaled(a.data_ptr(), sa.data_ptr(), w.data_ptr(), sw.data_ptr(), p32.data_ptr() if p32 is not None else None,
+                                                     p16.data_ptr() if p16 is not None else None, m, n, k, act, torch.cuda.current_stream().cuda_stream)
+        assert rc == api.VLA_OK and api.op_status(api.OP_LINEAR_SCALED) == api.VLA_OK
+        for o in (p32, p16):
+            if o is not None:
+                near(o, *want, act, True)
+        for b in (buf32, buf16):
+            assert bool((b[:32] == 7).all()) and bool((b[-32:] == 7).all())
+    if k % 8 == 0:
+        offsets, t = sort_of([m // 2 + 7, 0, m - m // 2 - 40], rest=33)
+        x = torch.randn(t, k, device="cuda", generator=gen(1)).to(torch.bfloat16)
+        v = (0.1 * torch.randn(3, n, k, device="cuda", generator=gen(2))).to(torch.bfloat16)
+        for bf16 in (False, True):
+            out = torch.full((t, n), 7.0, device="cuda", dtype=torch.bfloat16 if bf16 else torch.float32)
+            api.op_linear_grouped(x, v, offsets, act=act, out_bf16=bf16, out=out)
+            ends = offsets.tolist()
+            for e in (0, 2):
+                near(out[ends[e]:ends[e + 1]], x[ends[e]:ends[e + 1]].double(), v[e].double(), act, False)
+            assert bool((out[ends[-1]:] == 7).all())
+
+
 def test_scaled_takes_what_quantize_gives():
     import torch
     from paper_2609_22335_b200 import api
