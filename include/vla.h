@@ -295,7 +295,8 @@ int vla_op_quantize(const void* x, int32_t x_f32, int64_t ld, void* q, float* sc
  * w[i,j] * scale_w[i / 128, j / 128].  a [m,k] and w [n,k] e4m3 row-major, 16-byte aligned; scale_a fp32 [m, ceil(k/128)] and
  * scale_w fp32 [ceil(n/128), ceil(k/128)] as vla_op_quantize writes them with block_rows 1 and 128; k a multiple of 16.  Products
  * are exact, each block of 128 is summed by the tensor core in fp32, scaled, and added up in fp32.  out32, out16 and act as for vla_op_linear
- * (GeLU and SiLU to fp32 precision). */
+ * (GeLU and SiLU to fp32 precision); the outputs overlap no input.  Calls can be captured into graphs, the first one on a device
+ * among them. */
 int vla_op_linear_scaled(const void* a, const float* scale_a, const void* w, const float* scale_w, float* out32, void* out16,
                          int32_t m, int32_t n, int32_t k, int32_t act, void* stream);
 

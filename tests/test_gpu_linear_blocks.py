@@ -299,6 +299,27 @@ def test_a_wait_that_runs_out_is_reported_and_a_captured_call_works_again():
         assert all(torch.equal(p, q) for p, q in zip(graphs[0][1], want))
 
 
+FIRST = """
+import torch
+from paper_2609_22335_b200 import api
+x, w = torch.randn(70, 512, device="cuda").to(torch.bfloat16), torch.randn(2, 128, 512, device="cuda").to(torch.bfloat16)
+at = torch.tensor([0, 30, 70], dtype=torch.int32, device="cuda")
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    out = api.op_linear_grouped(x, w, at)
+    q, s = api.op_quantize(x)
+g.replay()
+assert torch.equal(out, api.op_linear_grouped(x, w, at)) and torch.equal(s, api.op_quantize(x)[1]) and api.op_status(api.OP_LINEAR_GROUPED) == api.VLA_OK
+"""
+
+
+def test_the_first_call_of_a_process_can_be_captured():
+    import os
+    import subprocess
+    import sys
+    subprocess.run([sys.executable, "-c", FIRST], check=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+
 LONG_K = [(1, 64), (128, 64), (128, 9500), (128, 19000), (300, 19000), (700, 12900)]
 
 
