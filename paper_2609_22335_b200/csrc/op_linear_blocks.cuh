@@ -191,25 +191,52 @@ __device__ __forceinline__ void finished(int act, const f32x2 (*sum)[8], float* 
     activate<ACT_SILU, N>(v);
   }
 }
+__device__ __forceinline__ void box_out(const void* tmap, const char* stage, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(smem_u32(stage)), "r"(x), "r"(y) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void boxes_read(bool who) {                // the stage is free again
+  if (who) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  __syncwarp();
+}
+// Of 256-wide tiles, 32 rows that all exist go out as boxes of 32 x 128 bytes that the copy engine takes from the stage on its own, the
+// last one while the warp is at the next tile's sums.  All CTAs' tiles end at about the same time, and a warp that stores itself waits for memory
+// then: 8192 x 8192 x 2048 in 8 bits to bf16 137 -> 134 us, bf16 8192 x 4096 x 2048 by eight experts to fp32 133 -> 126, 8-bit 16384 x 4096 x 2048
+// by 32 186 -> 182; a single tile 1 %.
+//
+// 64 columns a turn of a loop that is a loop, the sums moved down after each: a tile's end is run once where a CTA has one tile, and fetching its
+// instructions is much of what it takes (817 x 4304 x 1152 with GELU unrolled: 25.5 us for 17.4 when no cache
+// holds any of it, 12.5 for 12.4 when they all do).
 template <int COLS>
-__device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*sum)[8], char* stage, int lane, int row0, int live, int f, int n_end) {
+__device__ __forceinline__ void blocks_store(const BlocksArgs& g, const OpMaps& maps, f32x2 (*sum)[8], char* stage, int lane, int row0, int live, int f0, int n_end) {
   constexpr int GROUP = COLS < 64 ? COLS : 64;                        // columns at a time: 128 bytes of bf16 (64 where there are 32), or two halves in fp32
-#pragma unroll
+  constexpr bool BOXES = COLS == 128;
+  const bool who = lane == 0, box = BOXES && live == 32 && g.boxes;
+  auto send = [&](const void* tmap, int f) {                          // what all lanes have written (columns behind the width stay where they are)
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (who) box_out(tmap, stage, f, row0);
+  };
+#pragma unroll 1
   for (int p = 0; p < COLS; p += GROUP) {
-    if (f + p >= n_end) break;
+    const int f = f0 + p, cols = n_end - f;
+    if (cols <= 0) break;
     float v[GROUP];
-    finished<GROUP>(g.act, sum + p / 16, v);
+    finished<GROUP>(g.act, sum, v);
     if (g.out16) {
+      if (BOXES) boxes_read(who);
 #pragma unroll
       for (int j = 0; j < GROUP / 8; ++j)
         *reinterpret_cast<uint4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) =
             make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
-      unsigned short* const out = g.out16 + (size_t)row0 * g.n + f + p;
-      const int cols = n_end - f - p;
-      if (g.vec16 == 8) {
+      unsigned short* const out = g.out16 + (size_t)row0 * g.n + f;
+      if (box) {
+        send(&maps.m[2], f);
+      } else if (g.vec16 == 8) {
         rows_in_order<GROUP * 2>(stage, lane, live, 2 * cols, out, 2 * (size_t)g.n);
       } else {                                 // a row at a time, a lane two neighbouring values or one
         __syncwarp();
+#pragma unroll 1
         for (int row = 0; row < live; ++row) {
           if (g.vec16 == 2) {
             if (2 * lane < cols && 2 * lane < GROUP) *reinterpret_cast<uint32_t*>(out + (size_t)row * g.n + 2 * lane) = *reinterpret_cast<const uint32_t*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + 4 * (lane & 3));
@@ -225,65 +252,29 @@ __device__ __forceinline__ void blocks_store(const BlocksArgs& g, const f32x2 (*
     if (g.out32) {
 #pragma unroll
       for (int q = 0; q < GROUP; q += 32) {
-        if (f + p + q >= n_end) break;
+        if (q >= cols) break;
+        if (BOXES) boxes_read(who);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           *reinterpret_cast<float4*>(stage + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_float4(v[q + 4 * j], v[q + 4 * j + 1], v[q + 4 * j + 2], v[q + 4 * j + 3]);
-        float* const out = g.out32 + (size_t)row0 * g.n + f + p + q;
-        const int cols = n_end - f - p - q;
-        if (g.vec32 == 4) {
-          rows_in_order<128>(stage, lane, live, 4 * cols, out, 4 * (size_t)g.n);
+        float* const out = g.out32 + (size_t)row0 * g.n + f + q;
+        if (box) {
+          send(&maps.m[3], f + q);
+        } else if (g.vec32 == 4) {
+          rows_in_order<128>(stage, lane, live, 4 * (cols - q), out, 4 * (size_t)g.n);
         } else {
           __syncwarp();
+#pragma unroll 1
           for (int row = 0; row < live; ++row)
-            if (lane < cols) out[(size_t)row * g.n + lane] = *reinterpret_cast<const float*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + 4 * (lane & 3));
+            if (lane < cols - q) out[(size_t)row * g.n + lane] = *reinterpret_cast<const float*>(stage + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + 4 * (lane & 3));
           __syncwarp();
         }
       }
     }
-  }
-}
-// The same for 128 columns of 32 rows that all exist, as boxes of 32 rows x 128 bytes that the copy engine takes from the stage on its own, the last one
-// while the warp is at the next tile's sums.  (Columns behind the width are not written.)  All CTAs' tiles end at about the same time, and a warp that
-// stores itself waits for memory then.  Of several tiles a CTA: 8192 x 8192 x 2048 in 8 bits to bf16 136 -> 132 us, bf16 8192 x 4096 x 2048 by eight
-// experts to fp32 133 -> 125, 8-bit 16384 x 4096 x 2048 by 32 186 -> 178.
-__device__ __forceinline__ void box_out(const void* tmap, const char* stage, int x, int y) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(smem_u32(stage)), "r"(x), "r"(y) : "memory");
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-__device__ __forceinline__ void boxes_read(bool who) {                // the stage is free again
-  if (who) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-  __syncwarp();
-}
-__device__ __forceinline__ void blocks_store_boxes(const BlocksArgs& g, const OpMaps& maps, const f32x2 (*sum)[8], char* stage, int lane, int row0, int f0) {
-  const bool who = lane == 0;
-  char* const my_row = stage + lane * 128;
-  auto send = [&](const void* tmap, int f) {                          // what all lanes have written
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (who && f < g.n) box_out(tmap, stage, f, row0);
-  };
 #pragma unroll
-  for (int p = 0; p < 128; p += 64) {
-    float v[64];
-    finished<64>(g.act, sum + p / 16, v);
-    if (g.out16) {
-      boxes_read(who);
+    for (int c1 = 0; c1 + GROUP / 16 < COLS / 16; ++c1)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<uint4*>(my_row + ((j ^ (lane & 7)) << 4)) =
-            make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]), pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
-      send(&maps.m[2], f0 + p);
-    }
-    if (g.out32) {
-#pragma unroll
-      for (int q = 0; q < 64; q += 32) {
-        boxes_read(who);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(my_row + ((j ^ (lane & 7)) << 4)) = make_float4(v[q + 4 * j], v[q + 4 * j + 1], v[q + 4 * j + 2], v[q + 4 * j + 3]);
-        send(&maps.m[3], f0 + p + q);
-      }
-    }
+      for (int j = 0; j < 8; ++j) sum[c1][j] = sum[c1 + GROUP / 16][j];
   }
 }
 
@@ -650,12 +641,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
           for (int j = 0; j < 8; ++j) kept[SPLITS ? c1 : 0][j] = sum[c1][j];
         break;
       }
-      if (HALVES && live == 32 && g.boxes) {
-        if constexpr (HALVES) blocks_store_boxes(g, maps, sum, stage, lane, row0, b.n0 + col0);
-      } else {
-        if (HALVES) boxes_read(speaks);
-        blocks_store<OWN * 16>(g, sum, stage, lane, row0, live, b.n0 + (HALVES ? col0 : OWN * 16 * h), min(g.n, b.n0 + g.bn));
-      }
+      blocks_store<OWN * 16>(g, maps, sum, stage, lane, row0, live, b.n0 + (HALVES ? col0 : OWN * 16 * h), min(g.n, b.n0 + g.bn));
     }
     if (HALVES && speaks) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
@@ -687,7 +673,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
         for (int c1 = 0; c1 < OWN; ++c1)
 #pragma unroll
           for (int j = 0; j < 8; ++j) kept[c1][j] = add2(kept[c1][j], pack2(__float_as_uint(from[512 * c1 + 64 * j]), __float_as_uint(from[512 * c1 + 64 * j + 32])));
-      blocks_store<OWN * 16>(g, kept, smem_raw + BLK_SMEM + 4096 * (warp - 4), lane, keep_row0, keep_live, keep_f, keep_end);
+      blocks_store<OWN * 16>(g, maps, kept, smem_raw + BLK_SMEM + 4096 * (warp - 4), lane, keep_row0, keep_live, keep_f, keep_end);
     }
   }
   tc_fence_before();

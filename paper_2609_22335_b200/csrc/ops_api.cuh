@@ -240,8 +240,7 @@ inline int op_linear_blocks_run(int op, const void* a, const float* sa, const vo
   g.err = dev.error_of(op);
   OpMaps maps;
   const int ctas = p.few || !p.pair ? p.ks : 2, room = (p.few ? 2 : 1) * dev.sms / ctas;            // CTAs that share a tile, and such groups at once
-  // (With one tile a CTA nothing goes on while boxes are taken: 817 x 4304 x 1152 with GELU 12.5 us from the warps' own stores, 13.0 as boxes.)
-  g.boxes = p.bn == 256 && p.tiles > room && (!out16 || g.vec16 == 8) && (!out32 || g.vec32 == 4);
+  g.boxes = p.bn == 256 && (!out16 || g.vec16 == 8) && (!out32 || g.vec32 == 4);
   if (g.boxes && out16 && !op_encode(&maps.m[2], out16, rows, n, n, 32)) return VLA_ERR_CUDA;
   if (g.boxes && out32 && !op_encode(&maps.m[3], out32, rows, n, n, 32, 4)) return VLA_ERR_CUDA;
   if (!op_encode(&maps.m[0], w, (int64_t)n * (GROUPED ? experts : 1), k, k, p.pair ? 64 : p.bn, width) || !op_encode(&maps.m[1], a, rows, k, k, p.bm, width)) return VLA_ERR_CUDA;
