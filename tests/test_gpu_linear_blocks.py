@@ -304,11 +304,14 @@ import torch
 from paper_2609_22335_b200 import api
 x, w = torch.randn(70, 512, device="cuda").to(torch.bfloat16), torch.randn(2, 128, 512, device="cuda").to(torch.bfloat16)
 at = torch.tensor([0, 30, 70], dtype=torch.int32, device="cuda")
-g = torch.cuda.CUDAGraph()
-with torch.cuda.graph(g):
-    out = api.op_linear_grouped(x, w, at)
-    q, s = api.op_quantize(x)
+g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+with torch.cuda.graph(g, stream=side):
+    out = api.op_linear_grouped(x, w, at, stream=side)
+    q, s = api.op_quantize(x, stream=side)
+out.fill_(3)
+s.fill_(3)
 g.replay()
+torch.cuda.synchronize()
 assert torch.equal(out, api.op_linear_grouped(x, w, at)) and torch.equal(s, api.op_quantize(x)[1]) and api.op_status(api.OP_LINEAR_GROUPED) == api.VLA_OK
 """
 
