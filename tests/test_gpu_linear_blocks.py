@@ -411,3 +411,28 @@ def test_a_decoder_layer_of_them():
         again, _ = layer(side)
     torch.cuda.synchronize()
     assert torch.equal(again, got)
+
+
+def test_calls_on_two_streams_at_once():
+    """Calls of every kind from two streams, interleaved, with nothing between them but the order of each stream."""
+    import torch
+    from paper_2609_22335_b200 import api
+    a, sa = eight_bit(1, 300, 1024, 1)
+    w, sw = eight_bit(128, 1000, 1024, 2, groups=3)
+    x = torch.randn(300, 1024, device="cuda", generator=gen(3)).to(torch.bfloat16)
+    v = (0.1 * torch.randn(3, 1000, 1024, device="cuda", generator=gen(4))).to(torch.bfloat16)
+    offsets, _ = sort_of([100, 7, 193])
+    few, _ = sort_of([2, 0, 9])
+
+    def calls(s):
+        return [api.op_linear_scaled(a, sa, w[0], sw[0], stream=s), api.op_linear_grouped(x, v, offsets, act=2, stream=s), api.op_linear_grouped_scaled(a, sa, w, sw, offsets, act=1, stream=s),
+                api.op_linear_grouped(x[:11], v, few, out_bf16=True, stream=s), api.op_linear_scaled(a[:1], sa[:1], w[1], sw[1], stream=s), *api.op_quantize(x, stream=s)]
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [calls(streams[i & 1]) for i in range(20)]
+    torch.cuda.synchronize()
+    for each in got:
+        assert all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(each, want))
+    assert [api.op_status(o) for o in (api.OP_LINEAR_SCALED, api.OP_LINEAR_GROUPED, api.OP_LINEAR_GROUPED_SCALED)] == [api.VLA_OK] * 3
