@@ -46,7 +46,7 @@ def test_linear_grouped(lib, mem, f8):
     bads = [dict(a=None), dict(w=None), dict(off=None), dict(o32=None), dict(t=0), dict(n=0), dict(k=0), dict(k=36), dict(experts=0), dict(experts=1025),
             dict(experts=1024, n=1 << 21), dict(act=3), dict(a=p + 8), dict(w=p + 2056), dict(off=p + 4097), dict(t=(1 << 30) + 1)]
     if f8:
-        good = dict(a=p, sa=p + 1024, w=p + 2048, sw=p + 3072, **{k: v for k, v in good.items() if k not in ("a", "w")})
+        good = dict(a=p, sa=p + 1024, w=p + 2048, sw=p + 4096, **{k: v for k, v in good.items() if k not in ("a", "w")})
         call = lib.vla_op_linear_grouped_scaled
         bads += [dict(sa=None), dict(sw=None), dict(k=40), dict(sw=p + 3073)]
     for bad in bads:
