@@ -643,8 +643,8 @@ def op_status(op, scratch=None, stream=None) -> int:
 
 
 def debug_op_fault(drop_operand_loads, wait_limit_ns=0):
-    """Test hook: make the operators' bounded waits run out (see vla_debug_op_fault)."""
-    rc = load_library().vla_debug_op_fault(int(bool(drop_operand_loads)), int(wait_limit_ns))
+    """Test hook: make the operators' bounded waits run out (see vla_debug_op_fault; True is 1)."""
+    rc = load_library().vla_debug_op_fault(int(drop_operand_loads), int(wait_limit_ns))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_debug_op_fault failed")
 

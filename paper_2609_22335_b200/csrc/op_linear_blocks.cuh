@@ -487,6 +487,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
         const BlockTile b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
         if (GROUPED) {
           if (!(ok = blocks_wait(c, heard0 + 8u * told, tph))) break;
+          for (int i = 0; i < 100000 && fault.tell_late && *reinterpret_cast<volatile unsigned*>(&failed_s) == 0u; ++i) __nanosleep(1000);
           __syncwarp();
           if (lane == 0) {
             tiles_s[told] = b;
@@ -530,13 +531,15 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
     uint32_t unit = 0, s = HALVES ? 0u : (uint32_t)h, ph = 0u, slot = 0, lph = 0u, told = 0, tph = 0u;
     int dealt = h;
     for (int t = first; t < tiles && ok; t += step) {
-      BlockTile b;
+      BlockTile b = {0, 0, 0, 0};
       if (GROUPED) {
-        if (!(ok = blocks_wait(c, told0 + 8u * told, tph))) break;
-        b = tiles_s[told];
-        __syncwarp();
-        arrive_if(speaks, heard0 + 8u * told);
-        if (++told == BLK_TOLD) { told = 0; tph ^= 1u; }
+        // (A warp that gives up goes on without rows to where the two of a quarter meet: the other one may have been told all the same.)
+        if ((ok = blocks_wait(c, told0 + 8u * told, tph))) {
+          b = tiles_s[told];
+          __syncwarp();
+          arrive_if(speaks, heard0 + 8u * told);
+          if (++told == BLK_TOLD) { told = 0; tph ^= 1u; }
+        }
       } else {
         b = blocks_tile<GROUPED>(g, experts, t, tile_rows);
       }

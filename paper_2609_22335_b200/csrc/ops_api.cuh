@@ -48,9 +48,10 @@ inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t 
 struct OpFault {
   unsigned long long wait_limit_ns;
   int drop_loads;
+  int tell_late;                               // places of experts' tiles are told only once a wait has run out
 };
 inline OpFault& op_fault() {
-  static OpFault f = {2000000000ull, 0};
+  static OpFault f = {2000000000ull, 0, 0};
   return f;
 }
 
@@ -392,6 +393,7 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
 
 int vla_debug_op_fault(int32_t drop_operand_loads, uint64_t wait_limit_ns) {
   vla::op_fault().drop_loads = drop_operand_loads ? 1 : 0;
+  vla::op_fault().tell_late = drop_operand_loads == 2 ? 1 : 0;
   vla::op_fault().wait_limit_ns = wait_limit_ns ? wait_limit_ns : 2000000000ull;
   return VLA_OK;
 }

@@ -1,0 +1,19 @@
+"""The shapes of the tests that are about a kernel of the linear layers by blocks, and not about a size, reach all of these kernels."""
+import pytest
+
+from test_blocks_plan import kernel_of, plan  # noqa: F401  (a fixture)
+
+KERNELS = [("pair",), ("wide",), ("middle",)] + [("narrow", ks) for ks in (1, 2, 4)] + [("few", h, ks) for h in (16, 32, 64) for ks in (1, 2)] + [("few", 64, 4), ("few", 16, 4), ("few", 16, 8)]
+
+
+def taken(plan, scaled, grouped):
+    return ({("scaled",) + kernel_of(plan(m, n, -(-k // 128))) for m, n, k in scaled} |
+            {("grouped",) + kernel_of(plan(sum(c), n, -(-k // 64), len(c), False)) for c, n, k in grouped} |
+            {("grouped_scaled",) + kernel_of(plan(sum(c), n, -(-k // 128), len(c), True)) for c, n, k in grouped})
+
+
+@pytest.mark.parametrize("op", ["scaled", "grouped", "grouped_scaled"])
+def test_waits_that_run_out(plan, op):  # noqa: F811
+    import test_gpu_blocks_waits as T
+    seen = taken(plan, T.SCALED, T.GROUPED)
+    assert not [k for k in KERNELS if (op,) + k not in seen]
