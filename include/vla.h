@@ -327,8 +327,8 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
                         const float* gain_k, float eps, const int32_t* pos, int32_t pos0, int32_t rot, float base,
                         int32_t interleaved, void* stream);
 
-/* Every device-side wait of the operators is bounded (2 s by default); a wait that runs out makes the kernel set
- * the call's error word and return, leaving garbage in the output.  vla_op_status waits for `stream` to drain and
+/* Every device-side wait of the operators is bounded (2 s by default, each of them: a call may take longer); a wait that
+ * runs out makes the kernel set the call's error word and return, leaving garbage in the output.  vla_op_status waits for `stream` to drain and
  * reads that word back: VLA_OK, or VLA_ERR_TIMEOUT when a wait ran out.  op selects the word: VLA_OP_LINEAR (one
  * word per device, shared by all vla_op_linear calls on it: query before another call reuses it), VLA_OP_ATTENTION
  * (the word at the start of `scratch`, DEVICE), VLA_OP_ATTENTION_STATIC (the library's fixed array), or VLA_OP_LINEAR_SCALED,

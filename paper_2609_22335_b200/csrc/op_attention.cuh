@@ -81,9 +81,7 @@ __global__ void __launch_bounds__(OPA_THREADS, TERMS) vla_op_attention_kernel(co
   }
   op_wait_previous(maps, 3);
   if (threadIdx.x == 0 && blockIdx.x == 0) *err = 0u;
-  TileCtx c;                                    // (what the bounded waits look at)
-  c.error = &failed_s;
-  c.deadline = gtimer() + fault.wait_limit_ns;
+  const OpWaits c = {&failed_s, fault.wait_limit};
   tc_fence_before();
   __syncthreads();
   op_let_next_start();

@@ -165,9 +165,7 @@ __global__ void __launch_bounds__(LIN_THREADS, 2) vla_op_linear_kernel(const __g
   }
   op_wait_previous(maps, 2);
   if (threadIdx.x == 0 && blockIdx.x == 0) *g.err = 0u;
-  TileCtx c;                                   // (what the bounded waits look at)
-  c.error = &failed_s;
-  c.deadline = gtimer() + fault.wait_limit_ns;
+  const OpWaits c = {&failed_s, fault.wait_limit};
   tc_fence_before();
   __syncthreads();
   op_let_next_start();

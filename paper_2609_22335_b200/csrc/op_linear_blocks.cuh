@@ -283,7 +283,7 @@ struct BlocksNo { static constexpr bool value = false; };
 
 // What stands between two units is branches and barriers: a branch costs a warp that has its scheduler nearly to itself some 30 cycles, a look at a
 // barrier 61 (92 with a time to sleep).  So a wait looks once before it goes to sleep, arrivals are predicated, and loops over columns have no ends of their own.
-__device__ __forceinline__ bool blocks_wait(const TileCtx& c, uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool blocks_wait(const OpWaits& c, uint32_t bar, uint32_t parity) {
   uint32_t there;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -380,9 +380,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   op_wait_previous(maps, 2);
   if (threadIdx.x == 0 && blockIdx.x == 0) *g.err = 0u;
   if (GROUPED && warp == 2) blocks_lay_out(g, experts, lane, PAIR ? 2 * g.bm : g.bm);
-  TileCtx c;                                   // (what the bounded waits look at)
-  c.error = &failed_s;
-  c.deadline = gtimer() + fault.wait_limit_ns;
+  const OpWaits c = {&failed_s, fault.wait_limit};
   tc_fence_before();
   __syncthreads();
   op_let_next_start();

@@ -66,9 +66,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) vla_op_linear_few_kernel(const
   op_wait_previous(maps, 2);
   if (threadIdx.x == 0 && blockIdx.x == 0) *g.err = 0u;
   if (GROUPED && warp == 2) blocks_lay_out(g, experts, lane, ROWS);
-  TileCtx c;                                   // (what the bounded waits look at)
-  c.error = &failed_s;
-  c.deadline = gtimer() + fault.wait_limit_ns;
+  const OpWaits c = {&failed_s, fault.wait_limit};
   tc_fence_before();
   __syncthreads();
   op_let_next_start();
@@ -171,7 +169,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) vla_op_linear_few_kernel(const
           for (int i = 0; i < 8; i += 2) {
             const f32x2 x = pack2(v[2 * i], v[2 * i + 1]), y = pack2(v[2 * i + 2], v[2 * i + 3]);
             if (F8) {
-              const uint4 a = *reinterpret_cast<const uint4*>(&scales_s[s][16 * q + 2 * i]);
+              uint4 a;                          // (volatile: read here, not all of them ahead, which 128 registers have no room for beside the sums)
+              asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w) : "r"(smem_u32(&scales_s[s][16 * q + 2 * i])));
               sum[8 * q + i] = fma2(x, mul2(pack2(a.x, a.y), w2), sum[8 * q + i]);
               sum[8 * q + i + 1] = fma2(y, mul2(pack2(a.z, a.w), w2), sum[8 * q + i + 1]);
             } else {

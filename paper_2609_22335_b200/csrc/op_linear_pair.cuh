@@ -70,9 +70,7 @@ __global__ void __launch_bounds__(LIN_THREADS, 1) vla_op_linear_pair_kernel(cons
   tc_fence_after();
   op_wait_previous(maps, 2);
   if (threadIdx.x == 0 && blockIdx.x == 0) *g.err = 0u;
-  TileCtx c;                                   // (what the bounded waits look at)
-  c.error = &failed_s;
-  c.deadline = gtimer() + fault.wait_limit_ns;
+  const OpWaits c = {&failed_s, fault.wait_limit};
   op_let_next_start();
   const uint32_t tmem = tmem_base_s;
   // An accumulator for each of the parts K is summed in, and where there is room two sets of them.

@@ -44,15 +44,35 @@ inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t 
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+constexpr uint64_t OP_WAIT_LIMIT_NS = 2000000000ull;
 // Bound of the operators' device-side waits, and the test hook that makes one run out (vla_debug_op_fault).
 struct OpFault {
-  unsigned long long wait_limit_ns;
+  uint32_t wait_limit;                         // in 1024 ns
   int drop_loads;
   int tell_late;                               // places of experts' tiles are told only once a wait has run out
 };
 inline OpFault& op_fault() {
-  static OpFault f = {2000000000ull, 0, 0};
+  static OpFault f = {(uint32_t)(OP_WAIT_LIMIT_NS >> 10), 0, 0};
   return f;
+}
+
+// What an operator's waits look at: the CTA's word, set by the first of them that runs out, and how long one may take.  Each is bounded by itself: a call
+// may run for as long as it has work.
+struct OpWaits {
+  unsigned* error;
+  uint32_t limit;                              // in 1024 ns
+};
+__device__ __forceinline__ bool mbar_wait(const OpWaits& c, uint32_t bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity, 20000u)) return true;              // (a wait that is over at the first look, or within its sleep, reads no clock)
+  const uint32_t until = (uint32_t)(gtimer() >> 10) + c.limit;        // 1024 ns each, in one register
+  while (!mbar_try_wait(bar, parity, 20000u)) {
+    if (*reinterpret_cast<volatile unsigned*>(c.error) != 0u) return false;
+    if ((int)((uint32_t)(gtimer() >> 10) - until) > 0) {
+      atomicCAS(c.error, 0u, (unsigned)DEV_ERR_WAIT_MBAR);
+      return false;
+    }
+  }
+  return true;
 }
 
 // Start of an operator kernel.  A call's kernel is launched while the previous one on the stream is still running (programmatic
@@ -394,7 +414,8 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
 int vla_debug_op_fault(int32_t drop_operand_loads, uint64_t wait_limit_ns) {
   vla::op_fault().drop_loads = drop_operand_loads ? 1 : 0;
   vla::op_fault().tell_late = drop_operand_loads == 2 ? 1 : 0;
-  vla::op_fault().wait_limit_ns = wait_limit_ns ? wait_limit_ns : 2000000000ull;
+  const uint64_t limit = (wait_limit_ns ? wait_limit_ns : vla::OP_WAIT_LIMIT_NS) >> 10;
+  vla::op_fault().wait_limit = limit < INT32_MAX ? (uint32_t)limit : INT32_MAX;
   return VLA_OK;
 }
 

@@ -27,7 +27,7 @@ inline int run_tile_hook(TileHookBlock& h, int n_maps) {
   memset(&ctx, 0, sizeof ctx);    // (no arena: the Refs of a hook are absolute device addresses)
   ctx.nodes = &d->node; ctx.control = &d->control; ctx.error_host = &d->error_mirror;
   ctx.tmaps = d->maps; ctx.n_weight_tmaps = h.node.op == OP_GEMM ? 1 : 0; ctx.n_act_tmaps = n_maps - ctx.n_weight_tmaps;
-  ctx.wait_limit_ns = op_fault().wait_limit_ns; ctx.drop_loads = op_fault().drop_loads;
+  ctx.wait_limit_ns = (uint64_t)op_fault().wait_limit << 10; ctx.drop_loads = op_fault().drop_loads;
   cudaError_t e = cudaDeviceSynchronize();          // the caller's tensors are complete
   if (e == cudaSuccess) e = cudaMemcpy(d, &h, sizeof h, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) {
