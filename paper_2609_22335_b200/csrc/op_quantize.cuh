@@ -92,7 +92,9 @@ struct QuantBlock {
   bool plain;
   __device__ __forceinline__ void set(unsigned amax_bits) {
     const float a = __uint_as_float(amax_bits);
-    plain = amax_bits >= 0x12800000u && amax_bits < 0x7E000000u;      // 2^-90 to 2^125
+    // 2^-84 to 2^125.  (s is 2^-93 or more, so the remainder of a quotient that counts, 2^-10 and more, is a multiple of 2^-93-23-10-23 and no subnormal
+    // number has to round it.)
+    plain = amax_bits >= 0x15800000u && amax_bits < 0x7E000000u;
     if (!F32 && plain) {
       constexpr float c = 1.0f / E4M3_MAX;
       const float q0 = a * c;
