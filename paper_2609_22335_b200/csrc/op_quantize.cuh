@@ -110,15 +110,18 @@ struct QuantBlock {
   __device__ __forceinline__ uint2 eight(const float* f, bool all_plain) const {       // (two values an instruction)
     uint32_t w[4];
     if (all_plain) {
-      const f32x2 y2 = pack2(__float_as_uint(y), __float_as_uint(y)), m2 = pack2(__float_as_uint(-s), __float_as_uint(-s));
+      // The negative quotient: the remainder of a zero is +0, so the step from the quotient itself would make +0 of -0, where a division keeps the sign; from the
+      // negative one it leaves either zero as it is.  The bytes' signs are turned back at the end.
+      const f32x2 y2 = pack2(__float_as_uint(-y), __float_as_uint(-y)), s2 = pack2(__float_as_uint(s), __float_as_uint(s));
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const f32x2 x = pack2(__float_as_uint(f[2 * j]), __float_as_uint(f[2 * j + 1])), q0 = mul2(x, y2);
-        f32x2 q = fma2(fma2(q0, m2, x), y2, q0);
-        if (F32) q = fma2(fma2(q, m2, x), y2, q);
+        f32x2 q = fma2(fma2(q0, s2, x), y2, q0);
+        if (F32) q = fma2(fma2(q, s2, x), y2, q);
         const float2 r = unpack2(q);
         w[j] = e4m3_pair(r.x, r.y);
       }
+      return make_uint2((w[0] | (w[1] << 16)) ^ 0x80808080u, (w[2] | (w[3] << 16)) ^ 0x80808080u);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = e4m3_pair(__fdiv_rn(f[2 * j], s), __fdiv_rn(f[2 * j + 1], s));

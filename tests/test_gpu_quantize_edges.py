@@ -47,3 +47,24 @@ def test_quotients_next_to_ties_over_small_scales(rows):
     if rows == 128:                                              # (a block of 128 x 128 for each)
         x = np.concatenate([np.pad(b[None], ((0, 127), (0, 0))) for b in x])
     same(x, rows)
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("k", [128, 384, 1152, 2048])
+def test_zeros_keep_their_sign_whatever_is_beside_them(k, bf16, rows):
+    """Zeros of both signs, and values that become zero, in blocks of every kind: ordinary, all zero, tiny, with an infinity or a NaN."""
+    import torch
+    rng = np.random.default_rng(k)
+    x = rng.standard_normal((1500, k)).astype(np.float32)
+    x[rng.random(x.shape) < 0.2] = 0.0
+    x[rng.random(x.shape) < 0.1] *= np.float32(1e-5)
+    kinds = rng.integers(0, 8, (1500 if rows == 1 else -(-1500 // 128), k // 128)).repeat(rows, 0)[:1500].repeat(128, 1)
+    x[kinds == 0] = 0.0
+    x[kinds == 1] *= np.float32(1e-33)
+    x[(kinds == 2) & (rng.random(x.shape) < 0.01)] = np.inf
+    x[(kinds == 3) & (rng.random(x.shape) < 0.01)] = np.nan
+    x = np.where(rng.random(x.shape) < 0.5, -x, x)
+    if bf16:
+        x = torch.from_numpy(x).to(torch.bfloat16).float().numpy()
+    same(x, rows, bf16)
