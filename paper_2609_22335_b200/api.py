@@ -422,8 +422,22 @@ def policy_probe(taus, pending, feasible, cta_count, u, rr_start=0, u_max=0, pol
     return picked.value, phase.value, list(cc), list(uu)
 
 
+_current_stream = None
+
+
+def _look_up_current_stream():
+    """A function that asks torch for the current stream's handle.  (torch.cuda.current_stream() makes an object: a tenth of a small call's time.)"""
+    global _current_stream
+    import torch
+    torch.cuda.init()
+    of, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    _current_stream = lambda: of(device())                                       # noqa: E731
+    return _current_stream
+
+
 def _stream_ptr(stream):
-    return None if stream is None else stream.cuda_stream
+    """The stream a call runs on: the one given or, for None, torch's current one (of the current device), behind the work that made the call's inputs."""
+    return (_current_stream or _look_up_current_stream())() if stream is None else stream.cuda_stream
 
 
 def op_attention_scratch_bytes(tkv, hkv, hd) -> int:
@@ -435,7 +449,8 @@ def op_attention_scratch_bytes(tkv, hkv, hd) -> int:
 
 
 def op_attention(q, k, v, hq, hkv, hd, causal=False, scratch=None, stream=None):
-    """q [tq, hq*hd], k/v [tkv, hkv*hd]: CUDA bf16 torch tensors.  Returns out [tq, hq*hd] bf16."""
+    """q [tq, hq*hd], k/v [tkv, hkv*hd]: CUDA bf16 torch tensors.  Returns out [tq, hq*hd] bf16.  (Like every op_* below: on ``stream``, a
+    torch.cuda.Stream, or on torch's current one.)"""
     import torch
     tq, tkv = q.shape[0], k.shape[0]
     out = torch.empty_like(q)
@@ -460,7 +475,7 @@ def op_linear(a, w, act=0, out_bf16=False, stream=None):
         out = a.new_empty((m, n), dtype=torch.float32)
         p32, p16 = out.data_ptr(), None
     rc = (_lib or load_library()).vla_op_linear(a.data_ptr(), w.data_ptr(), p32, p16, m, n, k, act,
-                                                None if stream is None else stream.cuda_stream)
+                                                _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_linear failed")
     return out
@@ -499,7 +514,7 @@ def _elsewhere(first, *others):
 
 
 def _new(stream, shape, dtype, like):
-    """A result: memory of the stream that writes it, so that it is not handed out again while that one still runs."""
+    """A result: memory of the stream that writes it (None: the current one), so that it is not handed out again while that one still runs."""
     if stream is None:
         return like.new_empty(shape, dtype=dtype)
     import torch
@@ -521,7 +536,7 @@ def op_quantize(x, block_rows=1, stream=None):
     q = _new(stream, (m, k), torch.float8_e4m3fn, x)
     s = _new(stream, (m if block_rows == 1 else (m + 127) // 128, (k + 127) // 128), torch.float32, x)
     rc = (_lib or load_library()).vla_op_quantize(x.data_ptr(), int(f32), ld if m > 1 else k, q.data_ptr(), s.data_ptr(), m, k, block_rows,
-                                                  None if stream is None else stream.cuda_stream)
+                                                  _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_quantize failed")
     return q, s
@@ -551,7 +566,7 @@ def _blocks(name, a, scale_a, w, scale_w, offsets, out, act, out_bf16, stream):
         out = _new(stream, (m, n), result, a)
     elif out.shape != (m, n) or out.dtype != result or not out.is_contiguous():
         _refuse(name, "out is contiguous, [rows,n], fp32 or, with out_bf16, bf16")
-    return m, n, k, out, (None, out.data_ptr()) if out_bf16 else (out.data_ptr(), None), None if stream is None else stream.cuda_stream
+    return m, n, k, out, (None, out.data_ptr()) if out_bf16 else (out.data_ptr(), None), _stream_ptr(stream)
 
 
 def op_linear_scaled(a, scale_a, w, scale_w, act=0, out_bf16=False, stream=None):
@@ -631,14 +646,14 @@ def op_qk_norm_rope(q, k, hq, hkv, hd, gq=None, gk=None, eps=1e-6, pos=None, pos
     rc = (_lib or load_library()).vla_op_qk_norm_rope(q.data_ptr(), ptr_k, int(dt == f32), ld_q, ld_k, out_q.data_ptr(), ptr_ok, ld_oq, ld_ok, t, hq, hkv, hd,
                                                       None if gq is None else gq.data_ptr(), None if gk is None else gk.data_ptr(), eps,
                                                       None if pos is None else pos.data_ptr(), pos0, hd if rot is None else rot, base, int(interleaved),
-                                                      None if stream is None else stream.cuda_stream)
+                                                      _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_qk_norm_rope failed")
     return out_q, out_k
 
 
 def op_status(op, scratch=None, stream=None) -> int:
-    """Waits for ``stream`` and returns the operator's status word as a VLA_* code (VLA_OK or VLA_ERR_TIMEOUT)."""
+    """Waits for ``stream`` (None: torch's current one) and returns the operator's status word as a VLA_* code (VLA_OK or VLA_ERR_TIMEOUT)."""
     return load_library().vla_op_status(op, None if scratch is None else scratch.data_ptr(), _stream_ptr(stream))
 
 
