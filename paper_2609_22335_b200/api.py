@@ -455,7 +455,7 @@ def op_attention(q, k, v, hq, hkv, hd, causal=False, scratch=None, stream=None):
     tq, tkv = q.shape[0], k.shape[0]
     out = torch.empty_like(q)
     if scratch is None:
-        scratch = torch.empty(op_attention_scratch_bytes(tkv, hkv, hd), dtype=torch.uint8, device=q.device)
+        scratch = _new(stream, (op_attention_scratch_bytes(tkv, hkv, hd),), torch.uint8, q)       # (goes back to its stream's memory when this returns)
     rc = load_library().vla_op_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), tq, tkv, hq, hkv, hd,
                                          int(causal), scratch.data_ptr(), scratch.numel(), _stream_ptr(stream))
     if rc != VLA_OK:

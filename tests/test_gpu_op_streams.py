@@ -84,3 +84,22 @@ def test_status_waits_for_the_current_stream():
         late(inputs, values, side)
         call()
         assert api.op_status(api.OP_LINEAR_SCALED) == api.VLA_OK and side.query()
+
+
+def test_attentions_own_scratch_is_memory_of_its_stream():
+    """What the call allocates for itself goes back when it returns; it must not be handed to another stream before the kernel has written it."""
+    import torch
+    from paper_2609_22335_b200 import api
+    q, k = torch.randn(70, 256, device="cuda").to(torch.bfloat16), torch.randn(70, 128, device="cuda").to(torch.bfloat16)
+    n = api.op_attention_scratch_bytes(70, 2, 64)
+    api.op_attention(q, k, k, 4, 2, 64)
+    torch.full((n,), 7, dtype=torch.uint8, device="cuda")        # (kernels are loaded on their first call, which takes a while)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    got = api.op_attention(q, k, k, 4, 2, 64, stream=side)
+    mine = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    torch.cuda.synchronize()
+    assert all(bool((m == 7).all()) for m in mine) and got.shape == q.shape
