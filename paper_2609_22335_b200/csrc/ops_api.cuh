@@ -384,6 +384,7 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
   using namespace vla;
   if (!q || !out_q || t < 1 || hq < 1 || hkv < 0 || hd < 16 || hd > 256 || hd % 16 || rot < 0 || rot > hd || rot % 16) return VLA_ERR_INVALID;
   if (hq > 65536 || hkv > 65536 || (hkv > 0 && (!k || !out_k)) || !(eps >= 0.0f) || !(eps < 1e30f) || !(base > 1.0f) || !(base < 1e30f)) return VLA_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(gain_q) | reinterpret_cast<uintptr_t>(gain_k) | reinterpret_cast<uintptr_t>(pos)) & 3) return VLA_ERR_INVALID;
   const int width = in_f32 ? 4 : 2;
   const auto bad = [](const void* p, int64_t ld, int64_t least, int w) { return ld < least || ld * w % 16 || (reinterpret_cast<uintptr_t>(p) & 15); };
   if (bad(q, ld_q, (int64_t)hq * hd, width) || bad(out_q, ld_out_q, (int64_t)hq * hd, 2)) return VLA_ERR_INVALID;
