@@ -276,7 +276,7 @@ int vla_op_attention_static(const void* q, const void* k, const void* v, void* o
                             int32_t hkv, int32_t hd, int32_t causal, void* stream);
 
 /* Linear layer y = act(x W^T) -- the dense contractions of both phases (Section 2.1; Section 2.3 calls them the
- * VLM's "large GEMMs").  a [m,k] and w [n,k] bf16 row-major DEVICE; k a multiple of 8; fp32 accumulation.
+ * VLM's "large GEMMs").  a [m,k] and w [n,k] bf16 row-major DEVICE, 16-byte aligned; k a multiple of 8; fp32 accumulation.
  * out32 (fp32 [m,n]) and/or out16 (bf16 [m,n]) DEVICE, either may be NULL.  act: 0 none, 1 GeLU (tanh form), 2 SiLU. */
 int vla_op_linear(const void* a, const void* w, float* out32, void* out16, int32_t m, int32_t n, int32_t k, int32_t act,
                   void* stream);

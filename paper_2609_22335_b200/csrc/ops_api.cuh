@@ -4,6 +4,7 @@
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
+#include <initializer_list>
 
 #include "../../include/vla.h"
 #include "dispatch.cuh"
@@ -184,6 +185,12 @@ inline bool op_attention_shape_ok(int tq, int tkv, int hq, int hkv, int hd) {
   return tq >= 1 && tkv >= 1 && hq >= 1 && hkv >= 1 && hq % hkv == 0 && hd >= 16 && hd <= 256 && hd % 16 == 0;
 }
 
+inline bool op_aligned(int bytes, std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) return false;
+  return true;
+}
+
 inline size_t op_attention_scratch_bytes(int tkv, int hkv, int hd) {
   return OP_ATTN_HEADER + (size_t)hkv * hd * (size_t)op_pad(tkv, 64) * 2;
 }
@@ -295,7 +302,7 @@ int vla_op_attention_scratch_bytes(int32_t tkv, int32_t hkv, int32_t hd, size_t*
 int vla_op_attention(const void* q, const void* k, const void* v, void* out, int32_t tq, int32_t tkv, int32_t hq, int32_t hkv,
                      int32_t hd, int32_t causal, void* scratch, size_t scratch_bytes, void* stream) {
   if (!q || !k || !v || !out || !scratch || !vla::op_attention_shape_ok(tq, tkv, hq, hkv, hd)) return VLA_ERR_INVALID;
-  if (causal && tq != tkv) return VLA_ERR_INVALID;
+  if ((causal && tq != tkv) || !vla::op_aligned(16, {q, k, v, out})) return VLA_ERR_INVALID;
   if (scratch_bytes < vla::op_attention_scratch_bytes(tkv, hkv, hd) || (reinterpret_cast<uintptr_t>(scratch) & 255))
     return VLA_ERR_NOMEM;
   return vla::op_attention_run(q, k, v, out, tq, tkv, hq, hkv, hd, causal, scratch, static_cast<cudaStream_t>(stream));
@@ -305,6 +312,7 @@ int vla_op_linear(const void* a, const void* w, float* out32, void* out16, int32
                   void* stream) {
   using namespace vla;
   if (!a || !w || (!out32 && !out16) || m < 1 || n < 1 || k < 8 || k % 8 || act < 0 || act > 2) return VLA_ERR_INVALID;
+  if (!op_aligned(16, {a, w}) || !op_aligned(4, {out32}) || !op_aligned(2, {out16})) return VLA_ERR_INVALID;
   OpDevice dev;
   if (!op_device(&dev)) return VLA_ERR_CUDA;
   LinearArgs g;
@@ -384,7 +392,7 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
   using namespace vla;
   if (!q || !out_q || t < 1 || hq < 1 || hkv < 0 || hd < 16 || hd > 256 || hd % 16 || rot < 0 || rot > hd || rot % 16) return VLA_ERR_INVALID;
   if (hq > 65536 || hkv > 65536 || (hkv > 0 && (!k || !out_k)) || !(eps >= 0.0f) || !(eps < 1e30f) || !(base > 1.0f) || !(base < 1e30f)) return VLA_ERR_INVALID;
-  if ((reinterpret_cast<uintptr_t>(gain_q) | reinterpret_cast<uintptr_t>(gain_k) | reinterpret_cast<uintptr_t>(pos)) & 3) return VLA_ERR_INVALID;
+  if (!op_aligned(4, {gain_q, gain_k, pos})) return VLA_ERR_INVALID;
   const int width = in_f32 ? 4 : 2;
   const auto bad = [](const void* p, int64_t ld, int64_t least, int w) { return ld < least || ld * w % 16 || (reinterpret_cast<uintptr_t>(p) & 15); };
   if (bad(q, ld_q, (int64_t)hq * hd, width) || bad(out_q, ld_out_q, (int64_t)hq * hd, 2)) return VLA_ERR_INVALID;

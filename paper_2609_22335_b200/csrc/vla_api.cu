@@ -899,7 +899,7 @@ int vla_op_attention_static_capacity(size_t* out_bytes) {
 int vla_op_attention_static(const void* q, const void* k, const void* v, void* out, int32_t tq, int32_t tkv, int32_t hq,
                             int32_t hkv, int32_t hd, int32_t causal, void* stream) {
   if (!q || !k || !v || !out || !vla::op_attention_shape_ok(tq, tkv, hq, hkv, hd)) return VLA_ERR_INVALID;
-  if (causal && tq != tkv) return VLA_ERR_INVALID;
+  if ((causal && tq != tkv) || !vla::op_aligned(16, {q, k, v, out})) return VLA_ERR_INVALID;
   if (vla::op_attention_scratch_bytes(tkv, hkv, hd) > sizeof(g_attention_static_scratch)) return VLA_ERR_NOMEM;
   void* scratch = nullptr;
   int rc = static_scratch_for_current_device(&scratch);
