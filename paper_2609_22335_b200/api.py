@@ -531,8 +531,8 @@ def op_quantize(x, block_rows=1, stream=None):
         _refuse("op_quantize", "x is a bf16 or fp32 matrix on the current CUDA device")
     m, k = x.shape
     ld, step = x.stride()
-    if m < 1 or k < 16 or k % 16 or step != 1 or (block_rows != 1 and block_rows != 128):
-        _refuse("op_quantize", "rows in one piece, at least one, k a multiple of 16, block_rows 1 or 128")
+    if m < 1 or k < 16 or k % 16 or step != 1 or (block_rows != 1 and block_rows != 128) or (m | k) >> 31:
+        _refuse("op_quantize", "rows in one piece, at least one, k a multiple of 16, below 2^31 of either, block_rows 1 or 128")
     q = _new(stream, (m, k), torch.float8_e4m3fn, x)
     s = _new(stream, (m if block_rows == 1 else (m + 127) // 128, (k + 127) // 128), torch.float32, x)
     rc = (_lib or load_library()).vla_op_quantize(x.data_ptr(), int(f32), ld if m > 1 else k, q.data_ptr(), s.data_ptr(), m, k, block_rows,
@@ -552,8 +552,8 @@ def _blocks(name, a, scale_a, w, scale_w, offsets, out, act, out_bf16, stream):
     m, k = a.shape
     shape = w.shape
     n = shape[-2]
-    if shape[-1] != k or not a.is_contiguous() or not w.is_contiguous():
-        _refuse(name, "a and w are contiguous, rows of the same k")
+    if shape[-1] != k or not a.is_contiguous() or not w.is_contiguous() or (m | n | k | shape[0]) >> 31:
+        _refuse(name, "a and w are contiguous, rows of the same k, all sizes below 2^31")
     if scale_a is not None:
         kb, nb = (k + 127) // 128, (n + 127) // 128
         if (scale_a.shape != (m, kb) or scale_w.shape != ((shape[0], nb, kb) if grouped else (nb, kb)) or scale_a.dtype != torch.float32 or
@@ -612,8 +612,10 @@ def op_qk_norm_rope(q, k, hq, hkv, hd, gq=None, gk=None, eps=1e-6, pos=None, pos
     t, wq = q.shape
     ld_q, step = q.stride()
     wk, ld_k, ptr_k, ld_ok, ptr_ok = hkv * hd, 0, None, 0, None
-    if wq != hq * hd or step != 1 or t < 1:
-        _refuse(name, "q is [t, hq*hd], rows in one piece, at least one")
+    if wq != hq * hd or step != 1 or t < 1 or (t | wq) >> 31:
+        _refuse(name, "q is [t, hq*hd], rows in one piece, at least one, below 2^31 of either")
+    if pos0 >> 31 not in (0, -1):
+        _refuse(name, "pos0 is a 32-bit number")
     if k is not None:
         if k.dtype != dt or k.shape != (t, wk) or k.stride(1) != 1:
             _refuse(name, "k is [t, hkv*hd], of q's type, rows in one piece")
