@@ -17,3 +17,21 @@ def test_waits_that_run_out(plan, op):  # noqa: F811
     import test_gpu_blocks_waits as T
     seen = taken(plan, T.SCALED, T.GROUPED)
     assert not [k for k in KERNELS if (op,) + k not in seen]
+
+
+@pytest.mark.parametrize("op", ["grouped", "grouped_scaled"])
+def test_rows_of_nobody(plan, op):  # noqa: F811
+    """The same shapes with the rows in front of the first expert and behind the last."""
+    import test_gpu_blocks_every_kernel as T
+    seen = set()
+    for c, n, k in T.GROUPED:
+        f8 = op == "grouped_scaled"
+        seen.add((op,) + kernel_of(plan(sum(c) + T.LEAD + T.REST, n, -(-k // (128 if f8 else 64)), len(c), f8)))
+    assert not [k for k in KERNELS if (op,) + k not in seen]
+
+
+def test_long_sums(plan):  # noqa: F811
+    """Every width of bf16, and operands exchanged at every height."""
+    import test_gpu_blocks_every_kernel as T
+    seen = {kernel_of(plan(sum(c), n, -(-k // 64), len(c), False))[:2] for c, n, k in T.LONG}
+    assert {("few", 16), ("few", 32), ("few", 64), ("pair",), ("wide",), ("middle",)} <= seen and any(k[0] == "narrow" for k in seen)
