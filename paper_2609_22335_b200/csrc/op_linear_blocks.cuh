@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
   // this CTA's k-blocks: whole spans
   const int spans = (g.nkb + SPAN - 1) / SPAN, k0 = SPLITS ? spans * part / ks * SPAN : 0, nkb = SPLITS ? min(spans * (part + 1) / ks * SPAN, g.nkb) - k0 : g.nkb;
   bool ok = true, keep = false;                // (a tile whose K is split: what a warp of sums keeps for its end)
-  int keep_row0 = 0, keep_live = 0, keep_f = 0, keep_end = 0;
+  BlockTile kept_at = {0, 0, 0, 0};
   f32x2 kept[SPLITS ? OWN : 1][8];
   if (warp < 4) {
     if (ACC_COLS == 128) regs_dec<BLK_REGS_SERVICE>();
@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
       }
       if (SPLITS && ks > 1) {                  // one tile a cluster: what is left to do needs the others
         keep = true;
-        keep_row0 = row0; keep_live = live; keep_f = b.n0 + OWN * 16 * h; keep_end = min(g.n, b.n0 + g.bn);
+        kept_at = b;
 #pragma unroll
         for (int c1 = 0; c1 < OWN; ++c1)
 #pragma unroll
@@ -675,7 +675,9 @@ __global__ void __launch_bounds__(BLK_THREADS, 1) vla_op_linear_blocks_kernel(co
         for (int c1 = 0; c1 < OWN; ++c1)
 #pragma unroll
           for (int j = 0; j < 8; ++j) kept[c1][j] = add2(kept[c1][j], pack2(__float_as_uint(from[512 * c1 + 64 * j]), __float_as_uint(from[512 * c1 + 64 * j + 32])));
-      blocks_store<OWN * 16>(g, maps, kept, smem_raw + BLK_SMEM + 4096 * (warp - 4), lane, keep_row0, keep_live, keep_f, keep_end);
+      const int quarter = warp & 3;
+      blocks_store<OWN * 16>(g, maps, kept, smem_raw + BLK_SMEM + 4096 * (warp - 4), lane, kept_at.row0 + 32 * quarter, min(32, min(g.bm, kept_at.row_end - kept_at.row0) - 32 * quarter),
+                             kept_at.n0 + OWN * 16 * ((warp >> 2) - 1), min(g.n, kept_at.n0 + g.bn));
     }
   }
   tc_fence_before();
