@@ -339,7 +339,7 @@ enum { VLA_OP_LINEAR = 0, VLA_OP_ATTENTION = 1, VLA_OP_ATTENTION_STATIC = 2, VLA
 int vla_op_status(int32_t op, const void* scratch, void* stream);
 
 /* Test hook: while drop_operand_loads is non-zero the operators' TMA producers issue no loads, so their consumers
- * wait for operands that never come and the bounded waits (wait_limit_ns; 0 = the default 2 s) run out.  2: beside that the
+ * wait for operands that never come and the bounded waits (wait_limit_ns, in steps of 1024; 0 = the default 2 s) run out.  2: beside that the
  * layers grouped by expert tell their summing warps where a tile is only once one of them has given up waiting for it.
  * Process-wide; call with (0, 0) to restore normal operation. */
 int vla_debug_op_fault(int32_t drop_operand_loads, uint64_t wait_limit_ns);

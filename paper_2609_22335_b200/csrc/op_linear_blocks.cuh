@@ -4,7 +4,7 @@
 //   y[i, j] = act( sum_b  s_a[i, b] s_w[j / 128, b]  sum_{k in b} a[i, k] w[j, k] )
 //
 // A k-block is 128 bytes of a row (128 e4m3 or 64 bf16 numbers), so both types share the stages, the swizzle and the descriptors.  The
-// tensor core sums one k-block (e4m3) or two (bf16) into an accumulator in tensor memory; eight warps read it back, multiply it with
+// tensor core sums one k-block (in bf16 two where a tile is up to 64 wide or a pair's) into an accumulator in tensor memory; eight warps read it back, multiply it with
 // the scales and add it to the 32-bit sums that they keep in registers, while the next accumulator is filled.  (bf16 has no scales; its sums are
 // cut as well because the tensor core's additions truncate: the error grows with their number.)
 //
@@ -316,7 +316,7 @@ __device__ __forceinline__ bool both_sets(int bar, bool mine) {
 
 // F8: e4m3 with scales, else bf16.  WIDTH: 64, 128 or 256, the widest tile it takes.  PAIR: two CTAs (a cluster, an SM each) share a tile of 256 rows:
 // each stages its own rows and half of the weights and keeps its own rows' sums; the first one issues the MMAs for both.  A k-block then costs
-// an SM 32 KB from L2 where a tile of its own costs 48, and that path gives it 47 bytes a cycle: 48 KB take 0.58 us, 32
+// an SM 32 KB from L2 where a tile of its own costs 48, and a lone CTA gets 47 bytes a cycle that way (two of an SM 70): 48 KB take 0.58 us, 32
 // KB 0.39, the hand-overs 0.46.
 //
 // Between the tensor core and the sums a hand-over takes about 1100 cycles there and back (issue 60 a MMA, a commit that is seen 300 later, a look at

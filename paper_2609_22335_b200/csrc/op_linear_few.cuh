@@ -3,8 +3,8 @@
 // The weights are what such a call has to read, once, and nothing else takes time if nothing stands in their way.  So the roles of the operands are
 // exchanged: up to 128 features are the MMA's M (a tensor-memory lane each) and the rows its N.  A k-block's accumulator then has 16 to 64 columns where it has
 // 64 to 256 there, all lanes work, each stage has an accumulator of its own (a hand-over is only waited for a ring of stages later), and a
-// warp stores a row's 32 neighbouring features at a time.  1 x 11008 x 4096 in e4m3 14.1 -> 11.7 us (45 MB: 7.0 at the
-// copy's rate; the rest is the launch, the first loads and the last hand-over).
+// warp stores a row's 32 neighbouring features at a time.  1 x 11008 x 4096 in e4m3 14.1 -> 11.7 us, now 11.4 (45 MB: 7.0
+// at the copy's rate; the rest is the start, a launch of 1.5 us in it, the first loads and the last hand-over).
 //
 // CTA: 256 threads, half an SM.  Warp 0 issues TMA loads, warp 1 MMAs, warp 2 fetches scales, warps 4 to 7 add up: s_a differs by column here and s_w by
 // lane.  Persistent where the tiles are many; where they are few a cluster of up to 8 CTAs shares a tile's K and adds up in the first one's shared memory.

@@ -7,7 +7,7 @@
 //
 // Bound by memory (x in, y out).  A thread has sixteen values of a head, both halves of eight pairs (P threads a head), and keeps their
 // sines over the heads it takes in turn, so that they cost little; sixteen-byte loads and stores.  8192 rows of 24 heads of 128 in bf16, 101 MB:
-// 21.0 us (15.6 at the copy's rate), issue slots 58 % busy.
+// 21.1 us (15.6 at the copy's rate), issue slots 68 % busy.
 #pragma once
 #include "packed_f32.cuh"
 #include "tiles_common.cuh"
