@@ -453,7 +453,7 @@ def op_attention(q, k, v, hq, hkv, hd, causal=False, scratch=None, stream=None):
     torch.cuda.Stream, or on torch's current one.)"""
     import torch
     tq, tkv = q.shape[0], k.shape[0]
-    out = torch.empty_like(q)
+    out = _new(stream, q.shape, q.dtype, q)
     if scratch is None:
         scratch = _new(stream, (op_attention_scratch_bytes(tkv, hkv, hd),), torch.uint8, q)       # (goes back to its stream's memory when this returns)
     rc = load_library().vla_op_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), tq, tkv, hq, hkv, hd,
@@ -469,10 +469,10 @@ def op_linear(a, w, act=0, out_bf16=False, stream=None):
     m, k = a.shape
     n = w.shape[0]
     if out_bf16:
-        out = a.new_empty((m, n), dtype=torch.bfloat16)
+        out = _new(stream, (m, n), torch.bfloat16, a)
         p32, p16 = None, out.data_ptr()
     else:
-        out = a.new_empty((m, n), dtype=torch.float32)
+        out = _new(stream, (m, n), torch.float32, a)
         p32, p16 = out.data_ptr(), None
     rc = (_lib or load_library()).vla_op_linear(a.data_ptr(), w.data_ptr(), p32, p16, m, n, k, act,
                                                 _stream_ptr(stream))

@@ -103,3 +103,26 @@ def test_attentions_own_scratch_is_memory_of_its_stream():
     mine = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]
     torch.cuda.synchronize()
     assert all(bool((m == 7).all()) for m in mine) and got.shape == q.shape
+
+
+@pytest.mark.parametrize("name", ["linear", "attention", "quantize", "linear_scaled", "linear_grouped", "linear_grouped_scaled", "qk_norm_rope"])
+def test_results_are_memory_of_the_stream_that_writes_them(name):
+    """A result that is dropped before its kernel has run must not be written into what the current stream has made of its memory."""
+    import torch
+    from paper_2609_22335_b200 import api
+    entry, side = getattr(api, "op_" + name), torch.cuda.Stream()
+    inputs, call = case(name)
+    shapes = [t.shape for t in copies(call())]
+    [torch.full(s, 7, dtype=torch.uint8, device="cuda") for s in shapes]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    try:
+        setattr(api, "op_" + name, lambda *a, **k: entry(*a, stream=side, **k))
+        call()
+    finally:
+        setattr(api, "op_" + name, entry)
+    mine = [torch.full(s, 7, dtype=torch.uint8, device="cuda") for _ in range(8) for s in shapes]
+    torch.cuda.synchronize()
+    assert all(bool((m == 7).all()) for m in mine)
