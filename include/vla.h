@@ -281,6 +281,14 @@ int vla_op_attention_static(const void* q, const void* k, const void* v, void* o
 int vla_op_linear(const void* a, const void* w, float* out32, void* out16, int32_t m, int32_t n, int32_t k, int32_t act,
                   void* stream);
 
+/* The same with addends, y = act(x W^T + bias) + residual (no counterpart in the paper, like the operators below).  bias fp32 [n] or
+ * NULL; residual [m,n] bf16 (residual_f32 = 0) or fp32, rows ld_residual >= n elements apart, or NULL.  Added in fp32, rounded once; GeLU and SiLU
+ * to fp32 precision.  An output may be the residual itself (same type, ld_residual = n) and overlaps the inputs in no other way.  Calls can
+ * be captured into graphs, the first one on a device among them. */
+int vla_op_linear_bias(const void* a, const void* w, const float* bias, const void* residual, int32_t residual_f32,
+                       int64_t ld_residual, float* out32, void* out16, int32_t m, int32_t n, int32_t k, int32_t act,
+                       void* stream);
+
 /* Values to 8 bits (e4m3) with a scale for each block of block_rows x 128 (no counterpart in the paper, like the operators
  * below: what a decoder layer of the caller's own needs around vla_op_linear and vla_op_attention).
  *   scales[i / block_rows, j / 128] = max(largest |x| of the block / 448, 2^-126),  q[i,j] = e4m3(x[i,j] / scale)
@@ -332,10 +340,10 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
  * reads that word back: VLA_OK, or VLA_ERR_TIMEOUT when a wait ran out.  op selects the word: VLA_OP_LINEAR (one
  * word per device, shared by all vla_op_linear calls on it: query before another call reuses it), VLA_OP_ATTENTION
  * (the word at the start of `scratch`, DEVICE), VLA_OP_ATTENTION_STATIC (the library's fixed array), or VLA_OP_LINEAR_SCALED,
- * VLA_OP_LINEAR_GROUPED and VLA_OP_LINEAR_GROUPED_SCALED (a word per device each, as for VLA_OP_LINEAR; vla_op_quantize and
+ * VLA_OP_LINEAR_GROUPED, VLA_OP_LINEAR_GROUPED_SCALED and VLA_OP_LINEAR_BIAS (a word per device each, as for VLA_OP_LINEAR; vla_op_quantize and
  * vla_op_qk_norm_rope wait for nothing). */
 enum { VLA_OP_LINEAR = 0, VLA_OP_ATTENTION = 1, VLA_OP_ATTENTION_STATIC = 2, VLA_OP_LINEAR_SCALED = 3, VLA_OP_LINEAR_GROUPED = 4,
-       VLA_OP_LINEAR_GROUPED_SCALED = 5 };
+       VLA_OP_LINEAR_GROUPED_SCALED = 5, VLA_OP_LINEAR_BIAS = 6 };
 int vla_op_status(int32_t op, const void* scratch, void* stream);
 
 /* Test hook: while drop_operand_loads is non-zero the operators' TMA producers issue no loads, so their consumers

@@ -27,7 +27,7 @@ EXPORTS = ["vla_required_arena_bytes", "vla_init", "vla_load_weights", "vla_subm
            "vla_poll_actions", "vla_hold_launches", "vla_wait_idle", "vla_get_trace", "vla_reset_trace", "vla_program_info", "vla_debug_fetch",
            "vla_get_counters", "vla_set_class_tags", "vla_get_class_tags", "vla_policy_probe", "vla_policy_probe_ex", "vla_debug_bump_dependency", "vla_debug_guards", "vla_last_error",
            "vla_destroy", "vla_op_status", "vla_debug_op_fault", "vla_debug_tile_linear", "vla_debug_tile_addends", "vla_debug_tile_attention",
-           "vla_op_attention_scratch_bytes", "vla_op_attention", "vla_op_linear",
+           "vla_op_attention_scratch_bytes", "vla_op_attention", "vla_op_linear", "vla_op_linear_bias",
            "vla_op_attention_static_capacity", "vla_op_attention_static", "vla_op_quantize", "vla_op_linear_scaled",
            "vla_op_linear_grouped", "vla_op_linear_grouped_scaled", "vla_op_qk_norm_rope"]
 
@@ -108,6 +108,7 @@ def load_library() -> C.CDLL:
     lib.vla_op_attention_scratch_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, P(C.c_size_t)]
     lib.vla_op_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 6 + [C.c_void_p, C.c_size_t, C.c_void_p]
     lib.vla_op_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 4 + [C.c_void_p]
+    lib.vla_op_linear_bias.argtypes = [C.c_void_p] * 4 + [C.c_int32, C.c_int64] + [C.c_void_p] * 2 + [C.c_int32] * 4 + [C.c_void_p]
     lib.vla_op_attention_static_capacity.argtypes = [P(C.c_size_t)]
     lib.vla_op_attention_static.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p] + [C.c_int32] * 6 + [C.c_void_p]
     lib.vla_op_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p] + [C.c_int32] * 3 + [C.c_void_p]
@@ -397,7 +398,7 @@ class Engine:
 
 
 POLICIES = {"two_phase": 0, "class_order": 1, "round_robin": 2, "two_phase_g": 3, "two_phase_r": 4}
-OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED = range(6)
+OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED, OP_LINEAR_BIAS = range(7)
 
 
 def policy_probe(taus, pending, feasible, cta_count, u, rr_start=0, u_max=0, policy=0, grid=None, res=None):
@@ -567,6 +568,38 @@ def _blocks(name, a, scale_a, w, scale_w, offsets, out, act, out_bf16, stream):
     elif out.shape != (m, n) or out.dtype != result or not out.is_contiguous():
         _refuse(name, "out is contiguous, [rows,n], fp32 or, with out_bf16, bf16")
     return m, n, k, out, (None, out.data_ptr()) if out_bf16 else (out.data_ptr(), None), _stream_ptr(stream)
+
+
+def op_linear_bias(a, w, bias=None, residual=None, act=0, out_bf16=False, out=None, stream=None):
+    """a [m,k], w [n,k]: CUDA bf16, contiguous; bias fp32 [n]; residual bf16 or fp32 [m,n], rows may lie apart.  Returns act(a w^T + bias) + residual as
+    fp32 (or bf16) [m,n], in ``out`` where it is given, which may be the residual itself (see vla_op_linear_bias)."""
+    import torch
+    name, bf16 = "op_linear_bias", torch.bfloat16
+    if a.dtype != bf16 or w.dtype != bf16 or a.dim() != 2 or w.dim() != 2 or _elsewhere(a, w, bias, residual, out):
+        _refuse(name, "a [m,k] and w [n,k] are bf16 on the current CUDA device, like all else")
+    m, k = a.shape
+    n = w.shape[0]
+    if w.shape[1] != k or not a.is_contiguous() or not w.is_contiguous() or (m | n | k) >> 31:
+        _refuse(name, "a and w are contiguous, rows of the same k, all sizes below 2^31")
+    if bias is not None and (bias.shape != (n,) or bias.dtype != torch.float32 or not bias.is_contiguous()):
+        _refuse(name, "bias is contiguous fp32, [n]")
+    f32, ld, res = False, 0, None
+    if residual is not None:
+        f32 = residual.dtype == torch.float32
+        if not (f32 or residual.dtype == bf16) or residual.shape != (m, n) or (n > 1 and residual.stride(1) != 1):
+            _refuse(name, "residual is bf16 or fp32 [m,n], rows in one piece")
+        ld, res = residual.stride(0) if m > 1 else n, residual.data_ptr()
+    result = bf16 if out_bf16 else torch.float32
+    if out is None:
+        out = _new(stream, (m, n), result, a)
+    elif out.shape != (m, n) or out.dtype != result or not out.is_contiguous():
+        _refuse(name, "out is contiguous, [m,n], fp32 or, with out_bf16, bf16")
+    p32, p16 = (None, out.data_ptr()) if out_bf16 else (out.data_ptr(), None)
+    rc = (_lib or load_library()).vla_op_linear_bias(a.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(), res, int(f32), ld, p32, p16, m, n, k, act,
+                                                     _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_linear_bias failed")
+    return out
 
 
 def op_linear_scaled(a, scale_a, w, scale_w, act=0, out_bf16=False, stream=None):

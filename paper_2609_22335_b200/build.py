@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -26,23 +27,27 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
-           "-shared", "-Xcompiler", "-fPIC", "-x", "cu",
-           "-DVLA_EXPORTS", "-o", LIB,
-           # no implicit multiply-add contraction: the same tile body is compiled into several kernels (the
-           # persistent one, the per-node ones, the single-op ones) and must round identically in all of them;
-           # the fused multiply-adds the bodies want are written as fmaf()
-           "-fmad=false"]
+    flags = ["-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a", "-Xcompiler", "-fPIC", "-DVLA_EXPORTS",
+             # no implicit multiply-add contraction: the same tile body is compiled into several kernels (the
+             # persistent one, the per-node ones, the single-op ones) and must round identically in all of them;
+             # the fused multiply-adds the bodies want are written as fmaf()
+             "-fmad=false"]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-lcudart"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("nvcc failed building libvla_b200.so")
+        flags += ["-Xptxas", "-v"]
+    with tempfile.TemporaryDirectory() as objects:                  # (an object for each source, side by side)
+        out = [os.path.join(objects, s + ".o") for s in SOURCES]
+        steps = [subprocess.Popen([nvcc, *flags, "-x", "cu", "-c", "-o", o, os.path.join(CSRC, s)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+                 for s, o in zip(SOURCES, out)]
+        said = [p.communicate()[0] for p in steps]
+        if all(p.returncode == 0 for p in steps):
+            link = subprocess.run([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", LIB, *out, "-lcudart"], capture_output=True, text=True)
+            said.append(link.stdout + link.stderr)
+            steps.append(link)
+        if any(p.returncode != 0 for p in steps):
+            sys.stderr.write("".join(said))
+            raise RuntimeError("nvcc failed building libvla_b200.so")
     if verbose:
-        sys.stderr.write(r.stderr)
+        sys.stderr.write("".join(said))
     return LIB
 
 

@@ -24,6 +24,11 @@ struct LinearArgs {
   float* out32;
   unsigned short* out16;
   unsigned* err;                              // 0, or why a wait ran out
+  // Addends (kernels with ADD): y = act(product + bias) + residual.  Either may be null.
+  const float* bias;                          // [n]
+  const void* residual;                       // [m, n], rows ld_residual elements apart
+  long long ld_residual;
+  int residual_f32;
 };
 
 // Features a store may cover: what every row's start and the width allow.  Eight go out as 16 bytes of bf16 or four pairs of
@@ -35,11 +40,25 @@ inline int linear_vec(int n, const float* out32, const void* out16) {
   if (n % 8 == 0 && ((a32 | a16) & 15) == 0) return 8;
   return n % 2 == 0 && (a32 & 7) == 0 && (a16 & 3) == 0 ? 2 : 1;
 }
+inline int linear_add_vec(int n, const float* out32, const void* out16, const float* bias, const void* residual, bool residual_f32, long long ld) {
+  const int vec = linear_vec(n, out32, out16);
+  const uintptr_t b = reinterpret_cast<uintptr_t>(bias), r = reinterpret_cast<uintptr_t>(residual);
+  if (vec == 8 && (!bias || b % 8 == 0) && (!residual || (residual_f32 ? r % 8 == 0 && ld % 2 == 0 : r % 16 == 0 && ld % 8 == 0))) return 8;
+  return vec >= 2 && (!bias || b % 8 == 0) && (!residual || (r % (residual_f32 ? 8 : 4) == 0 && ld % 2 == 0)) ? 2 : 1;
+}
 inline int linear_smem(const LinearArgs& g) {
   const int stage = (g.bm + g.bn) * GEMM_BK * 2;
   return g.stages * stage + (stage < 16384 ? 16384 - stage : 0);
 }
 
+// 0.5 x (1 + tanh(u)) = x / (1 + e^-2u): to fp32 precision at the price of a SiLU (tanh.approx is off by 2^-11, which shows in fp32 results).
+__device__ __forceinline__ float gelu_exact_f(float x) {
+  const float c = 2.0f * 0.7978845608028654f, u = x * fmaf(x * x, c * 0.044715f, c);
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * -1.44269504f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return x * r;
+}
 // 4 x 4 transposition of one register each over a quad: lane q gets the four lanes' w[q], in lane order.
 __device__ __forceinline__ void quad_transpose(uint32_t* w, int q) {
   const bool o1 = (q & 1) != 0, o2 = (q & 2) != 0;
@@ -96,10 +115,78 @@ __device__ __forceinline__ void linear_store(const LinearArgs& g, float* v, int 
     }
   }
 }
+// Residual rows of one fragment, in the order in which linear_store gives out rows: fp32 pairs where the fragment has them, bf16 eight at a time
+// (VEC 8: exchanged over the quad when they are added) or pair by pair.  They are asked for a group of 32 columns ahead, so that the trip to
+// L2 lies under the work on the group before; places behind the tile's end read its last row or the last columns instead (in bounds, and nobody
+// stores them).  With the output in the residual's place each element is read by the thread that writes it, before it does.
+template <int VEC>
+__device__ __forceinline__ void residual_load(const LinearArgs& g, uint32_t* w, int row, int f, int q) {
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const long long at = (long long)min(row + 8 * r, g.m - 1) * g.ld_residual;
+    if (g.residual_f32) {
+      const float* p = static_cast<const float*>(g.residual) + at;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int c = f + 8 * b + 2 * q;
+        if (VEC >= 2) {
+          const float2 v = *reinterpret_cast<const float2*>(p + min(c, g.n - 2));
+          w[4 * b + 2 * r] = __float_as_uint(v.x); w[4 * b + 2 * r + 1] = __float_as_uint(v.y);
+        } else {
+          w[4 * b + 2 * r] = __float_as_uint(p[min(c, g.n - 1)]); w[4 * b + 2 * r + 1] = __float_as_uint(p[min(c + 1, g.n - 1)]);
+        }
+      }
+    } else {
+      const unsigned short* p = static_cast<const unsigned short*>(g.residual) + at;
+      if (VEC == 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p + min(f + 8 * q, g.n - 8));
+        w[4 * r] = v.x; w[4 * r + 1] = v.y; w[4 * r + 2] = v.z; w[4 * r + 3] = v.w;
+      } else {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int c = f + 8 * b + 2 * q;
+          if (VEC == 2) w[4 * r + b] = *reinterpret_cast<const uint32_t*>(p + min(c, g.n - 2));
+          else w[4 * r + b] = (uint32_t)p[min(c, g.n - 1)] | (uint32_t)p[min(c + 1, g.n - 1)] << 16;
+        }
+      }
+    }
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void residual_add(const LinearArgs& g, uint32_t* w, float* v, int q) {
+  if (g.residual_f32) {
+#pragma unroll
+    for (int j = 0; j < EPI; ++j) v[j] += __uint_as_float(w[j]);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      if (VEC == 8) quad_transpose(w + 4 * r, q);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        v[4 * b + 2 * r] += __uint_as_float(w[4 * r + b] << 16);
+        v[4 * b + 2 * r + 1] += __uint_as_float(w[4 * r + b] & 0xFFFF0000u);
+      }
+    }
+  }
+}
+// The bias of the lane's columns of a fragment, b[2 i + e] for column 8 i + 2 q + e.
+template <int VEC>
+__device__ __forceinline__ void bias_load(const LinearArgs& g, float* b, int f, int q) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = f + 8 * i + 2 * q;
+    if (VEC >= 2) {
+      const float2 v = __ldg(reinterpret_cast<const float2*>(g.bias + min(c, g.n - 2)));
+      b[2 * i] = v.x; b[2 * i + 1] = v.y;
+    } else {
+      b[2 * i] = __ldg(g.bias + min(c, g.n - 1)); b[2 * i + 1] = __ldg(g.bias + min(c + 1, g.n - 1));
+    }
+  }
+}
 // This warp's share of a tile's columns: groups of 32, [lo, hi), for its 32 lanes.  `part` (split K): the other CTAs'
 // fragments of the same group, written by the threads that hold the same place.  `n_acc`: accumulators of the same columns,
 // `acc_stride` apart, that add up to the result.
-template <int ACT, int VEC>
+template <int ACT, int VEC, bool ADD>
 __device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, int lane, int row0, int rows, int n0, int lo, int hi, const float4* part,
                                             int n_part, int part_stride, int n_acc = 1, uint32_t acc_stride = 0) {
   const int q = lane & 3;
@@ -107,7 +194,9 @@ __device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, 
   for (int h = 0; h < 2 && 16 * h < rows; ++h) {
     if (lo >= hi) break;
     const uint32_t th = tmem + ((uint32_t)(16 * h) << 16);
-    uint32_t nx[EPI];
+    uint32_t nx[EPI], res[EPI];
+    const int row = row0 + 16 * h + (lane >> 2);
+    if (ADD && g.residual) residual_load<VEC>(g, res, row, n0 + 32 * lo, q);
     tmem_ld_frag(th + 32u * (uint32_t)lo, nx);
 #pragma unroll 1
     for (int c = lo; c < hi; ++c) {
@@ -133,14 +222,33 @@ __device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, 
           v[4 * j] += t.x; v[4 * j + 1] += t.y; v[4 * j + 2] += t.z; v[4 * j + 3] += t.w;
         }
       }
-      activate<ACT, EPI>(v);
-      linear_store<VEC>(g, v, row0 + 16 * h + (lane >> 2), n0 + 32 * c, q);
+      if (ADD) {
+        if (g.bias) {
+          float b[8];
+          bias_load<VEC>(g, b, n0 + 32 * c, q);
+#pragma unroll
+          for (int j = 0; j < EPI; ++j) v[j] += b[2 * (j >> 2) + (j & 1)];
+        }
+        if (ACT == ACT_GELU) {
+#pragma unroll
+          for (int j = 0; j < EPI; ++j) v[j] = gelu_exact_f(v[j]);
+        } else {
+          activate<ACT, EPI>(v);
+        }
+        if (g.residual) {
+          residual_add<VEC>(g, res, v, q);
+          if (c + 1 < hi) residual_load<VEC>(g, res, row, n0 + 32 * (c + 1), q);
+        }
+      } else {
+        activate<ACT, EPI>(v);
+      }
+      linear_store<VEC>(g, v, row, n0 + 32 * c, q);
     }
     tmem_ld_wait();
   }
 }
 
-template <int VEC>
+template <int VEC, bool ADD = false>
 __global__ void __launch_bounds__(LIN_THREADS, 2) vla_op_linear_kernel(const __grid_constant__ LinearArgs g, const __grid_constant__ OpMaps maps,
                                                                        OpFault fault) {
   extern __shared__ __align__(1024) char smem_raw[];
@@ -224,9 +332,9 @@ __global__ void __launch_bounds__(LIN_THREADS, 2) vla_op_linear_kernel(const __g
     LinearArgs gg = g;
     gg.m = row0 + max(rows, 0);                                       // (this tile's rows and features only)
     gg.n_end = min(g.n, n0 + g.bn);
-    if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
-    else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
-    else linear_rows<ACT_NONE, VEC>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
+    if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
+    else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
+    else linear_rows<ACT_NONE, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
   };
   if (g.ks == 1) {
     if (warp >= 2) {

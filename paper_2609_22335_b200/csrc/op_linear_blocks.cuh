@@ -79,15 +79,6 @@ __device__ __forceinline__ void scales_landed(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// 0.5 x (1 + tanh(u)) = x / (1 + e^-2u): to fp32 precision at the price of a SiLU (tanh.approx is off by 2^-11, which shows in fp32 results).
-__device__ __forceinline__ float gelu_exact_f(float x) {
-  const float c = 2.0f * 0.7978845608028654f, u = x * fmaf(x * x, c * 0.044715f, c);
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(u * -1.44269504f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  return x * r;
-}
-
 __device__ __forceinline__ void st_cluster_f1(uint32_t a, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(x) : "memory"); }
 
 // Where a tile is: `row_end` is the end of its expert's rows.

@@ -43,7 +43,7 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
 }
 
 // PARTS: accumulators that take a part of K each (a kernel of its own for 1: worked out at run time, 8192 x 3072 x 768 42.2 -> 44.2 us).
-template <int VEC, bool PARTS>
+template <int VEC, bool PARTS, bool ADD = false>
 __global__ void __launch_bounds__(LIN_THREADS, 1) vla_op_linear_pair_kernel(const __grid_constant__ LinearArgs g, const __grid_constant__ OpMaps maps,
                                                                             OpFault fault) {
   extern __shared__ __align__(1024) char smem_raw[];
@@ -144,9 +144,9 @@ __global__ void __launch_bounds__(LIN_THREADS, 1) vla_op_linear_pair_kernel(cons
       LinearArgs gg = g;
       gg.m = row0 + max(rows, 0);                                     // (this tile's rows and features only)
       gg.n_end = min(g.n, n0 + g.bn);
-      if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
-      else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
-      else linear_rows<ACT_NONE, VEC>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
+      if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
+      else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
+      else linear_rows<ACT_NONE, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(acce_leader + 8u * buf) : "memory");

@@ -2,95 +2,7 @@
 // want the kernels without the frame pipeline.  They are kernels of their own (op_linear.cuh, op_attention.cuh); the engine's
 // tile bodies are reached one by one through tile_hooks.cuh.
 #pragma once
-#include <cuda.h>
-#include <cuda_runtime.h>
-#include <initializer_list>
-
-#include "../../include/vla.h"
-#include "dispatch.cuh"
-#include "per_device.h"
-
-namespace vla {
-
-struct OpMaps {
-  alignas(64) CUtensorMap m[4];
-};
-
-typedef CUresult (*OpEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-inline OpEncodeFn op_encoder() {
-  static OpEncodeFn fn = nullptr;
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<OpEncodeFn>(p);
-  }
-  return fn;
-}
-
-// 2-D row-major tensor, bf16 (or, by `width`, bytes or fp32), boxes of 128 bytes of a row, 128-byte swizzle, zero fill outside.
-inline bool op_encode(CUtensorMap* out, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int width = 2) {
-  OpEncodeFn enc = op_encoder();
-  if (!enc) return false;
-  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)ld * width};
-  cuuint32_t box[2] = {(cuuint32_t)(128 / width), (cuuint32_t)box_rows};
-  cuuint32_t estr[2] = {1, 1};
-  return enc(out, width == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : (width == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16), 2, const_cast<void*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-constexpr uint64_t OP_WAIT_LIMIT_NS = 2000000000ull;
-// Bound of the operators' device-side waits, and the test hook that makes one run out (vla_debug_op_fault).
-struct OpFault {
-  uint32_t wait_limit;                         // in 1024 ns
-  int drop_loads;
-  int tell_late;                               // places of experts' tiles are told only once a wait has run out
-};
-inline OpFault& op_fault() {
-  static OpFault f = {(uint32_t)(OP_WAIT_LIMIT_NS >> 10), 0, 0};
-  return f;
-}
-
-// What an operator's waits look at: the CTA's word, set by the first of them that runs out, and how long one may take.  Each is bounded by itself: a call
-// may run for as long as it has work.
-struct OpWaits {
-  unsigned* error;
-  uint32_t limit;                              // in 1024 ns
-};
-__device__ __forceinline__ bool mbar_wait(const OpWaits& c, uint32_t bar, uint32_t parity) {
-  if (mbar_try_wait(bar, parity, 20000u)) return true;              // (a wait that is over at the first look, or within its sleep, reads no clock)
-  const uint32_t until = (uint32_t)(gtimer() >> 10) + c.limit;        // 1024 ns each, in one register
-  while (!mbar_try_wait(bar, parity, 20000u)) {
-    if (*reinterpret_cast<volatile unsigned*>(c.error) != 0u) return false;
-    if ((int)((uint32_t)(gtimer() >> 10) - until) > 0) {
-      atomicCAS(c.error, 0u, (unsigned)DEV_ERR_WAIT_MBAR);
-      return false;
-    }
-  }
-  return true;
-}
-
-// Start of an operator kernel.  A call's kernel is launched while the previous one on the stream is still running (programmatic
-// stream serialisation, op_launch): barriers, tensor memory and descriptors are set up behind that one's last tiles, and
-// nothing of global memory is touched before op_wait_previous has returned, that is before all earlier work on the stream is
-// complete and visible.  op_let_next_start lets the next call's kernel do the same.  It takes effect once every block of this
-// grid has come to it, and stands behind the block's tensor-memory allocation: a block that waits for this grid can then
-// neither keep one of its blocks out nor hold columns that one of them still needs.  Back to back: linear 50x2048x720
-// 8.2 -> 6.1 us, 288x11008x4096 45.9 -> 43.9, attention 1024x1024 (12 heads of 64) 16.4 -> 14.5.
-__device__ __forceinline__ void op_wait_previous(const OpMaps& maps, int n) {
-  if ((int)threadIdx.x < n) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[threadIdx.x]) : "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-}
-__device__ __forceinline__ void op_let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
-}  // namespace vla
-
+#include "op_common.cuh"
 #include "op_attention.cuh"
 #include "op_linear.cuh"
 #include "op_linear_blocks.cuh"
@@ -106,7 +18,7 @@ constexpr size_t OP_ATTN_HEADER = 256;   // error word + padding (behind it: roo
 // What vla_op_linear keeps per device, looked up on the first call made with that device current: SM count and the error word
 // (in a fixed device array of the library).  The kernel clears the word itself before it waits for anything, so that a call
 // that was captured into a graph reports on its latest replay like any other.
-static __device__ __align__(256) unsigned g_op_linear_error[64];
+static __device__ __align__(256) unsigned g_op_linear_error[80];
 constexpr int OP_ERROR_WORDS = 16;             // words (64 bytes) between two operators' own
 struct OpDevice {
   unsigned* error = nullptr;                   // of vla_op_linear; the others that have one: error_of
@@ -152,43 +64,8 @@ inline bool op_device(OpDevice* d) {
   return cudaGetDevice(&dev) == cudaSuccess && devices.get(dev, d, [dev](OpDevice* r) { return op_look_up(dev, r); });
 }
 
-// Reads an operator's error word back after the stream has drained.
-inline int op_status_of(const unsigned* dev_word, cudaStream_t s) {
-  if (cudaStreamSynchronize(s) != cudaSuccess) return VLA_ERR_CUDA;
-  unsigned v = 0;
-  if (cudaMemcpy(&v, dev_word, sizeof v, cudaMemcpyDeviceToHost) != cudaSuccess) return VLA_ERR_CUDA;
-  return v == 0 ? VLA_OK : VLA_ERR_TIMEOUT;
-}
-
-// Launches a kernel in clusters of `cluster` blocks (1: none), overlapping the end of the kernel in front of it
-// (op_wait_previous).
-template <typename... P, typename... A>
-inline int op_launch(void (*kernel)(P...), int grid, int threads, int smem, int cluster, cudaStream_t s, const A&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[2];
-  cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = (size_t)smem;
-  cfg.stream = s;
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? VLA_OK : VLA_ERR_CUDA;
-}
-
-inline int64_t op_pad(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-
 inline bool op_attention_shape_ok(int tq, int tkv, int hq, int hkv, int hd) {
   return tq >= 1 && tkv >= 1 && hq >= 1 && hkv >= 1 && hq % hkv == 0 && hd >= 16 && hd <= 256 && hd % 16 == 0;
-}
-
-inline bool op_aligned(int bytes, std::initializer_list<const void*> pointers) {
-  for (const void* p : pointers)
-    if (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) return false;
-  return true;
 }
 
 inline size_t op_attention_scratch_bytes(int tkv, int hkv, int hd) {
@@ -289,6 +166,45 @@ inline bool op_scales_ok(const float* sa, const float* sw) {
   return sa && sw && ((reinterpret_cast<uintptr_t>(sa) | reinterpret_cast<uintptr_t>(sw)) & 3) == 0;
 }
 
+// The layer with or without addends, which are in `g` already, as is where the results go.
+template <bool ADD>
+inline int op_linear_run(const void* a, const void* w, LinearArgs& g, int m, int n, int k, int act, int vec, const OpDevice& dev, cudaStream_t s) {
+  g.m = m; g.n = n; g.kp = (int)op_pad(k, GEMM_BK); g.act = act;
+  const LinearPlan p = linear_plan(m, n, k, g.out32 != nullptr, dev.sms, LinearRoom{dev.room.alone[4], dev.room.two[4]});
+  const LinearPairPlan pp = linear_pair_plan(m, n, k, p, dev.sms);
+  OpMaps maps;
+  if (pp.bn > 0) {
+    g.bm = pp.bm; g.bn = pp.bn; g.ks = p.ks; g.tiles_m = pp.tiles_m; g.tiles = pp.tiles; g.stages = pp.stages;
+    if (!op_encode(&maps.m[0], w, n, k, k, g.bn / 2) || !op_encode(&maps.m[1], a, m, k, k, g.bm)) return VLA_ERR_CUDA;
+    const int pairs = g.tiles < dev.sms / 2 ? g.tiles : dev.sms / 2;
+    const auto kernel = g.ks > 1 ? (vec == 8 ? vla_op_linear_pair_kernel<8, true, ADD> : (vec == 2 ? vla_op_linear_pair_kernel<2, true, ADD> : vla_op_linear_pair_kernel<1, true, ADD>))
+                                 : (vec == 8 ? vla_op_linear_pair_kernel<8, false, ADD> : (vec == 2 ? vla_op_linear_pair_kernel<2, false, ADD> : vla_op_linear_pair_kernel<1, false, ADD>));
+    return op_launch(kernel, 2 * pairs, LIN_THREADS, LINP_SMEM, 2, s, g, maps, op_fault());
+  }
+  g.bm = p.bm; g.bn = p.bn; g.ks = p.ks; g.tiles_m = p.tiles_m; g.tiles = p.tiles; g.stages = p.stages;
+  if (!op_encode(&maps.m[0], w, n, k, k, g.bn) || !op_encode(&maps.m[1], a, m, k, k, g.bm)) return VLA_ERR_CUDA;
+  const int grid = g.ks > 1 ? g.tiles * g.ks : (g.tiles < 2 * dev.sms ? g.tiles : 2 * dev.sms);
+  const auto kernel = vec == 8 ? vla_op_linear_kernel<8, ADD> : (vec == 2 ? vla_op_linear_kernel<2, ADD> : vla_op_linear_kernel<1, ADD>);
+  return op_launch(kernel, grid, LIN_THREADS, linear_smem(g), g.ks, s, g, maps, op_fault());
+}
+// What the layer with addends needs beside op_device, looked up on its own first call (so that nobody else waits for its kernels to be loaded).
+struct OpAddendsDevice { bool ready = false; };
+inline bool op_addends_look_up(OpAddendsDevice* d) {
+  for (auto* kernel : {vla_op_linear_kernel<1, true>, vla_op_linear_kernel<2, true>, vla_op_linear_kernel<8, true>})
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LIN_SMEM) != cudaSuccess) return false;
+  for (auto* kernel : {vla_op_linear_pair_kernel<1, false, true>, vla_op_linear_pair_kernel<2, false, true>, vla_op_linear_pair_kernel<8, false, true>,
+                       vla_op_linear_pair_kernel<1, true, true>, vla_op_linear_pair_kernel<2, true, true>, vla_op_linear_pair_kernel<8, true, true>})
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LINP_SMEM) != cudaSuccess) return false;
+  d->ready = true;
+  return true;
+}
+inline bool op_addends_device() {
+  static PerDevice<OpAddendsDevice> devices;
+  int dev = -1;
+  OpAddendsDevice d;
+  return cudaGetDevice(&dev) == cudaSuccess && devices.get(dev, &d, op_addends_look_up) && d.ready;
+}
+
 }  // namespace vla
 
 extern "C" {
@@ -315,27 +231,25 @@ int vla_op_linear(const void* a, const void* w, float* out32, void* out16, int32
   if (!op_aligned(16, {a, w}) || !op_aligned(4, {out32}) || !op_aligned(2, {out16})) return VLA_ERR_INVALID;
   OpDevice dev;
   if (!op_device(&dev)) return VLA_ERR_CUDA;
-  LinearArgs g;
-  g.m = m; g.n = n; g.kp = (int)op_pad(k, GEMM_BK); g.act = act;
+  LinearArgs g = {};
   g.out32 = out32; g.out16 = static_cast<unsigned short*>(out16);
   g.err = dev.error;
-  const LinearPlan p = linear_plan(m, n, k, out32 != nullptr, dev.sms, LinearRoom{dev.room.alone[4], dev.room.two[4]});
-  const LinearPairPlan pp = linear_pair_plan(m, n, k, p, dev.sms);
-  const int vec = linear_vec(n, out32, out16);
-  OpMaps maps;
-  if (pp.bn > 0) {
-    g.bm = pp.bm; g.bn = pp.bn; g.ks = p.ks; g.tiles_m = pp.tiles_m; g.tiles = pp.tiles; g.stages = pp.stages;
-    if (!op_encode(&maps.m[0], w, n, k, k, g.bn / 2) || !op_encode(&maps.m[1], a, m, k, k, g.bm)) return VLA_ERR_CUDA;
-    const int pairs = g.tiles < dev.sms / 2 ? g.tiles : dev.sms / 2;
-    const auto kernel = g.ks > 1 ? (vec == 8 ? vla_op_linear_pair_kernel<8, true> : (vec == 2 ? vla_op_linear_pair_kernel<2, true> : vla_op_linear_pair_kernel<1, true>))
-                                 : (vec == 8 ? vla_op_linear_pair_kernel<8, false> : (vec == 2 ? vla_op_linear_pair_kernel<2, false> : vla_op_linear_pair_kernel<1, false>));
-    return op_launch(kernel, 2 * pairs, LIN_THREADS, LINP_SMEM, 2, static_cast<cudaStream_t>(stream), g, maps, op_fault());
-  }
-  g.bm = p.bm; g.bn = p.bn; g.ks = p.ks; g.tiles_m = p.tiles_m; g.tiles = p.tiles; g.stages = p.stages;
-  if (!op_encode(&maps.m[0], w, n, k, k, g.bn) || !op_encode(&maps.m[1], a, m, k, k, g.bm)) return VLA_ERR_CUDA;
-  const int grid = g.ks > 1 ? g.tiles * g.ks : (g.tiles < 2 * dev.sms ? g.tiles : 2 * dev.sms);
-  const auto kernel = vec == 8 ? vla_op_linear_kernel<8> : (vec == 2 ? vla_op_linear_kernel<2> : vla_op_linear_kernel<1>);
-  return op_launch(kernel, grid, LIN_THREADS, linear_smem(g), g.ks, static_cast<cudaStream_t>(stream), g, maps, op_fault());
+  return op_linear_run<false>(a, w, g, m, n, k, act, linear_vec(n, out32, out16), dev, static_cast<cudaStream_t>(stream));
+}
+
+int vla_op_linear_bias(const void* a, const void* w, const float* bias, const void* residual, int32_t residual_f32, int64_t ld_residual,
+                       float* out32, void* out16, int32_t m, int32_t n, int32_t k, int32_t act, void* stream) {
+  using namespace vla;
+  if (!a || !w || (!out32 && !out16) || m < 1 || m > 1 << 30 || n < 1 || n > 1 << 30 || k < 8 || k > 1 << 30 || k % 8 || act < 0 || act > 2) return VLA_ERR_INVALID;
+  if (!op_aligned(16, {a, w}) || !op_aligned(4, {out32, bias}) || !op_aligned(2, {out16}) || !op_aligned(residual_f32 ? 4 : 2, {residual})) return VLA_ERR_INVALID;
+  if (residual && (ld_residual < n || ld_residual > (int64_t)1 << 40)) return VLA_ERR_INVALID;
+  OpDevice dev;
+  if (!op_device(&dev) || !op_addends_device()) return VLA_ERR_CUDA;
+  LinearArgs g = {};
+  g.out32 = out32; g.out16 = static_cast<unsigned short*>(out16);
+  g.bias = bias; g.residual = residual; g.residual_f32 = residual_f32 ? 1 : 0; g.ld_residual = ld_residual;
+  g.err = dev.error_of(VLA_OP_LINEAR_BIAS);
+  return op_linear_run<true>(a, w, g, m, n, k, act, linear_add_vec(n, out32, out16, bias, residual, residual_f32 != 0, ld_residual), dev, static_cast<cudaStream_t>(stream));
 }
 
 int vla_op_linear_scaled(const void* a, const float* scale_a, const void* w, const float* scale_w, float* out32, void* out16,

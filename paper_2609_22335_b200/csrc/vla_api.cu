@@ -910,7 +910,8 @@ int vla_op_attention_static(const void* q, const void* k, const void* v, void* o
 
 int vla_op_status(int32_t op, const void* scratch, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (op == VLA_OP_LINEAR || op == VLA_OP_LINEAR_SCALED || op == VLA_OP_LINEAR_GROUPED || op == VLA_OP_LINEAR_GROUPED_SCALED) {
+  if (op == VLA_OP_LINEAR || op == VLA_OP_LINEAR_SCALED || op == VLA_OP_LINEAR_GROUPED || op == VLA_OP_LINEAR_GROUPED_SCALED ||
+      op == VLA_OP_LINEAR_BIAS) {
     vla::OpDevice d;
     return vla::op_device(&d) ? vla::op_status_of(d.error_of(op), s) : VLA_ERR_CUDA;
   }
