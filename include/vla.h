@@ -335,15 +335,52 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
                         const float* gain_k, float eps, const int32_t* pos, int32_t pos0, int32_t rot, float base,
                         int32_t interleaved, void* stream);
 
+/* Attention of several sequences in one call (no counterpart in the paper): softmax(s) V per head with grouped KV heads, where
+ *   s(i, j) = cap tanh(scale q_i.k_j / cap) - slopes[h] |p_i - j|       (cap = 0: not capped; slopes NULL: no bias)
+ * Sequence s has rows offsets_q[s] <= i < offsets_q[s + 1] of q and out [tq, hq*hd] and offsets_k[s] <= j < offsets_k[s + 1] of k and v
+ * [tk, hkv*hd] (the two may be the same array), nq and nk of them, and attends within itself.  Its row i is at position p = nk - nq + i: the rows are the
+ * last of its tokens.  causal: row i sees keys j <= p, with window > 0 those with p - j < window, and of every row's keys the first prefix[s] (prefix NULL: none).
+ * Not causal: all nk, and neither prefix nor window.  A row that sees no key becomes zeros.
+ * bf16, rows ld_* elements apart, 16-byte aligned, rows too; hd a multiple of 8, at most 256; hq a multiple of hkv; scale > 0.  offsets_q,
+ * offsets_k int32 [seqs + 1], prefix int32 [seqs], slopes fp32 [hq], all DEVICE and read by the kernel.  Offsets ascend; what lies outside of 0 .. tq (tk)
+ * counts as the nearer end.  Rows of no sequence are not written.  Keys that a row does not see have no part in it, whatever their values.
+ * out overlaps no input.  scratch: DEVICE, 256-byte aligned, vla_op_attention_sequences_scratch_bytes(hd) or more; its first word is the call's
+ * error word, its contents matter to nobody afterwards, and calls that share it must not overlap on the GPU (two captured graphs among them). */
+int vla_op_attention_sequences_scratch_bytes(int32_t hd, size_t* out_bytes);
+int vla_op_attention_packed(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* out,
+                            int64_t ld_out, const int32_t* offsets_q, const int32_t* offsets_k, int32_t seqs, int32_t tq,
+                            int32_t tk, int32_t hq, int32_t hkv, int32_t hd, float scale, int32_t causal, const int32_t* prefix,
+                            int32_t window, float cap, const float* slopes, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The same over a paged cache: sequence s has lengths[s] tokens, the new ones (its rows of q) last, and token j's key and value are row
+ * j % page_size of page pages[s * max_pages + j / page_size] of k_cache and v_cache [n_pages, page_size, hkv*hd], rows row_* and pages page_* elements
+ * apart.  page_size a multiple of 8; max_pages * page_size at most 2^30; lengths beyond that many tokens count as that many.  A page that does not
+ * exist (an entry below 0 or from n_pages on) reads as zeros; entries behind a sequence's length are not looked at, nor rows behind it. */
+int vla_op_attention_paged(const void* q, int64_t ld_q, const void* k_cache, int64_t row_k, int64_t page_k, const void* v_cache,
+                           int64_t row_v, int64_t page_v, void* out, int64_t ld_out, const int32_t* pages, const int32_t* lengths,
+                           const int32_t* offsets, int32_t seqs, int32_t tq, int32_t n_pages, int32_t page_size,
+                           int32_t max_pages, int32_t hq, int32_t hkv, int32_t hd, float scale, int32_t causal,
+                           const int32_t* prefix, int32_t window, float cap, const float* slopes, void* scratch,
+                           size_t scratch_bytes, void* stream);
+
+/* New rows of such a cache: rows offsets[s] <= i < offsets[s + 1] of k and v [t, width] (width = hkv*hd, a multiple of 8) become tokens lengths[s] -
+ * (offsets[s + 1] - i) of sequence s.  lengths count the new tokens.  A row whose token is below 0 or behind the table, or on a page that does
+ * not exist, is not written; two rows for one place are the caller's mistake.  Any page_size.  Strides and alignment as above. */
+int vla_op_cache_store(const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* k_cache, int64_t row_k, int64_t page_k,
+                       void* v_cache, int64_t row_v, int64_t page_v, const int32_t* pages, const int32_t* lengths,
+                       const int32_t* offsets, int32_t seqs, int32_t t, int32_t n_pages, int32_t page_size, int32_t max_pages,
+                       int32_t width, void* stream);
+
 /* Every device-side wait of the operators is bounded (2 s by default, each of them: a call may take longer); a wait that
  * runs out makes the kernel set the call's error word and return, leaving garbage in the output.  vla_op_status waits for `stream` to drain and
  * reads that word back: VLA_OK, or VLA_ERR_TIMEOUT when a wait ran out.  op selects the word: VLA_OP_LINEAR (one
  * word per device, shared by all vla_op_linear calls on it: query before another call reuses it), VLA_OP_ATTENTION
  * (the word at the start of `scratch`, DEVICE), VLA_OP_ATTENTION_STATIC (the library's fixed array), or VLA_OP_LINEAR_SCALED,
  * VLA_OP_LINEAR_GROUPED, VLA_OP_LINEAR_GROUPED_SCALED and VLA_OP_LINEAR_BIAS (a word per device each, as for VLA_OP_LINEAR; vla_op_quantize and
- * vla_op_qk_norm_rope wait for nothing). */
+ * vla_op_qk_norm_rope wait for nothing, nor does vla_op_cache_store), or VLA_OP_ATTENTION_PACKED and VLA_OP_ATTENTION_PAGED (the word at the start
+ * of `scratch`). */
 enum { VLA_OP_LINEAR = 0, VLA_OP_ATTENTION = 1, VLA_OP_ATTENTION_STATIC = 2, VLA_OP_LINEAR_SCALED = 3, VLA_OP_LINEAR_GROUPED = 4,
-       VLA_OP_LINEAR_GROUPED_SCALED = 5, VLA_OP_LINEAR_BIAS = 6 };
+       VLA_OP_LINEAR_GROUPED_SCALED = 5, VLA_OP_LINEAR_BIAS = 6, VLA_OP_ATTENTION_PACKED = 7, VLA_OP_ATTENTION_PAGED = 8 };
 int vla_op_status(int32_t op, const void* scratch, void* stream);
 
 /* Test hook: while drop_operand_loads is non-zero the operators' TMA producers issue no loads, so their consumers

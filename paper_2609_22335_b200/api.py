@@ -29,7 +29,8 @@ EXPORTS = ["vla_required_arena_bytes", "vla_init", "vla_load_weights", "vla_subm
            "vla_destroy", "vla_op_status", "vla_debug_op_fault", "vla_debug_tile_linear", "vla_debug_tile_addends", "vla_debug_tile_attention",
            "vla_op_attention_scratch_bytes", "vla_op_attention", "vla_op_linear", "vla_op_linear_bias",
            "vla_op_attention_static_capacity", "vla_op_attention_static", "vla_op_quantize", "vla_op_linear_scaled",
-           "vla_op_linear_grouped", "vla_op_linear_grouped_scaled", "vla_op_qk_norm_rope"]
+           "vla_op_linear_grouped", "vla_op_linear_grouped_scaled", "vla_op_qk_norm_rope",
+           "vla_op_attention_sequences_scratch_bytes", "vla_op_attention_packed", "vla_op_attention_paged", "vla_op_cache_store"]
 
 
 class vla_model_desc(C.Structure):
@@ -117,6 +118,12 @@ def load_library() -> C.CDLL:
     lib.vla_op_linear_grouped_scaled.argtypes = [C.c_void_p] * 7 + [C.c_int32] * 5 + [C.c_void_p]
     lib.vla_op_qk_norm_rope.argtypes = ([C.c_void_p] * 2 + [C.c_int32] + [C.c_int64] * 2 + [C.c_void_p] * 2 + [C.c_int64] * 2 + [C.c_int32] * 4 +
                                         [C.c_void_p] * 2 + [C.c_float, C.c_void_p] + [C.c_int32] * 2 + [C.c_float, C.c_int32, C.c_void_p])
+    lib.vla_op_attention_sequences_scratch_bytes.argtypes = [C.c_int32, P(C.c_size_t)]
+    lib.vla_op_attention_packed.argtypes = ([C.c_void_p, C.c_int64] * 4 + [C.c_void_p] * 2 + [C.c_int32] * 6 + [C.c_float, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_void_p] +
+                                            [C.c_void_p, C.c_size_t, C.c_void_p])
+    lib.vla_op_attention_paged.argtypes = ([C.c_void_p, C.c_int64] + [C.c_void_p, C.c_int64, C.c_int64] * 2 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 3 + [C.c_int32] * 8 +
+                                           [C.c_float, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_void_p] + [C.c_void_p, C.c_size_t, C.c_void_p])
+    lib.vla_op_cache_store.argtypes = [C.c_void_p, C.c_int64] * 2 + [C.c_void_p, C.c_int64, C.c_int64] * 2 + [C.c_void_p] * 3 + [C.c_int32] * 6 + [C.c_void_p]
     lib.vla_last_error.argtypes = [C.c_void_p]
     lib.vla_last_error.restype = C.c_char_p
     lib.vla_destroy.argtypes = [C.c_void_p]
@@ -398,7 +405,7 @@ class Engine:
 
 
 POLICIES = {"two_phase": 0, "class_order": 1, "round_robin": 2, "two_phase_g": 3, "two_phase_r": 4}
-OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED, OP_LINEAR_BIAS = range(7)
+OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED, OP_LINEAR_BIAS, OP_ATTENTION_PACKED, OP_ATTENTION_PAGED = range(9)
 
 
 def policy_probe(taus, pending, feasible, cta_count, u, rr_start=0, u_max=0, policy=0, grid=None, res=None):
@@ -685,6 +692,140 @@ def op_qk_norm_rope(q, k, hq, hkv, hd, gq=None, gk=None, eps=1e-6, pos=None, pos
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_qk_norm_rope failed")
     return out_q, out_k
+
+
+def op_attention_sequences_scratch_bytes(hd) -> int:
+    """Scratch memory of ``op_attention_packed`` and ``op_attention_paged`` at this head width."""
+    out = C.c_size_t(0)
+    rc = load_library().vla_op_attention_sequences_scratch_bytes(hd, C.byref(out))
+    if rc != VLA_OK:
+        raise VlaError(rc, "bad head width")
+    return out.value
+
+
+def _rows(name, what, x, rows, width):
+    """Elements from one row of x [rows, width] (bf16) to the next."""
+    import torch
+    if x.dtype != torch.bfloat16 or x.shape != (rows, width) or x.stride(1) != 1:
+        _refuse(name, f"{what}, rows in one piece")
+    return x.stride(0) if rows > 1 else width                       # (the stride of one row says nothing)
+
+
+def _counts32(name, what, x, n):
+    import torch
+    if x is not None and (x.shape != (n,) or x.dtype != torch.int32 or not x.is_contiguous()):
+        _refuse(name, f"{what} is contiguous int32, [{n}]")
+    return None if x is None else x.data_ptr()
+
+
+def _sequences(name, q, offsets, hq, hkv, hd, prefix, slopes, scale, out, scratch, stream, others):
+    """What the two attentions below have in common: (tq, seqs, ld_q, out, ld_out, scale, scratch and the pointers of prefix and slopes)."""
+    import torch
+    if q.dim() != 2 or offsets.dim() != 1 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8 or (hq * hd) >> 31 or _elsewhere(q, offsets, prefix, slopes, out, scratch, *others):
+        _refuse(name, "q is a matrix on the current CUDA device, like all else; hd a multiple of 8, at most 256")
+    tq, seqs = q.shape[0], offsets.shape[0] - 1
+    if tq < 1 or tq >> 31 or seqs < 1:
+        _refuse(name, "at least one row and one sequence, below 2^31 rows")
+    ld_q = _rows(name, "q is bf16 [tq, hq*hd]", q, tq, hq * hd)
+    _counts32(name, "offsets", offsets, seqs + 1)
+    if slopes is not None and (slopes.shape != (hq,) or slopes.dtype != torch.float32 or not slopes.is_contiguous()):
+        _refuse(name, "slopes is contiguous fp32, [hq]")
+    if out is None:
+        out, ld_out = _new(stream, (tq, hq * hd), torch.bfloat16, q), hq * hd
+    else:
+        ld_out = _rows(name, "out is bf16 [tq, hq*hd]", out, tq, hq * hd)
+    if scratch is None:
+        scratch = _new(stream, (op_attention_sequences_scratch_bytes(hd),), torch.uint8, q)     # (goes back to its stream's memory when the call returns)
+    elif scratch.dtype != torch.uint8 or not scratch.is_contiguous():
+        _refuse(name, "scratch is contiguous uint8")
+    return (tq, seqs, ld_q, out, ld_out, hd ** -0.5 if scale is None else scale, scratch, _counts32(name, "prefix", prefix, seqs),
+            None if slopes is None else slopes.data_ptr())
+
+
+def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=False, prefix=None, window=0, cap=0.0, slopes=None, scale=None, out=None,
+                        scratch=None, stream=None):
+    """Attention of sequences that lie behind one another, each within itself: rows offsets[s] .. offsets[s + 1] of q [tq, hq*hd], and of k and v
+    [tk, hkv*hd] (or offsets_k[s] .. offsets_k[s + 1] of them), are sequence s.  CUDA bf16, rows may lie apart; offsets int32 [seqs + 1] on the GPU.
+    causal: row i of nq sees the keys up to nk - nq + i, the last ``window`` of them (0: all), and the first prefix[s] whatever their place.  cap: scores become
+    cap tanh(s / cap); slopes fp32 [hq]: a score loses slopes[h] times the distance.  scale None: 1 / sqrt(hd).  Returns out [tq, hq*hd] bf16; rows that no
+    sequence has are left as they were in ``out`` (without one: undefined), rows that see no key are zeros (see vla_op_attention_packed)."""
+    name = "op_attention_packed"
+    tq, seqs, ld_q, out, ld_out, scale, scratch, p_prefix, p_slopes = _sequences(name, q, offsets, hq, hkv, hd, prefix, slopes, scale, out, scratch, stream, (k, v, offsets_k))
+    tk = k.shape[0]
+    if offsets_k is None:
+        offsets_k = offsets
+        if tk != tq:
+            _refuse(name, "without offsets_k, k and v have q's rows")
+    if k.dim() != 2 or v.dim() != 2 or tk < 1 or tk >> 31 or (hkv * hd) >> 31:
+        _refuse(name, "k and v are matrices of at least one row, below 2^31 of them")
+    ld_k, ld_v = _rows(name, "k is bf16 [tk, hkv*hd]", k, tk, hkv * hd), _rows(name, "v is bf16 [tk, hkv*hd]", v, tk, hkv * hd)
+    rc = (_lib or load_library()).vla_op_attention_packed(
+        q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, out.data_ptr(), ld_out, offsets.data_ptr(), _counts32(name, "offsets_k", offsets_k, seqs + 1), seqs, tq, tk,
+        hq, hkv, hd, scale, int(causal), p_prefix, _c32(name, window), cap, p_slopes, scratch.data_ptr(), scratch.numel(), _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_attention_packed failed")
+    return out
+
+
+def _c32(name, x):
+    if x >> 31:
+        _refuse(name, "window is a number from 0 to 2^31 - 1")
+    return x
+
+
+def _cache(name, k_cache, v_cache, pages, lengths, seqs, width):
+    """Sizes and strides of a cache's two tensors: (n_pages, page_size, max_pages, row_k, page_k, row_v, page_v)."""
+    import torch
+    if k_cache.dim() != 3 or v_cache.shape != k_cache.shape or k_cache.shape[2] != width or k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16:
+        _refuse(name, "k_cache and v_cache are bf16 [n_pages, page_size, hkv*hd]")
+    n, size = k_cache.shape[:2]
+    if k_cache.stride(2) != 1 or v_cache.stride(2) != 1 or n < 1 or size < 1 or n >> 31 or size >> 31:
+        _refuse(name, "the caches' rows are in one piece, at least one page of at least one row, below 2^31 of either")
+    if pages.dim() != 2 or pages.shape[0] != seqs or pages.shape[1] < 1 or pages.dtype != torch.int32 or not pages.is_contiguous() or pages.shape[1] >> 31:
+        _refuse(name, "pages is contiguous int32, [seqs, max_pages]")
+    _counts32(name, "lengths", lengths, seqs)
+    at = []
+    for x in (k_cache, v_cache):                                    # (the stride of a single row or page says nothing)
+        row = x.stride(1) if size > 1 else width
+        at += [row, x.stride(0) if n > 1 else size * row]
+    return n, size, pages.shape[1], at[0], at[1], at[2], at[3]
+
+
+def op_attention_paged(q, k_cache, v_cache, pages, lengths, offsets, hq, hkv, hd, causal=True, prefix=None, window=0, cap=0.0, slopes=None, scale=None, out=None,
+                       scratch=None, stream=None):
+    """``op_attention_packed`` of the new tokens over keys and values that lie in pages: rows offsets[s] .. offsets[s + 1] of q are the last ones of
+    lengths[s] tokens, of which token j is row j % page_size of page pages[s, j // page_size] of k_cache and v_cache [n_pages, page_size, hkv*hd].
+    page_size a multiple of 8; pages int32 [seqs, max_pages], lengths int32 [seqs], offsets int32 [seqs + 1], all on the GPU; entries of ``pages`` behind a
+    sequence's length are not looked at (see vla_op_attention_paged)."""
+    name = "op_attention_paged"
+    tq, seqs, ld_q, out, ld_out, scale, scratch, p_prefix, p_slopes = _sequences(name, q, offsets, hq, hkv, hd, prefix, slopes, scale, out, scratch, stream,
+                                                                                  (k_cache, v_cache, pages, lengths))
+    n, size, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, hkv * hd)
+    rc = (_lib or load_library()).vla_op_attention_paged(
+        q.data_ptr(), ld_q, k_cache.data_ptr(), row_k, page_k, v_cache.data_ptr(), row_v, page_v, out.data_ptr(), ld_out, pages.data_ptr(), lengths.data_ptr(), offsets.data_ptr(),
+        seqs, tq, n, size, most, hq, hkv, hd, scale, int(causal), p_prefix, _c32(name, window), cap, p_slopes, scratch.data_ptr(), scratch.numel(), _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_attention_paged failed")
+    return out
+
+
+def op_cache_store(k, v, k_cache, v_cache, pages, lengths, offsets, stream=None):
+    """New keys and values into the pages that ``op_attention_paged`` reads: rows offsets[s] .. offsets[s + 1] of k and v [t, hkv*hd] (CUDA bf16, rows may lie
+    apart) become the last ones of lengths[s] tokens.  Rows whose place is in front of the first token, behind the table or on a page that does not exist
+    are left out (see vla_op_cache_store)."""
+    name = "op_cache_store"
+    if k.dim() != 2 or v.dim() != 2 or offsets.dim() != 1 or _elsewhere(k, v, k_cache, v_cache, pages, lengths, offsets):
+        _refuse(name, "k and v are matrices on the current CUDA device, like all else")
+    (t, width), seqs = k.shape, offsets.shape[0] - 1
+    if t < 1 or (t | width) >> 31 or seqs < 1:
+        _refuse(name, "at least one row and one sequence, below 2^31 rows")
+    ld_k, ld_v = _rows(name, "k is bf16 [t, hkv*hd]", k, t, width), _rows(name, "v is bf16 [t, hkv*hd]", v, t, width)
+    _counts32(name, "offsets", offsets, seqs + 1)
+    n, size, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, width)
+    rc = (_lib or load_library()).vla_op_cache_store(k.data_ptr(), ld_k, v.data_ptr(), ld_v, k_cache.data_ptr(), row_k, page_k, v_cache.data_ptr(), row_v, page_v, pages.data_ptr(),
+                                                     lengths.data_ptr(), offsets.data_ptr(), seqs, t, n, size, most, width, _stream_ptr(stream))
+    if rc != VLA_OK:
+        raise VlaError(rc, "vla_op_cache_store failed")
 
 
 def op_status(op, scratch=None, stream=None) -> int:

@@ -9,7 +9,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvla_b200.so")
-SOURCES = ["vla_api.cu", "program.cc"]
+SOURCES = ["vla_api.cu", "ops_sequences.cu", "program.cc"]
 HEADERS = []
 
 

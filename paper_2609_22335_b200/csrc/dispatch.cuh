@@ -13,11 +13,6 @@ constexpr int SM_CTL_BYTES = 1024;       // per-worker control block (mbarriers,
 constexpr int SM_STATE_BASE = 8192;      // dispatcher state of the SM
 constexpr int SM_STATE_BYTES = SM_STATE_BASE + MAX_WORKERS * SM_CTL_BYTES;   // then the tile slab, 1024-byte aligned
 
-__device__ __forceinline__ uint64_t gtimer() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
 __device__ __forceinline__ unsigned smid() {
   unsigned s;
   asm volatile("mov.u32 %0, %%smid;" : "=r"(s));
@@ -63,15 +58,6 @@ __device__ __forceinline__ bool bell_wait(const void* bell, uint32_t& parity, ui
       : "memory");
   if (ok) parity ^= 1u;
   return ok != 0;
-}
-
-// ------------------------------------------------------------------ tensor memory (whole-warp calls)
-__device__ __forceinline__ void tmem_alloc(uint32_t* smem_dst, uint32_t cols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(smem_dst)), "r"(cols) : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t cols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
 }
 
 // ------------------------------------------------------------------ tile queues

@@ -6,7 +6,7 @@
 #include <initializer_list>
 
 #include "../../include/vla.h"
-#include "dispatch.cuh"
+#include "attn_tc.cuh"
 #include "per_device.h"
 
 namespace vla {
@@ -112,6 +112,21 @@ inline int op_launch(void (*kernel)(P...), int grid, int threads, int smem, int 
   at[1].val.clusterDim.x = (unsigned)cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? VLA_OK : VLA_ERR_CUDA;
+}
+
+// The same without clusters, in two dimensions.
+template <typename... P, typename... A>
+inline int op_launch_2d(void (*kernel)(P...), int x, int y, int threads, cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at;
+  cfg.gridDim = dim3((unsigned)x, (unsigned)y);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = s;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...) == cudaSuccess ? VLA_OK : VLA_ERR_CUDA;
 }
 

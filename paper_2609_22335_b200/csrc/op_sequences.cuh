@@ -1,0 +1,723 @@
+// Attention of several sequences in one call: packed behind one another, or new tokens over a paged cache; causal, with a prefix that
+// all rows see, over a window, with capped scores and a bias by distance.
+//
+//   s(i, j) = cap tanh(scale q_i . k_j / cap) - slope_h |p_i - j|,    o_i = sum_j softmax_j(s(i, j)) v_j   over the keys j that row i sees
+//
+// One pass over the keys with the running maximum and sum of the softmax.  A tile is 128 rows: the query heads that share a key head side by side,
+// then the next token, so that a key block serves all of them and ragged ends cost little.  Scores and result are tensor-core accumulators (tensor
+// memory), a row a lane; softmax threads own a row each and leave the probabilities, as bf16, in the scores' place, from where the second product
+// takes them.  The running maximum may lag the true one by 2^8, so the result is rescaled on few blocks only.
+//
+// Shares of key blocks (sequences_plan.h) are dealt out evenly, lengths being read on the GPU: a call of one long sequence splits its keys over the
+// chip, one of many short ones has several of them a CTA.  Parts of a split item go to scratch memory in 32 bits; a second kernel puts them together
+// in the order of the shares, so results do not depend on who comes first.
+//
+// Warps: 0-3 and 4-7 softmax (8 and 9 loads and MMAs; in the wide kernel 4 and 5).  K and V blocks share one ring of stages.  Order of the MMAs: with two
+// tiles S0(0) S1(0), then for each block PV0 S0(next) PV1 S1(next), else S(0) S(1), then PV(i) S(i + 2): while one softmax works, the tensor core has
+// the other's products.  S of a later block is issued behind the P V that reads the probabilities in the same columns; MMAs run in the order of issue.
+#pragma once
+#include "op_common.cuh"
+#include "sequences_plan.h"
+
+namespace vla {
+
+constexpr int SEQ_MAX_STAGES = 8;
+// Shared memory for tiles and stages, with 1 KB to begin on a boundary; the rest of the SM's 227 KB is for what is declared in the kernels.
+SEQ_HD int seq_smem(int mode) { return (mode == SEQ_ALTERNATE ? 220 : 225) * 1024; }
+
+struct SeqArgs {
+  const int *offsets_q, *offsets_k;            // packed; paged: offsets_k null and
+  const int *lengths, *pages;                  // keys of each sequence, [seqs, max_pages]
+  const int* prefix;
+  const float* slopes;
+  const unsigned short *q, *k, *v;             // (read key by key where a row's result is not finite)
+  unsigned short* out;
+  char* scratch;                               // header (error word), records, parts
+  long long ld_q, ld_k, ld_v, page_k, page_v, ld_out;
+  int seqs, tq, tk, n_pages, page_size, max_pages, chunk;      // chunk: rows of a box of keys, all of one page
+  int hq, hkv, hd, group, fold, per_group, tokens;             // see SeqFold
+  int causal, window, capped, stages;
+  float scale_log2, cap_in, cap_log2;          // capped scores, in log2 units: cap_log2 tanh(cap_in q.k); others scale_log2 q.k
+};
+struct SeqMaps {
+  alignas(64) CUtensorMap m[3];                // Q {hd, hq, tq}; K, V {hd, hkv, rows of a page, pages}
+};
+struct SeqRecord { int parts, s, unit, first; };      // of an item that begins in this share and ends in a later one; parts = 0: none
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+               ::"r"(dst), "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(tmap), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+      "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+template <int N>
+__device__ __forceinline__ void seq_regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void seq_regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+constexpr int SEQ_REGS_SERVICE = 88, SEQ_REGS_SOFTMAX = 208;     // 128 x 88 + 256 x 208 = 384 x 168
+
+// ---------------------------------------------------------------- a sequence, and the walk over a share's items
+struct Seq { int q0, nq, k0, nk, prefix; };
+__device__ __forceinline__ Seq seq_load(const SeqArgs& a, int s) {
+  Seq r;
+  r.q0 = min(max(__ldcg(a.offsets_q + s), 0), a.tq);
+  r.nq = max(min(__ldcg(a.offsets_q + s + 1), a.tq) - r.q0, 0);
+  if (a.offsets_k) {
+    r.k0 = min(max(__ldcg(a.offsets_k + s), 0), a.tk);
+    r.nk = max(min(__ldcg(a.offsets_k + s + 1), a.tk) - r.k0, 0);
+  } else {
+    r.k0 = 0;
+    r.nk = min(max(__ldcg(a.lengths + s), 0), a.max_pages * a.page_size);
+  }
+  r.prefix = a.prefix && a.causal ? min(max(__ldcg(a.prefix + s), 0), r.nk) : 0;
+  return r;
+}
+__device__ __forceinline__ SeqBlocks seq_blocks_of(const SeqArgs& a, const Seq& q, int first, int tokens, int bn) {
+  return seq_blocks(q.nq, q.nk, q.prefix, first, tokens, bn, a.causal, a.window);
+}
+// Blocks of a sequence over all its items of one unit.
+__device__ __forceinline__ int64_t seq_blocks_all(const SeqArgs& a, const Seq& q, int tokens, int bn) {
+  int64_t n = 0;
+  for (int first = 0; first < q.nq; first += tokens) n += seq_blocks_of(a, q, first, tokens, bn).n;
+  return n;
+}
+__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+struct SeqStart { int64_t total, begin, end; int n, s, unit, first, block; };      // n: shares that have blocks
+// One warp: where share `c` of `ctas` begins.
+__device__ __forceinline__ SeqStart seq_start(const SeqArgs& a, int tokens, int bn, int ctas, int c, int lane) {
+  const int units = a.hkv * a.per_group;
+  int64_t total = 0, mine = 0;
+  for (int s0 = 0; s0 < a.seqs; s0 += 32) {
+    if (s0 + lane < a.seqs) mine += seq_blocks_all(a, seq_load(a, s0 + lane), tokens, bn);
+  }
+  total = units * __shfl_sync(0xffffffffu, warp_scan(mine, lane), 31);
+  SeqStart r;
+  r.total = total;
+  r.n = total < ctas ? (int)total : ctas;
+  r.s = r.unit = r.first = r.block = 0;
+  if (c >= r.n) { r.begin = r.end = 0; return r; }
+  r.begin = seq_share(total, r.n, c); r.end = seq_share(total, r.n, c + 1);
+  int64_t before = 0;
+  for (int s0 = 0; s0 < a.seqs; s0 += 32) {
+    const int64_t own = s0 + lane < a.seqs ? units * seq_blocks_all(a, seq_load(a, s0 + lane), tokens, bn) : 0;
+    const int64_t upto = before + warp_scan(own, lane);
+    const unsigned m = __ballot_sync(0xffffffffu, upto > r.begin);
+    if (m) {
+      const int at = __ffs(m) - 1;
+      const int64_t all = __shfl_sync(0xffffffffu, own, at), in = r.begin - __shfl_sync(0xffffffffu, upto - own, at);
+      r.s = s0 + at;
+      const int64_t each = all / units;
+      r.unit = (int)(in / each);
+      int64_t left = in % each;
+      const Seq q = seq_load(a, r.s);
+      for (;;) {
+        const int n = seq_blocks_of(a, q, r.first, tokens, bn).n;
+        if (left < n) break;
+        left -= n;
+        r.first += tokens;
+      }
+      r.block = (int)left;
+      break;
+    }
+    before = __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return r;
+}
+// The items of a share, one after another; every warp walks for itself.
+struct SeqWalk {
+  int64_t left;                                // blocks of the share from here on
+  int s, unit, first, b0, b1;                  // item, and its blocks that are this share's
+  Seq q;
+  SeqBlocks blocks;
+  int head, kvh, heads;                        // first query head, key head, heads
+  __device__ __forceinline__ void place(const SeqArgs& a, int tokens, int bn) {
+    blocks = seq_blocks_of(a, q, first, tokens, bn);
+    b1 = (int)min((int64_t)blocks.n, b0 + left);
+    kvh = unit / a.per_group;
+    const int part = unit - kvh * a.per_group;
+    head = kvh * a.group + part * a.fold;
+    heads = min(a.fold, a.group - part * a.fold);
+  }
+  __device__ __forceinline__ void begin(const SeqArgs& a, const SeqStart& st, int tokens, int bn) {
+    left = st.end - st.begin; s = st.s; unit = st.unit; first = st.first; b0 = st.block;
+    if (left > 0) { q = seq_load(a, s); place(a, tokens, bn); }
+  }
+  __device__ __forceinline__ void next(const SeqArgs& a, int tokens, int bn) {
+    left -= b1 - b0;
+    if (left <= 0) return;
+    b0 = 0;
+    first += tokens;
+    if (first >= q.nq) {
+      first = 0;
+      if (++unit == a.hkv * a.per_group) {
+        unit = 0;
+        do { ++s; q = seq_load(a, s); } while (q.nq == 0 && s + 1 < a.seqs);
+      }
+    }
+    place(a, tokens, bn);
+  }
+};
+
+// ---------------------------------------------------------------- scores
+// tanh to 32-bit precision, (e - 1) / (e + 1) with e = 2^(2 x log2 e); the fast form is off by 2^-11, which a cap of 50 would turn into a logit's error of 0.02.
+__device__ __forceinline__ float seq_tanh(float x) {
+  const float t = fminf(fabsf(x), 15.0f);      // (NaN: fminf would drop it, see below)
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t * 2.885390082f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  const float y = copysignf(fmaf(-2.0f, r, 1.0f), x);
+  const float small = x * fmaf(x * x, fmaf(x * x, 0.133333333f, -0.333333333f), 1.0f);      // near 0, where 1 - 2 r has few bits left
+  return x != x ? x : (fabsf(x) < 0.07f ? small : y);
+}
+// A score in log2 units: capped, with the bias by distance (d = p - j).
+__device__ __forceinline__ float seq_score(const SeqArgs& a, float dot, float slope_log2, float d) {
+  const float s = a.capped ? a.cap_log2 * seq_tanh(dot * a.cap_in) : dot * a.scale_log2;
+  return fmaf(-slope_log2, fabsf(d), s);
+}
+
+// A row's result key by key, from the keys it sees alone, by one warp: eight head dims a lane.  Where a value that a row does not see is infinite or
+// NaN, the tensor core's 0 x inf spoils the row; such rows are done again this way, which also is what the kernels are checked against.
+struct SeqRow { float m, l, acc[8]; };
+__device__ __noinline__ void seq_row_alone(const SeqArgs& a, const Seq& q, int s, const SeqBlocks& blocks, int b0, int b1, int bn, int token, int head, int kvh, SeqRow& r) {
+  const int lane = threadIdx.x & 31, d0 = 8 * lane, p = q.nk - q.nq + token;
+  const bool have = d0 < a.hd;
+  const SeqSeen seen = seq_seen(p, q.nk, q.prefix, a.causal, a.window);
+  const float slope = a.slopes ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
+  float x[8], y[8];
+  uint4 w = make_uint4(0, 0, 0, 0);
+  if (have) w = *reinterpret_cast<const uint4*>(a.q + (q.q0 + token) * a.ld_q + head * a.hd + d0);
+  unpack8(w, x);
+  r.m = -INFINITY; r.l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.acc[i] = 0.f;
+#pragma unroll 1
+  for (int b = b0; b < b1; ++b) {
+    const int c0 = seq_block(blocks, b) * bn;
+#pragma unroll 1
+    for (int j = c0; j < min(c0 + bn, seen.hi); ++j) {
+      if (j < seen.lo && j >= q.prefix) continue;
+      const unsigned short *kp = a.k + kvh * a.hd + d0, *vp = a.v + kvh * a.hd + d0;
+      bool there = have;
+      if (a.offsets_k) {
+        kp += (q.k0 + j) * a.ld_k; vp += (q.k0 + j) * a.ld_v;
+      } else {
+        const int page = __ldcg(a.pages + (long long)s * a.max_pages + j / a.page_size), in = j % a.page_size;
+        there = have && page >= 0 && page < a.n_pages;             // (a page that does not exist reads as zeros)
+        kp += page * a.page_k + in * a.ld_k; vp += page * a.page_v + in * a.ld_v;
+      }
+      uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
+      if (there) { kw = *reinterpret_cast<const uint4*>(kp); vw = *reinterpret_cast<const uint4*>(vp); }
+      unpack8(kw, y);
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dot = fmaf(x[i], y[i], dot);
+      const float sc = seq_score(a, warp_sum(dot), slope, (float)(p - j));
+      const float m = fmaxf(r.m, sc), keep = r.m == -INFINITY ? 0.f : exp2_fast(r.m - m), e = m == -INFINITY && sc == sc ? 0.f : exp2_fast(sc - m);
+      unpack8(vw, y);
+      r.l = fmaf(r.l, keep, e);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.acc[i] = fmaf(r.acc[i], keep, e * y[i]);
+      r.m = m;
+    }
+  }
+}
+
+// One block of a row's online softmax: BN scores in, BN / 2 pairs of bf16 probabilities out (front half of the registers).
+template <int BN>
+__device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_run, float& l_run, float& alpha) {
+  float m4[4] = {m_run, __uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2])};
+#pragma unroll
+  for (int j = 3; j < BN - 1; j += 2) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
+  float mx = fmaxf(max3(m4[0], m4[1], m4[2]), fmaxf(m4[3], __uint_as_float(sr[BN - 1])));
+  alpha = 1.0f;
+  if (m_run != -INFINITY) {
+    if ((mx - m_run) * sl2 <= ATTN_RESCALE_LOG2) mx = m_run;
+    else alpha = exp2_fast((m_run - mx) * sl2);
+  }
+  const float mb = mx == -INFINITY ? 0.f : -mx * sl2;
+  const uint64_t sl2_2 = pack2(sl2, sl2), mb_2 = pack2(mb, mb);
+  uint64_t s2[2] = {0ull, 0ull};
+#pragma unroll
+  for (int j = 0; j < BN; j += 2) {
+    float p0, p1;
+    unpack2(fma2(pack2(__uint_as_float(sr[j]), __uint_as_float(sr[j + 1])), sl2_2, mb_2), p0, p1);
+    p0 = exp2_fast(p0); p1 = exp2_fast(p1);
+    s2[(j >> 1) & 1] = add2(s2[(j >> 1) & 1], pack2(p0, p1));
+    sr[j >> 1] = pack_bf16(p0, p1);
+  }
+  float x0, x1;
+  unpack2(add2(s2[0], s2[1]), x0, x1);
+  l_run = l_run * alpha + (x0 + x1);
+  m_run = mx;
+}
+// Bits of the columns of a block that begins at key c0 which a row sees, 32 from column 32 w on.
+__device__ __forceinline__ uint32_t seq_mask_word(int hi, int lo, int prefix, int w) {
+  auto below = [w](int n) { const int k = min(max(n - 32 * w, 0), 32); return k == 32 ? 0xFFFFFFFFu : (1u << k) - 1u; };
+  return below(hi) & (~below(lo) | below(prefix));
+}
+// Eight or sixteen columns of a finished row.
+__device__ __forceinline__ void seq_put(unsigned short* o, const float* v, int cols) {
+  *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  if (cols >= 16) *reinterpret_cast<uint4*>(o + 8) = make_uint4(pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]), pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
+}
+__device__ __forceinline__ float* seq_part(const SeqArgs& a, int mode, int share, int which) {
+  const int64_t floats = (int64_t)seq_item_rows(mode) * (seq_cols(a.hd) + 2);
+  return reinterpret_cast<float*>(a.scratch + SEQ_HEADER + SEQ_MAX_CTAS * SEQ_RECORD) + (2 * share + which) * floats;
+}
+__device__ __forceinline__ float2* seq_part_ml(const SeqArgs& a, int mode, float* part) {
+  return reinterpret_cast<float2*>(part + (int64_t)seq_item_rows(mode) * seq_cols(a.hd));
+}
+
+// EXTRA: scores are capped or have a bias by distance.
+template <int MODE, bool EXTRA>
+__global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequences_kernel(const __grid_constant__ SeqArgs a, const __grid_constant__ SeqMaps maps, OpFault fault) {
+  constexpr bool TWO = MODE == SEQ_TWO, ALT = MODE == SEQ_ALTERNATE, WIDE = MODE == SEQ_WIDE;
+  constexpr int BN = WIDE ? 64 : 128, SOFT = WIDE ? 4 : 8;          // keys of a block; softmax warps
+  extern __shared__ char smem_dyn[];
+  __shared__ __align__(8) uint64_t bars[2 * SEQ_MAX_STAGES + 10];
+  __shared__ uint32_t tmem_base_s;
+  __shared__ unsigned failed_s;
+  __shared__ SeqStart start_s;
+  __shared__ float2 ml_s[ALT ? 2 : 1][2][ALT ? SEQ_ROWS : 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, NS = a.stages;
+  const int nbox = (a.hd + 63) / 64, hdc = seq_cols(a.hd), tokens = (TWO ? 2 : 1) * a.tokens;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * SEQ_MAX_STAGES, s_full = empty + 8 * SEQ_MAX_STAGES, p_full = s_full + 16, o_done = p_full + 16,
+                 o_free = o_done + 16, q_full = o_free + 16, q_empty = q_full + 8;
+  const uint32_t tile_bytes = (uint32_t)nbox * (SEQ_ROWS * 128), stage_bytes = (uint32_t)nbox * (BN * 128);
+  const uint32_t Qs = (smem_u32(smem_dyn) + 1023u) & ~1023u, ring = Qs + (TWO ? 2u : 1u) * tile_bytes;
+  unsigned* const err = reinterpret_cast<unsigned*>(a.scratch);
+  SeqRecord* const record = reinterpret_cast<SeqRecord*>(a.scratch + SEQ_HEADER) + blockIdx.x * (SEQ_RECORD / sizeof(SeqRecord));
+  if (warp == SOFT) {
+    if (lane < 2 * SEQ_MAX_STAGES + 10) {
+      const int i = lane - 2 * SEQ_MAX_STAGES;      // s_full 0 1, p_full 2 3, o_done 4 5, o_free 6 7, q_full 8, q_empty 9
+      mbar_init(full + 8u * lane, i == 2 || i == 3 ? 4 : (i == 6 || i == 7 ? (ALT ? 8 : 4) : 1));
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (lane == 0) failed_s = 0;
+  } else if (warp == SOFT + 1) {
+    tmem_alloc(&tmem_base_s, 512);
+  }
+  if (threadIdx.x < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[threadIdx.x]) : "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (warp == 0) {
+    const SeqStart st = seq_start(a, tokens, BN, (int)gridDim.x, (int)blockIdx.x, lane);
+    if (lane == 0) {
+      start_s = st;
+      record->parts = 0;
+      if (blockIdx.x == 0) *err = 0u;
+    }
+  }
+  const OpWaits c = {&failed_s, fault.wait_limit};
+  tc_fence_before();
+  __syncthreads();
+  op_let_next_start();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_s, tmem_o = tmem + 2 * BN;
+  SeqWalk w;
+
+  if (warp >= SOFT) {
+    if (!WIDE) seq_regs_dec<SEQ_REGS_SERVICE>();
+    bool ok = true;
+    if (warp == SOFT && !fault.drop_loads) {
+      // ---------------- loads.  A block of keys is one box of a head's columns, or a box for each piece of a page, issued side by side by the lanes.
+      uint32_t s = 0, ph = 1u, items = 0;
+      const int chunks = BN / a.chunk;
+      w.begin(a, start_s, tokens, BN);
+      for (; w.left > 0 && ok; w.next(a, tokens, BN), ++items) {
+        const int n = w.b1 - w.b0;
+        auto load = [&](int which, int i) {
+          const int c0 = seq_block(w.blocks, w.b0 + i) * BN + lane * a.chunk;
+          int z = w.q.k0 + c0, page = 0;
+          if (!a.offsets_k) {
+            page = lane < chunks && c0 < w.q.nk ? __ldcg(a.pages + (long long)w.s * a.max_pages + c0 / a.page_size) : a.n_pages;      // (none: outside, zeros)
+            z = c0 % a.page_size;
+          }
+          int went = 1;
+          if (lane == 0) {
+            went = mbar_wait(c, empty + 8u * s, ph);
+            if (went) mbar_expect_tx(full + 8u * s, stage_bytes);
+          }
+          ok = __shfl_sync(0xffffffffu, went, 0) != 0;
+          if (!ok) return;
+          if (lane < chunks) {
+            const uint32_t dst = ring + s * stage_bytes + (uint32_t)(lane * a.chunk * 128);
+#pragma unroll 1
+            for (int b = 0; b < nbox; ++b) tma_load_4d(dst + (uint32_t)b * (BN * 128), &maps.m[1 + which], full + 8u * s, b * 64, w.kvh, z, page);
+          }
+          __syncwarp();
+          if (++s == (uint32_t)NS) { s = 0; ph ^= 1u; }
+        };
+        if (lane == 0) {
+          ok = items == 0 || mbar_wait(c, q_empty, (items - 1) & 1u);
+          if (ok) {
+            const uint32_t bytes = (uint32_t)(a.fold * a.tokens * 128);
+            mbar_expect_tx(q_full, (TWO ? 2u : 1u) * (uint32_t)nbox * bytes);
+#pragma unroll 1
+            for (int t = 0; t < (TWO ? 2 : 1); ++t)
+#pragma unroll 1
+              for (int b = 0; b < nbox; ++b)
+                tma_load_3d(Qs + (uint32_t)t * tile_bytes + (uint32_t)b * (SEQ_ROWS * 128), &maps.m[0], q_full, b * 64, w.head, w.q.q0 + w.first + t * a.tokens);
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok) break;
+        if (TWO) {
+          for (int i = 0; i < n && ok; ++i) { load(0, i); if (ok) load(1, i); }
+        } else {
+          load(0, 0);
+          if (ok && n > 1) load(0, 1);
+          for (int i = 0; i < n && ok; ++i) { load(1, i); if (ok && i + 2 < n) load(0, i + 2); }
+        }
+      }
+      if (!ok) for (int i = 0; i < 100; ++i) __nanosleep(1000);        // gave up: the copies in flight land before the CTA ends
+    } else if (warp == SOFT + 1) {
+      // ---------------- MMAs.  A commit covers all MMAs before it, so that S of a later block tells its softmax that P V of the one before is done, too.
+      const uint32_t idesc_s = umma_idesc_bf16(BN), idesc_o = umma_idesc_bf16(hdc) | (1u << 16);      // (second operand MN-major)
+      const uint64_t qdesc = umma_desc_sw128(Qs);
+      uint32_t s = 0, ph = 0u, items = 0, np[2] = {0, 0}, no[2] = {0, 0};      // ring; blocks of a slot so far; items of an accumulator so far
+      auto step = [&]() { if (++s == (uint32_t)NS) { s = 0; ph ^= 1u; } };
+      auto issue_s = [&](int tile, uint32_t stage, int slot) {
+        uint64_t qd = qdesc + (uint32_t)tile * (tile_bytes >> 4), kd = umma_desc_sw128(ring + stage * stage_bytes);
+        const uint32_t ts = tmem + (uint32_t)(BN * slot);
+        int kc = 0;
+#pragma unroll 1
+        for (; kc + 4 <= hdc / 16; kc += 4) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) umma_bf16(ts, qd + 2u * k, kd + 2u * k, idesc_s, (kc | k) != 0 ? 1u : 0u);
+          qd += (SEQ_ROWS * 128) >> 4; kd += (BN * 128) >> 4;
+        }
+#pragma unroll 1
+        for (int k = 0; kc < hdc / 16; ++kc, ++k) umma_bf16(ts, qd + 2u * k, kd + 2u * k, idesc_s, kc != 0 ? 1u : 0u);
+      };
+      auto issue_pv = [&](int slot, uint32_t stage, uint32_t to, bool first) {
+        const uint64_t vd = umma_desc_mn_sw128(ring + stage * stage_bytes, BN * 128);
+        const uint32_t tp = tmem + (uint32_t)(BN * slot);
+#pragma unroll
+        for (int k = 0; k < BN / 16; ++k) umma_bf16_ta(to, tp + 8u * k, vd + (uint64_t)(k * (16 * 128 >> 4)), idesc_o, first && k == 0 ? 0u : 1u);
+      };
+      w.begin(a, start_s, tokens, BN);
+      for (; w.left > 0 && ok; w.next(a, tokens, BN), ++items) {
+        const int n = w.b1 - w.b0;
+        if (!(ok = mbar_wait(c, q_full, items & 1u)) || !(ok = mbar_wait(c, full + 8u * s, ph))) break;
+        tc_fence_after();
+        if (TWO) {
+          if (elect_one()) {
+            issue_s(0, s, 0); umma_commit(s_full);
+            issue_s(1, s, 1); umma_commit(s_full + 8u);
+            umma_commit(empty + 8u * s);
+            if (n == 1) umma_commit(q_empty);
+          }
+          __syncwarp();
+          step();
+          for (int i = 0; i < n && ok; ++i) {
+            const uint32_t sv = s;
+            if (!(ok = mbar_wait(c, full + 8u * s, ph))) break;
+            step();
+            const uint32_t sk = s;
+            const bool more = i + 1 < n;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (t == 0 && more && !(ok = mbar_wait(c, full + 8u * sk, ph))) break;
+              if (!(ok = mbar_wait(c, p_full + 8u * t, np[t] & 1u))) break;
+              ++np[t];
+              if (i == 0) {
+                if (no[t] > 0 && !(ok = mbar_wait(c, o_free + 8u * t, (no[t] - 1) & 1u))) break;
+                ++no[t];
+              }
+              tc_fence_after();
+              if (elect_one()) {
+                issue_pv(t, sv, tmem_o + 128u * t, i == 0);
+                if (more) { issue_s(t, sk, t); umma_commit(s_full + 8u * t); }
+                if (t == 1) {
+                  umma_commit(empty + 8u * sv);
+                  if (more) umma_commit(empty + 8u * sk);
+                  if (i + 2 == n) umma_commit(q_empty);
+                }
+                if (!more) umma_commit(o_done + 8u * t);              // (last: who has seen it has seen all arrivals before)
+              }
+              __syncwarp();
+            }
+            if (more) step();
+          }
+        } else {
+          if (elect_one()) { issue_s(0, s, 0); umma_commit(s_full); umma_commit(empty + 8u * s); if (n == 1) umma_commit(q_empty); }
+          __syncwarp();
+          step();
+          if (n > 1) {
+            if (!(ok = mbar_wait(c, full + 8u * s, ph))) break;
+            tc_fence_after();
+            if (elect_one()) { issue_s(0, s, 1); umma_commit(s_full + 8u); umma_commit(empty + 8u * s); if (n == 2) umma_commit(q_empty); }
+            __syncwarp();
+            step();
+          }
+          for (int i = 0; i < n && ok; ++i) {
+            const int t = i & 1;
+            const uint32_t acc = WIDE ? 0u : (uint32_t)t;
+            const bool first = WIDE ? i == 0 : i < 2;
+            if (!(ok = mbar_wait(c, full + 8u * s, ph)) || !(ok = mbar_wait(c, p_full + 8u * t, np[t] & 1u))) break;
+            ++np[t];
+            if (first) {
+              if (no[acc] > 0 && !(ok = mbar_wait(c, o_free + 8u * acc, (no[acc] - 1) & 1u))) break;
+              ++no[acc];
+            }
+            tc_fence_after();
+            if (elect_one()) {
+              issue_pv(t, s, tmem_o + 128u * acc, first);
+              umma_commit(empty + 8u * s);
+              if (WIDE || i + 2 >= n) umma_commit(o_done + 8u * t);
+            }
+            __syncwarp();
+            step();
+            if (i + 2 < n) {
+              if (!(ok = mbar_wait(c, full + 8u * s, ph))) break;
+              tc_fence_after();
+              if (elect_one()) { issue_s(0, s, t); umma_commit(s_full + 8u * t); umma_commit(empty + 8u * s); if (i + 3 == n) umma_commit(q_empty); }
+              __syncwarp();
+              step();
+            }
+          }
+        }
+      }
+    }
+  } else {
+    // ---------------- softmax: a row a thread.  After a wait that ran out a warp goes on without waiting, through the same named barriers as its partners.
+    if (!WIDE) seq_regs_inc<SEQ_REGS_SOFTMAX>();
+    const int t = warp >> 2, row = (int)threadIdx.x & 127, tt = row / a.fold, hh = row - tt * a.fold;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    bool ok = true;
+    uint32_t ns[2] = {0, 0}, nd[2] = {0, 0}, ring0 = 0, items = 0;      // blocks of a slot, results, ring places and items so far
+    w.begin(a, start_s, tokens, BN);
+    for (; w.left > 0; w.next(a, tokens, BN), ++items) {
+      const int n = w.b1 - w.b0, token = w.first + (TWO ? t * a.tokens : 0) + tt, head = w.head + hh;
+      const bool valid = tt < a.tokens && token < w.q.nq && hh < w.heads;
+      const int p = w.q.nk - w.q.nq + token;
+      SeqSeen seen = seq_seen(p, w.q.nk, w.q.prefix, a.causal, a.window);
+      if (!valid) { seen.hi = INT_MAX / 2; seen.lo = 0; }              // (nobody stores it: nothing to mask)
+      const float slope = EXTRA && a.slopes && valid ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
+      float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll 1
+      for (int i = ALT ? t : 0; i < n; i += ALT ? 2 : 1) {
+        const int slot = TWO ? t : i & 1, c0 = seq_block(w.blocks, w.b0 + i) * BN;
+        const uint32_t ts = tmem + lanes + (uint32_t)(BN * slot);
+        if (ok) ok = mbar_wait(c, s_full + 8u * slot, ns[slot] & 1u);
+        __syncwarp();
+        tc_fence_after();
+        uint32_t sr[BN];
+#pragma unroll
+        for (int k = 0; k < BN; k += 32) tmem_ld32_nowait(ts + k, sr + k);
+        tmem_ld_wait();
+        float sl2 = a.scale_log2;
+        if (EXTRA) {
+          const float d = (float)(p - c0);
+          if (a.capped) {
+#pragma unroll
+            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(a.cap_log2 * seq_tanh(__uint_as_float(sr[j]) * a.cap_in));
+          } else {
+#pragma unroll
+            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(__uint_as_float(sr[j]) * a.scale_log2);
+          }
+          if (a.slopes) {
+#pragma unroll
+            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(fmaf(-slope, fabsf(d - (float)j), __uint_as_float(sr[j])));
+          }
+          sl2 = 1.0f;
+        }
+        if (__any_sync(0xffffffffu, c0 + BN > seen.hi || (c0 < seen.lo && c0 + BN > w.q.prefix))) {
+#pragma unroll
+          for (int k = 0; k < BN / 32; ++k) {
+            const uint32_t bits = seq_mask_word(seen.hi - c0, seen.lo - c0, w.q.prefix - c0, k);
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (!(bits >> j & 1u)) sr[32 * k + j] = 0xFF800000u;
+          }
+        }
+        float alpha;
+        seq_softmax<BN>(sr, sl2, m_run, l_run, alpha);
+        const bool begun = ALT ? i >= 2 : i > 0;
+        if (begun && __any_sync(0xffffffffu, alpha != 1.0f)) {
+          if (WIDE && ok) ok = mbar_wait(c, o_done + 8u * ((i - 1) & 1), (ns[(i - 1) & 1] - 1) & 1u);
+          __syncwarp();
+          tc_fence_after();
+          attn_rescale(tmem_o + lanes + (TWO || ALT ? 128u * t : 0u), hdc, alpha);
+        }
+        // Rows of V behind the last key (of other sequences, or what a page held before) may be anything, and 0 x inf is NaN: they become zeros.
+        if ((TWO ? t == 0 : true) && w.q.nk - c0 < BN) {
+          const uint32_t place = ring0 + (uint32_t)(TWO ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1)), stage = place % (uint32_t)NS;
+          if (ok) ok = mbar_wait(c, full + 8u * stage, place / (uint32_t)NS & 1u);
+          const int from = max(w.q.nk - c0, 0);
+          char* const v0 = smem_dyn + (ring + stage * stage_bytes - smem_u32(smem_dyn));
+          for (int x = from * 8 + row; x < BN * 8; x += 128)
+            for (int b = 0; b < nbox; ++b) *reinterpret_cast<uint4*>(v0 + b * (BN * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+#pragma unroll
+        for (int k = 0; k < BN / 2; k += 16) tmem_st16u(ts + k, sr + k);
+        tmem_st_wait();
+        tc_fence_before();
+        arrive_warp(p_full + 8u * slot, lane);
+        ++ns[slot];
+      }
+      ring0 += 2u * (uint32_t)n;
+      // ---------------- the row's result
+      const bool whole = w.b0 == 0 && w.b1 == w.blocks.n, used = ALT ? t < n : true;
+      if (used) {
+        const int slot = WIDE ? (n - 1) & 1 : t;
+        const uint32_t count = WIDE ? ns[slot] - 1 : nd[t]++;
+        if (ok) ok = mbar_wait(c, o_done + 8u * slot, count & 1u);
+      }
+      __syncwarp();
+      tc_fence_after();
+      float f[2] = {1.0f, 0.f};               // weights of the two accumulators
+      bool both = false;
+      const float unit = EXTRA ? 1.0f : a.scale_log2;
+      m_run *= unit;                          // (log2 units from here on; -inf stays, scale > 0)
+      if (ALT) {
+        ml_s[items & 1][t][row] = make_float2(m_run, l_run);
+        tc_fence_before();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        tc_fence_after();
+        both = n > 1;
+        const float2 x = ml_s[items & 1][0][row], y = both ? ml_s[items & 1][1][row] : make_float2(-INFINITY, 0.f);
+        m_run = fmaxf(x.x, y.x);
+        f[0] = x.x == -INFINITY ? (x.y == 0.f ? 0.f : x.y) : exp2_fast(x.x - m_run);
+        f[1] = y.x == -INFINITY ? (y.y == 0.f ? 0.f : y.y) : exp2_fast(y.x - m_run);
+        l_run = f[0] * x.y;
+        if (both) l_run = fmaf(f[1], y.y, l_run);
+      }
+      float bad = 0.f;
+      const float inv = l_run == 0.f ? (seen.hi > 0 ? NAN : 0.f) : 1.0f / l_run;
+      unsigned short* const o = a.out + (int64_t)(w.q.q0 + token) * a.ld_out + head * a.hd;
+      const int at = (TWO ? t * SEQ_ROWS : 0) + row;
+      float* const part = whole ? nullptr : seq_part(a, MODE, (int)blockIdx.x, w.b0 == 0 ? 1 : 0);
+      const int half = (hdc / 16 + 1) / 2 * 16, lo = ALT && t == 1 ? half : 0, hi = ALT && t == 0 ? half : hdc;
+#pragma unroll 1
+      for (int col = lo; col < hi; col += 16) {
+        float v[16];
+        tmem_ld16(tmem_o + lanes + (TWO ? 128u * t : 0u) + (uint32_t)col, v);
+        if (ALT) {
+          float u[16];
+          if (both) tmem_ld16(tmem_o + lanes + 128u + (uint32_t)col, u);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = both ? fmaf(f[1], u[j], f[0] * v[j]) : f[0] * v[j];
+        }
+        if (whole) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) { v[j] = inv == 0.f ? 0.f : v[j] * inv; bad = fmaf(v[j], 0.f, bad); }
+          if (valid) seq_put(o + col, v, a.hd - col);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) bad = fmaf(v[j], 0.f, bad);
+          if (valid) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(part + at * hdc + col + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          }
+        }
+      }
+      if (!whole && valid && (!ALT || t == 0)) seq_part_ml(a, MODE, part)[at] = make_float2(m_run, l_run);
+      tc_fence_before();
+      if (ALT) {
+        arrive_warp(o_free, lane);
+        if (both) arrive_warp(o_free + 8u, lane);
+      } else {
+        arrive_warp(o_free + 8u * (TWO ? t : 0), lane);
+      }
+      if (threadIdx.x == 0 && !whole && w.b0 == 0) {
+        const int64_t end = start_s.end - w.left + w.blocks.n;
+        *record = SeqRecord{seq_owner(start_s.total, start_s.n, end - 1) - (int)blockIdx.x + 1, w.s, w.unit, w.first};
+      }
+      // Rows that are not finite, once more from the keys they see alone.
+      unsigned again = __ballot_sync(0xffffffffu, valid && seen.hi > 0 && bad != 0.f);
+      while (again) {
+        const int src = __ffs(again) - 1;
+        again &= again - 1;
+        const int r_token = __shfl_sync(0xffffffffu, token, src), r_head = __shfl_sync(0xffffffffu, head, src), r_at = __shfl_sync(0xffffffffu, at, src);
+        const float r_m = __shfl_sync(0xffffffffu, m_run, src);
+        SeqRow r;
+        seq_row_alone(a, w.q, w.s, w.blocks, w.b0, w.b1, BN, r_token, r_head, w.kvh, r);
+        if (8 * lane < a.hd && 8 * lane >= lo && 8 * lane < hi) {      // (a warpgroup's own columns)
+          if (whole) {
+            const float i_ = r.l == 0.f ? NAN : 1.0f / r.l;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r.acc[j] *= i_;
+            seq_put(a.out + (int64_t)(w.q.q0 + r_token) * a.ld_out + r_head * a.hd + 8 * lane, r.acc, 8);
+          } else {                             // (relative to the maximum that the row's sum, which is as it was, is relative to)
+            const float as = r.m == -INFINITY ? 0.f : exp2_fast(r.m - r_m);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r.acc[j] *= as;
+            float4* const x = reinterpret_cast<float4*>(part + r_at * hdc + 8 * lane);
+            x[0] = make_float4(r.acc[0], r.acc[1], r.acc[2], r.acc[3]);
+            x[1] = make_float4(r.acc[4], r.acc[5], r.acc[6], r.acc[7]);
+          }
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (warp == SOFT + 1) tmem_dealloc(tmem, 512);
+  if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(&failed_s) != 0u) *err = (unsigned)DEV_ERR_WAIT_MBAR;
+}
+
+// Parts of the items that were cut, put together: a block for each share that begins such an item and for 32 of its rows, a warp a row.
+constexpr int SEQ_JOIN_THREADS = 256, SEQ_JOIN_ROWS = 32;
+__global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel(const __grid_constant__ SeqArgs a, int mode) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  op_let_next_start();
+  const int share = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, hdc = seq_cols(a.hd);
+  const int4 got = __ldcg(reinterpret_cast<const int4*>(a.scratch + SEQ_HEADER + share * SEQ_RECORD));
+  const int parts = got.x, s = got.y, unit = got.z, first = got.w;
+  if (parts <= 0) return;
+  const Seq q = seq_load(a, s);
+  const int kvh = unit / a.per_group, in = unit - kvh * a.per_group, head0 = kvh * a.group + in * a.fold, heads = min(a.fold, a.group - in * a.fold);
+  for (int r = (int)blockIdx.y * SEQ_JOIN_ROWS + warp; r < min((int)(blockIdx.y + 1) * SEQ_JOIN_ROWS, seq_item_rows(mode)); r += SEQ_JOIN_THREADS / 32) {
+    const int tile = r / SEQ_ROWS, rr = r % SEQ_ROWS, tt = rr / a.fold, hh = rr - tt * a.fold, token = first + tile * a.tokens + tt;
+    if (tt >= a.tokens || token >= q.nq || hh >= heads) continue;
+    float m = -INFINITY;
+    for (int k = lane; k < parts; k += 32) m = fmaxf(m, __ldcg(seq_part_ml(a, mode, seq_part(a, mode, share + k, k == 0 ? 1 : 0)) + r).x);
+    m = warp_max(m);
+    float acc[8], l = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) {
+      float* const part = seq_part(a, mode, share + k, k == 0 ? 1 : 0);
+      const float2 ml = __ldcg(seq_part_ml(a, mode, part) + r);
+      const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : ml.y) : exp2_fast(ml.x - m);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+      if (8 * lane < hdc) {
+        x = __ldcg(reinterpret_cast<const float4*>(part + r * hdc + 8 * lane));
+        y = __ldcg(reinterpret_cast<const float4*>(part + r * hdc + 8 * lane + 4));
+      }
+      if (f != 0.f) {
+        l = fmaf(f, ml.y, l);
+        acc[0] = fmaf(f, x.x, acc[0]); acc[1] = fmaf(f, x.y, acc[1]); acc[2] = fmaf(f, x.z, acc[2]); acc[3] = fmaf(f, x.w, acc[3]);
+        acc[4] = fmaf(f, y.x, acc[4]); acc[5] = fmaf(f, y.y, acc[5]); acc[6] = fmaf(f, y.z, acc[6]); acc[7] = fmaf(f, y.w, acc[7]);
+      }
+    }
+    const float inv = l == 0.f ? (seq_seen(q.nk - q.nq + token, q.nk, q.prefix, a.causal, a.window).hi > 0 ? NAN : 0.f) : 1.0f / l;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] *= inv;
+    if (8 * lane < a.hd) seq_put(a.out + (int64_t)(q.q0 + token) * a.ld_out + (head0 + hh) * a.hd + 8 * lane, acc, 8);
+  }
+}
+
+}  // namespace vla

@@ -915,7 +915,7 @@ int vla_op_status(int32_t op, const void* scratch, void* stream) {
     vla::OpDevice d;
     return vla::op_device(&d) ? vla::op_status_of(d.error_of(op), s) : VLA_ERR_CUDA;
   }
-  if (op == VLA_OP_ATTENTION) {
+  if (op == VLA_OP_ATTENTION || op == VLA_OP_ATTENTION_PACKED || op == VLA_OP_ATTENTION_PAGED) {
     if (!scratch) return VLA_ERR_INVALID;
     return vla::op_status_of(static_cast<const unsigned*>(scratch), s);
   }
