@@ -197,6 +197,20 @@ __device__ __forceinline__ void tmem_st_frag(uint32_t taddr, const float* v) {
         "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
       : "memory");
 }
+// 4 x 4 transposition of one register each over a quad: lane q gets the four lanes' w[q], in lane order.
+__device__ __forceinline__ void quad_transpose(uint32_t* w, int q) {
+  const bool o1 = (q & 1) != 0, o2 = (q & 2) != 0;
+#pragma unroll
+  for (int b = 0; b < 4; b += 2) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, o1 ? w[b] : w[b + 1], 1);
+    if (o1) w[b] = got; else w[b + 1] = got;
+  }
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const uint32_t got = __shfl_xor_sync(0xffffffffu, o2 ? w[b] : w[b + 2], 2);
+    if (o2) w[b] = got; else w[b + 2] = got;
+  }
+}
 // Calls body(c0, v) for the accumulator columns [lo, hi) of this thread's token (one TMEM lane), scaled by rs; the next
 // chunk is on its way from tensor memory meanwhile.
 template <typename F>

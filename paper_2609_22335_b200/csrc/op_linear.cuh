@@ -59,20 +59,6 @@ __device__ __forceinline__ float gelu_exact_f(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
   return x * r;
 }
-// 4 x 4 transposition of one register each over a quad: lane q gets the four lanes' w[q], in lane order.
-__device__ __forceinline__ void quad_transpose(uint32_t* w, int q) {
-  const bool o1 = (q & 1) != 0, o2 = (q & 2) != 0;
-#pragma unroll
-  for (int b = 0; b < 4; b += 2) {
-    const uint32_t got = __shfl_xor_sync(0xffffffffu, o1 ? w[b] : w[b + 1], 1);
-    if (o1) w[b] = got; else w[b + 1] = got;
-  }
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const uint32_t got = __shfl_xor_sync(0xffffffffu, o2 ? w[b] : w[b + 2], 2);
-    if (o2) w[b] = got; else w[b + 2] = got;
-  }
-}
 // One fragment (see tmem_ld_frag) of finished values: rows `row` and `row` + 8 of the output, 32 features from `f`.
 // VEC: features a store may cover (linear_vec).
 template <int VEC>

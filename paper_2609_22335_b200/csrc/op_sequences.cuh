@@ -12,7 +12,7 @@
 // chip, one of many short ones has several of them a CTA.  Parts of a split item go to scratch memory in 32 bits; a second kernel puts them together
 // in the order of the shares, so results do not depend on who comes first.
 //
-// Warps: 0-3 and 4-7 softmax (8 and 9 loads and MMAs; in the wide kernel 4 and 5).  K and V blocks share one ring of stages.  Order of the MMAs: with two
+// Warps: 0-3, with two tiles 4-7 too, softmax; the next loads, the one after that MMAs.  K and V blocks share one ring of stages.  Order of the MMAs: with two
 // tiles S0(0) S1(0), then for each block PV0 S0(next) PV1 S1(next), else S(0) S(1), then PV(i) S(i + 2): while one softmax works, the tensor core has
 // the other's products.  S of a later block is issued behind the P V that reads the probabilities in the same columns; MMAs run in the order of issue.
 #pragma once
@@ -22,8 +22,6 @@
 namespace vla {
 
 constexpr int SEQ_MAX_STAGES = 8;
-// Shared memory for tiles and stages, with 1 KB to begin on a boundary; the rest of the SM's 227 KB is for what is declared in the kernels.
-SEQ_HD int seq_smem(int mode) { return (mode == SEQ_ALTERNATE ? 220 : 225) * 1024; }
 
 struct SeqArgs {
   const int *offsets_q, *offsets_k;            // packed; paged: offsets_k null and
@@ -35,6 +33,7 @@ struct SeqArgs {
   char* scratch;                               // header (error word), records, parts
   long long ld_q, ld_k, ld_v, page_k, page_v, ld_out;
   int seqs, tq, tk, n_pages, page_size, max_pages, chunk;      // chunk: rows of a box of keys, all of one page
+  uint32_t page_magic, page_shift;             // x / page_size = x * page_magic >> page_shift for x below 2^31
   int hq, hkv, hd, group, fold, per_group, tokens;             // see SeqFold
   int causal, window, capped, stages;
   float scale_log2, cap_in, cap_log2;          // capped scores, in log2 units: cap_log2 tanh(cap_in q.k); others scale_log2 q.k
@@ -42,7 +41,7 @@ struct SeqArgs {
 struct SeqMaps {
   alignas(64) CUtensorMap m[3];                // Q {hd, hq, tq}; K, V {hd, hkv, rows of a page, pages}
 };
-struct SeqRecord { int parts, s, unit, first; };      // of an item that begins in this share and ends in a later one; parts = 0: none
+struct SeqRecord { int parts, s, head, first; };      // of an item that begins in this share and ends in a later one; parts = 0: none
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -88,93 +87,145 @@ __device__ __forceinline__ Seq seq_load(const SeqArgs& a, int s) {
 __device__ __forceinline__ SeqBlocks seq_blocks_of(const SeqArgs& a, const Seq& q, int first, int tokens, int bn) {
   return seq_blocks(q.nq, q.nk, q.prefix, first, tokens, bn, a.causal, a.window);
 }
-// Blocks of a sequence over all its items of one unit.
-__device__ __forceinline__ int64_t seq_blocks_all(const SeqArgs& a, const Seq& q, int tokens, int bn) {
-  int64_t n = 0;
-  for (int first = 0; first < q.nq; first += tokens) n += seq_blocks_of(a, q, first, tokens, bn).n;
-  return n;
-}
-__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {
+__device__ __forceinline__ int warp_scan(int v, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, v, o);
+    const int x = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += x;
   }
   return v;
 }
-struct SeqStart { int64_t total, begin, end; int n, s, unit, first, block; };      // n: shares that have blocks
-// One warp: where share `c` of `ctas` begins.
-__device__ __forceinline__ SeqStart seq_start(const SeqArgs& a, int tokens, int bn, int ctas, int c, int lane) {
-  const int units = a.hkv * a.per_group;
-  int64_t total = 0, mine = 0;
-  for (int s0 = 0; s0 < a.seqs; s0 += 32) {
-    if (s0 + lane < a.seqs) mine += seq_blocks_all(a, seq_load(a, s0 + lane), tokens, bn);
-  }
-  total = units * __shfl_sync(0xffffffffu, warp_scan(mine, lane), 31);
-  SeqStart r;
-  r.total = total;
-  r.n = total < ctas ? (int)total : ctas;
-  r.s = r.unit = r.first = r.block = 0;
-  if (c >= r.n) { r.begin = r.end = 0; return r; }
-  r.begin = seq_share(total, r.n, c); r.end = seq_share(total, r.n, c + 1);
-  int64_t before = 0;
-  for (int s0 = 0; s0 < a.seqs; s0 += 32) {
-    const int64_t own = s0 + lane < a.seqs ? units * seq_blocks_all(a, seq_load(a, s0 + lane), tokens, bn) : 0;
-    const int64_t upto = before + warp_scan(own, lane);
-    const unsigned m = __ballot_sync(0xffffffffu, upto > r.begin);
-    if (m) {
-      const int at = __ffs(m) - 1;
-      const int64_t all = __shfl_sync(0xffffffffu, own, at), in = r.begin - __shfl_sync(0xffffffffu, upto - own, at);
-      r.s = s0 + at;
-      const int64_t each = all / units;
-      r.unit = (int)(in / each);
-      int64_t left = in % each;
-      const Seq q = seq_load(a, r.s);
-      for (;;) {
-        const int n = seq_blocks_of(a, q, r.first, tokens, bn).n;
-        if (left < n) break;
-        left -= n;
-        r.first += tokens;
-      }
-      r.block = (int)left;
-      break;
-    }
-    before = __shfl_sync(0xffffffffu, upto, 31);
-  }
+__device__ __forceinline__ Seq seq_of_lane(const Seq& q, int src) {
+  Seq r;
+  r.q0 = __shfl_sync(0xffffffffu, q.q0, src); r.nq = __shfl_sync(0xffffffffu, q.nq, src);
+  r.k0 = __shfl_sync(0xffffffffu, q.k0, src); r.nk = __shfl_sync(0xffffffffu, q.nk, src);
+  r.prefix = __shfl_sync(0xffffffffu, q.prefix, src);
   return r;
 }
-// The items of a share, one after another; every warp walks for itself.
-struct SeqWalk {
-  int64_t left;                                // blocks of the share from here on
-  int s, unit, first, b0, b1;                  // item, and its blocks that are this share's
-  Seq q;
-  SeqBlocks blocks;
-  int head, kvh, heads;                        // first query head, key head, heads
-  __device__ __forceinline__ void place(const SeqArgs& a, int tokens, int bn) {
-    blocks = seq_blocks_of(a, q, first, tokens, bn);
-    b1 = (int)min((int64_t)blocks.n, b0 + left);
-    kvh = unit / a.per_group;
-    const int part = unit - kvh * a.per_group;
-    head = kvh * a.group + part * a.fold;
-    heads = min(a.fold, a.group - part * a.fold);
-  }
-  __device__ __forceinline__ void begin(const SeqArgs& a, const SeqStart& st, int tokens, int bn) {
-    left = st.end - st.begin; s = st.s; unit = st.unit; first = st.first; b0 = st.block;
-    if (left > 0) { q = seq_load(a, s); place(a, tokens, bn); }
-  }
-  __device__ __forceinline__ void next(const SeqArgs& a, int tokens, int bn) {
-    left -= b1 - b0;
-    if (left <= 0) return;
-    b0 = 0;
-    first += tokens;
-    if (first >= q.nq) {
-      first = 0;
-      if (++unit == a.hkv * a.per_group) {
-        unit = 0;
-        do { ++s; q = seq_load(a, s); } while (q.nq == 0 && s + 1 < a.seqs);
+// One warp: the ticks of the 32 items of one sequence and unit from token f0 on, an item a lane.
+__device__ __forceinline__ int seq_ticks32(const SeqArgs& a, const Seq& x, int f0, int tokens, int bn, int w, int lane) {
+  const int64_t first = f0 + (int64_t)lane * tokens;
+  return first < x.nq ? w + seq_blocks_of(a, x, (int)first, tokens, bn).n : 0;
+}
+// The share's first item (of unit, sequence s, tokens from `first` on), its first tick of it, and where the share ends.
+struct SeqStart { SeqShares shares; int64_t left; int s, unit, first, tick; bool whole; Seq q; };
+// One warp: where share `c` begins.  A sequence a lane; those of several items are summed by all lanes together, one after another.
+__device__ __forceinline__ SeqStart seq_start(const SeqArgs& a, int tokens, int bn, int w, int most, int c, int lane) {
+  const int units = a.hkv * a.per_group;
+  int all = 0, longest = 0, own = 0;           // ticks of one unit; the most of an item; of this lane's sequence
+  Seq q = {0, 0, 0, 0, 0};
+  auto count = [&](int s0) {
+    q = {0, 0, 0, 0, 0};
+    if (s0 + lane < a.seqs) q = seq_load(a, s0 + lane);
+    own = q.nq > 0 ? w + seq_blocks_of(a, q, 0, tokens, bn).n : 0;
+    longest = max(longest, own);
+    unsigned many = __ballot_sync(0xffffffffu, q.nq > tokens);
+    const int most_tokens = (int)__reduce_max_sync(0xffffffffu, (unsigned)q.nq);
+    if (many && most_tokens <= (int64_t)8 * __popc(many) * tokens) {      // few items each: every lane its own
+      for (int64_t f0 = tokens; f0 < q.nq; f0 += tokens) {
+        const int n = w + seq_blocks_of(a, q, (int)f0, tokens, bn).n;
+        own += n;
+        longest = max(longest, n);
       }
+      many = 0;
     }
-    place(a, tokens, bn);
+    for (; many; many &= many - 1) {           // many items: all lanes one sequence after another
+      const int src = __ffs(many) - 1;
+      const Seq x = seq_of_lane(q, src);
+      int sum = 0;
+      for (int64_t f0 = 0; f0 < x.nq; f0 += 32 * (int64_t)tokens) {
+        const int n = seq_ticks32(a, x, (int)f0, tokens, bn, w, lane);
+        sum += n;
+        longest = max(longest, n);
+      }
+      sum = __reduce_add_sync(0xffffffffu, sum);
+      if (lane == src) own = sum;
+    }
+  };
+  for (int s0 = 0; s0 < a.seqs; s0 += 32) {
+    count(s0);
+    all += __reduce_add_sync(0xffffffffu, own);
+  }
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  SeqStart r;
+  r.shares = seq_shares_of((int64_t)all * units, most);
+  r.left = 0;
+  if (c >= r.shares.n) return r;
+  r.whole = seq_whole(r.shares, longest, w);
+  const int64_t begin = seq_share(r.shares, c);
+  r.left = seq_share(r.shares, c + 1) - begin;
+  r.unit = (int)seq_div(begin, all);
+  int in = (int)(begin - (int64_t)r.unit * all);
+  // (The loops end whatever the offsets are, even if somebody changes them meanwhile.)
+  r.s = -1;
+  for (int s0 = 0; s0 < a.seqs; s0 += 32) {
+    if (a.seqs > 32) count(s0);
+    const int upto = warp_scan(own, lane);
+    const unsigned m = __ballot_sync(0xffffffffu, upto > in);
+    if (m) {
+      const int at = __ffs(m) - 1;
+      in -= __shfl_sync(0xffffffffu, upto - own, at);
+      r.s = s0 + at;
+      r.q = seq_of_lane(q, at);
+      break;
+    }
+    in -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  r.first = -1;
+  for (int64_t f0 = 0; r.s >= 0 && f0 < r.q.nq; f0 += 32 * (int64_t)tokens) {
+    const int n = seq_ticks32(a, r.q, (int)f0, tokens, bn, w, lane), upto = warp_scan(n, lane);
+    const unsigned m = __ballot_sync(0xffffffffu, upto > in);
+    if (m) {
+      const int l = __ffs(m) - 1;
+      r.first = (int)(f0 + (int64_t)l * tokens);
+      r.tick = in - __shfl_sync(0xffffffffu, upto - n, l);
+      break;
+    }
+    in -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  if (r.first < 0) r.left = 0;
+  return r;
+}
+// An item as the loading warp tells the others of it.
+struct __align__(16) SeqItem {
+  int n, b0, na, lo;                           // blocks to do (0: no item any more), the first of them, see SeqBlocks
+  int first, q0, nq, nk;
+  int prefix, head, heads, kvh;
+  int s, k0, part, blocks;                     // part: -1 the whole item, 0 its end or middle, 1 its beginning
+};
+// The items of a share, one after another (one warp).
+struct SeqWalk {
+  int64_t left;                                // ticks of the share from here on
+  int s, unit, first, tick;
+  Seq q;
+  // The item here, and on to the next one.  Items of no blocks (their beginning alone is this share's) are none.
+  __device__ __forceinline__ SeqItem take(const SeqArgs& a, bool whole, int tokens, int bn, int w) {
+    SeqItem it;
+    it.n = 0;
+    if (left <= 0) return it;
+    const SeqBlocks blocks = seq_blocks_of(a, q, first, tokens, bn);
+    const int all = w + blocks.n, end = whole ? all : (int)min((int64_t)all, tick + left);
+    it.b0 = max(0, tick - w);
+    it.n = max(0, end - w) - it.b0;
+    it.na = blocks.na; it.lo = blocks.lo; it.blocks = blocks.n;
+    it.first = first; it.q0 = q.q0; it.nq = q.nq; it.nk = q.nk; it.prefix = q.prefix; it.k0 = q.k0; it.s = s;
+    it.kvh = a.per_group == 1 ? unit : unit / a.per_group;
+    const int in = unit - it.kvh * a.per_group;
+    it.head = it.kvh * a.group + in * a.fold;
+    it.heads = min(a.fold, a.group - in * a.fold);
+    it.part = it.n == blocks.n ? -1 : (it.b0 == 0 ? 1 : 0);
+    left -= end - tick;
+    tick = 0;
+    first += tokens;
+    if (first >= q.nq && left > 0) {
+      first = 0;
+      do {
+        if (++s == a.seqs) { s = 0; ++unit; }
+        if (unit == a.hkv * a.per_group) { left = 0; break; }
+        q = seq_load(a, s);
+      } while (q.nq == 0);                     // (there is one: the share goes on)
+    }
+    return it;
   }
 };
 
@@ -198,7 +249,7 @@ __device__ __forceinline__ float seq_score(const SeqArgs& a, float dot, float sl
 // A row's result key by key, from the keys it sees alone, by one warp: eight head dims a lane.  Where a value that a row does not see is infinite or
 // NaN, the tensor core's 0 x inf spoils the row; such rows are done again this way, which also is what the kernels are checked against.
 struct SeqRow { float m, l, acc[8]; };
-__device__ __noinline__ void seq_row_alone(const SeqArgs& a, const Seq& q, int s, const SeqBlocks& blocks, int b0, int b1, int bn, int token, int head, int kvh, SeqRow& r) {
+__device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, int bn, int token, int head, SeqRow& r) {
   const int lane = threadIdx.x & 31, d0 = 8 * lane, p = q.nk - q.nq + token;
   const bool have = d0 < a.hd;
   const SeqSeen seen = seq_seen(p, q.nk, q.prefix, a.causal, a.window);
@@ -211,17 +262,17 @@ __device__ __noinline__ void seq_row_alone(const SeqArgs& a, const Seq& q, int s
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.acc[i] = 0.f;
 #pragma unroll 1
-  for (int b = b0; b < b1; ++b) {
-    const int c0 = seq_block(blocks, b) * bn;
+  for (int b = q.b0; b < q.b0 + q.n; ++b) {
+    const int c0 = seq_block(SeqBlocks{q.na, q.lo, 0}, b) * bn;
 #pragma unroll 1
     for (int j = c0; j < min(c0 + bn, seen.hi); ++j) {
       if (j < seen.lo && j >= q.prefix) continue;
-      const unsigned short *kp = a.k + kvh * a.hd + d0, *vp = a.v + kvh * a.hd + d0;
+      const unsigned short *kp = a.k + q.kvh * a.hd + d0, *vp = a.v + q.kvh * a.hd + d0;
       bool there = have;
       if (a.offsets_k) {
         kp += (q.k0 + j) * a.ld_k; vp += (q.k0 + j) * a.ld_v;
       } else {
-        const int page = __ldcg(a.pages + (long long)s * a.max_pages + j / a.page_size), in = j % a.page_size;
+        const int page = __ldcg(a.pages + (long long)q.s * a.max_pages + j / a.page_size), in = j % a.page_size;
         there = have && page >= 0 && page < a.n_pages;             // (a page that does not exist reads as zeros)
         kp += page * a.page_k + in * a.ld_k; vp += page * a.page_v + in * a.ld_v;
       }
@@ -270,6 +321,15 @@ __device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_ru
   l_run = l_run * alpha + (x0 + x1);
   m_run = mx;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t* v) {      // 32 bytes on their boundary
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
 // Bits of the columns of a block that begins at key c0 which a row sees, 32 from column 32 w on.
 __device__ __forceinline__ uint32_t seq_mask_word(int hi, int lo, int prefix, int w) {
   auto below = [w](int n) { const int k = min(max(n - 32 * w, 0), 32); return k == 32 ? 0xFFFFFFFFu : (1u << k) - 1u; };
@@ -281,24 +341,25 @@ __device__ __forceinline__ void seq_put(unsigned short* o, const float* v, int c
   if (cols >= 16) *reinterpret_cast<uint4*>(o + 8) = make_uint4(pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]), pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
 }
 __device__ __forceinline__ float* seq_part(const SeqArgs& a, int mode, int share, int which) {
-  const int64_t floats = (int64_t)seq_item_rows(mode) * (seq_cols(a.hd) + 2);
-  return reinterpret_cast<float*>(a.scratch + SEQ_HEADER + SEQ_MAX_CTAS * SEQ_RECORD) + (2 * share + which) * floats;
+  return reinterpret_cast<float*>(a.scratch + SEQ_HEADER + SEQ_MAX_SHARES * SEQ_RECORD) + (2 * share + which) * seq_part_floats(mode, a.hd);
 }
 __device__ __forceinline__ float2* seq_part_ml(const SeqArgs& a, int mode, float* part) {
   return reinterpret_cast<float2*>(part + (int64_t)seq_item_rows(mode) * seq_cols(a.hd));
 }
 
+constexpr int seq_threads(int mode) { return mode == SEQ_TWO ? 384 : 192; }
 // EXTRA: scores are capped or have a bias by distance.
 template <int MODE, bool EXTRA>
-__global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequences_kernel(const __grid_constant__ SeqArgs a, const __grid_constant__ SeqMaps maps, OpFault fault) {
-  constexpr bool TWO = MODE == SEQ_TWO, ALT = MODE == SEQ_ALTERNATE, WIDE = MODE == SEQ_WIDE;
-  constexpr int BN = WIDE ? 64 : 128, SOFT = WIDE ? 4 : 8;          // keys of a block; softmax warps
+__global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vla_op_sequences_kernel(const __grid_constant__ SeqArgs a, const __grid_constant__ SeqMaps maps, OpFault fault) {
+  constexpr bool TWO = MODE == SEQ_TWO;
+  constexpr int W = seq_item_ticks(MODE);
+  constexpr int BN = TWO ? 128 : 64, SOFT = TWO ? 8 : 4;              // keys of a block; softmax warps
+  constexpr uint32_t COLS = MODE == SEQ_ONE ? 256 : 512;              // tensor memory: two tiles of scores, then the results
   extern __shared__ char smem_dyn[];
   __shared__ __align__(8) uint64_t bars[2 * SEQ_MAX_STAGES + 10];
   __shared__ uint32_t tmem_base_s;
   __shared__ unsigned failed_s;
-  __shared__ SeqStart start_s;
-  __shared__ float2 ml_s[ALT ? 2 : 1][2][ALT ? SEQ_ROWS : 1];
+  __shared__ SeqItem item_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, NS = a.stages;
   const int nbox = (a.hd + 63) / 64, hdc = seq_cols(a.hd), tokens = (TWO ? 2 : 1) * a.tokens;
   const uint32_t full = smem_u32(bars), empty = full + 8 * SEQ_MAX_STAGES, s_full = empty + 8 * SEQ_MAX_STAGES, p_full = s_full + 16, o_done = p_full + 16,
@@ -310,22 +371,18 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
   if (warp == SOFT) {
     if (lane < 2 * SEQ_MAX_STAGES + 10) {
       const int i = lane - 2 * SEQ_MAX_STAGES;      // s_full 0 1, p_full 2 3, o_done 4 5, o_free 6 7, q_full 8, q_empty 9
-      mbar_init(full + 8u * lane, i == 2 || i == 3 ? 4 : (i == 6 || i == 7 ? (ALT ? 8 : 4) : 1));
+      mbar_init(full + 8u * lane, i == 2 || i == 3 || i == 6 || i == 7 ? 4 : (i == 9 ? 1 + SOFT : 1));
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (lane == 0) failed_s = 0;
   } else if (warp == SOFT + 1) {
-    tmem_alloc(&tmem_base_s, 512);
+    tmem_alloc(&tmem_base_s, COLS);
   }
   if (threadIdx.x < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[threadIdx.x]) : "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (warp == 0) {
-    const SeqStart st = seq_start(a, tokens, BN, (int)gridDim.x, (int)blockIdx.x, lane);
-    if (lane == 0) {
-      start_s = st;
-      record->parts = 0;
-      if (blockIdx.x == 0) *err = 0u;
-    }
+  if (threadIdx.x == 0) {
+    record->parts = 0;
+    if (blockIdx.x == 0) *err = 0u;
   }
   const OpWaits c = {&failed_s, fault.wait_limit};
   tc_fence_before();
@@ -333,61 +390,83 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
   op_let_next_start();
   tc_fence_after();
   const uint32_t tmem = tmem_base_s, tmem_o = tmem + 2 * BN;
-  SeqWalk w;
 
   if (warp >= SOFT) {
-    if (!WIDE) seq_regs_dec<SEQ_REGS_SERVICE>();
+    if (TWO) seq_regs_dec<SEQ_REGS_SERVICE>();
     bool ok = true;
     if (warp == SOFT && !fault.drop_loads) {
       // ---------------- loads.  A block of keys is one box of a head's columns, or a box for each piece of a page, issued side by side by the lanes.
       uint32_t s = 0, ph = 1u, items = 0;
       const int chunks = BN / a.chunk;
-      w.begin(a, start_s, tokens, BN);
-      for (; w.left > 0 && ok; w.next(a, tokens, BN), ++items) {
-        const int n = w.b1 - w.b0;
-        auto load = [&](int which, int i) {
-          const int c0 = seq_block(w.blocks, w.b0 + i) * BN + lane * a.chunk;
-          int z = w.q.k0 + c0, page = 0;
-          if (!a.offsets_k) {
-            page = lane < chunks && c0 < w.q.nk ? __ldcg(a.pages + (long long)w.s * a.max_pages + c0 / a.page_size) : a.n_pages;      // (none: outside, zeros)
-            z = c0 % a.page_size;
-          }
-          int went = 1;
-          if (lane == 0) {
-            went = mbar_wait(c, empty + 8u * s, ph);
-            if (went) mbar_expect_tx(full + 8u * s, stage_bytes);
-          }
-          ok = __shfl_sync(0xffffffffu, went, 0) != 0;
-          if (!ok) return;
-          if (lane < chunks) {
-            const uint32_t dst = ring + s * stage_bytes + (uint32_t)(lane * a.chunk * 128);
-#pragma unroll 1
-            for (int b = 0; b < nbox; ++b) tma_load_4d(dst + (uint32_t)b * (BN * 128), &maps.m[1 + which], full + 8u * s, b * 64, w.kvh, z, page);
-          }
-          __syncwarp();
-          if (++s == (uint32_t)NS) { s = 0; ph ^= 1u; }
-        };
+      const SeqStart st = seq_start(a, tokens, BN, W, (int)gridDim.x, (int)blockIdx.x, lane);
+      SeqWalk walk = {st.left, st.s, st.unit, st.first, st.tick, st.q};
+      if (st.whole && st.tick > 0) walk.take(a, true, tokens, BN, W);      // (that item is the share's before)
+      for (;; ++items) {
+        const SeqItem w = walk.take(a, st.whole, tokens, BN, W);
+        const int n = w.n;
         if (lane == 0) {
-          ok = items == 0 || mbar_wait(c, q_empty, (items - 1) & 1u);
+          ok = items == 0 || mbar_wait(c, q_empty, (items - 1) & 1u);      // Q's tiles are free, and everybody knows the item before
           if (ok) {
-            const uint32_t bytes = (uint32_t)(a.fold * a.tokens * 128);
-            mbar_expect_tx(q_full, (TWO ? 2u : 1u) * (uint32_t)nbox * bytes);
+            item_s = w;
+            if (n == 0) {
+              asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(q_full) : "memory");
+            } else {
+              const uint32_t bytes = (uint32_t)(a.fold * a.tokens * 128);
+              mbar_expect_tx(q_full, (TWO ? 2u : 1u) * (uint32_t)nbox * bytes);
 #pragma unroll 1
-            for (int t = 0; t < (TWO ? 2 : 1); ++t)
+              for (int t = 0; t < (TWO ? 2 : 1); ++t)
 #pragma unroll 1
-              for (int b = 0; b < nbox; ++b)
-                tma_load_3d(Qs + (uint32_t)t * tile_bytes + (uint32_t)b * (SEQ_ROWS * 128), &maps.m[0], q_full, b * 64, w.head, w.q.q0 + w.first + t * a.tokens);
+                for (int b = 0; b < nbox; ++b)
+                  tma_load_3d(Qs + (uint32_t)t * tile_bytes + (uint32_t)b * (SEQ_ROWS * 128), &maps.m[0], q_full, b * 64, w.head, w.q0 + w.first + t * a.tokens);
+              if (w.part == 1) {               // (the item's last tick lies behind the share's end by as many as its blocks that are left)
+                const int64_t last = seq_share(st.shares, (int)blockIdx.x + 1) + w.blocks - n - 1;
+                *record = SeqRecord{seq_owner(st.shares, last) - (int)blockIdx.x + 1, w.s, w.head, w.first};
+              }
+            }
           }
         }
         ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-        if (!ok) break;
-        if (TWO) {
-          for (int i = 0; i < n && ok; ++i) { load(0, i); if (ok) load(1, i); }
-        } else {
-          load(0, 0);
-          if (ok && n > 1) load(0, 1);
-          for (int i = 0; i < n && ok; ++i) { load(1, i); if (ok && i + 2 < n) load(0, i + 2); }
+        if (!ok || n == 0) break;
+        // The order in which the blocks' MMAs come: K0 V0 K1 V1 .. with two tiles, else K0 K1 V0 K2 V1 .. V(n-2) V(n-1).  A page's number is asked for a block ahead.
+        struct Box { int which, z, page; };
+        auto box = [&](int m) {
+          Box x;
+          int i;
+          if (TWO) {
+            x.which = m & 1; i = m >> 1;
+          } else {
+            i = (m + 1) >> 1;
+            x.which = m > 0 && (!(m & 1) || i >= n) ? 1 : 0;
+            if (x.which) i = m & 1 ? n - 1 : i - 1;
+          }
+          const int c0 = seq_block(SeqBlocks{w.na, w.lo, 0}, w.b0 + i) * BN + lane * a.chunk;
+          x.z = w.k0 + c0; x.page = 0;
+          if (!a.offsets_k) {
+            const int slot = (int)((uint64_t)(uint32_t)c0 * a.page_magic >> a.page_shift);
+            x.z = c0 - slot * a.page_size;
+            x.page = a.n_pages;                // (outside: zeros)
+            if (lane < chunks && c0 < w.nk) x.page = __ldcg(a.pages + (long long)w.s * a.max_pages + slot);
+          }
+          return x;
+        };
+        Box next = box(0);
+#pragma unroll 1
+        for (int m = 0; m < 2 * n; ++m) {
+          const Box x = next;
+          if (m + 1 < 2 * n) next = box(m + 1);
+          const uint32_t bar = full + 8u * s, dst = ring + s * stage_bytes + (uint32_t)(lane * a.chunk * 128);
+          ok = __all_sync(0xffffffffu, mbar_wait(c, empty + 8u * s, ph));
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(bar, stage_bytes);
+          __syncwarp();
+          if (lane < chunks) {
+#pragma unroll 1
+            for (int b = 0; b < nbox; ++b) tma_load_4d(dst + (uint32_t)b * (BN * 128), &maps.m[1 + x.which], bar, b * 64, w.kvh, x.z, x.page);
+          }
+          if (++s == (uint32_t)NS) { s = 0; ph ^= 1u; }
         }
+        __syncwarp();
+        if (!ok) break;
       }
       if (!ok) for (int i = 0; i < 100; ++i) __nanosleep(1000);        // gave up: the copies in flight land before the CTA ends
     } else if (warp == SOFT + 1) {
@@ -415,10 +494,10 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
 #pragma unroll
         for (int k = 0; k < BN / 16; ++k) umma_bf16_ta(to, tp + 8u * k, vd + (uint64_t)(k * (16 * 128 >> 4)), idesc_o, first && k == 0 ? 0u : 1u);
       };
-      w.begin(a, start_s, tokens, BN);
-      for (; w.left > 0 && ok; w.next(a, tokens, BN), ++items) {
-        const int n = w.b1 - w.b0;
-        if (!(ok = mbar_wait(c, q_full, items & 1u)) || !(ok = mbar_wait(c, full + 8u * s, ph))) break;
+      for (; ok; ++items) {
+        if (!(ok = mbar_wait(c, q_full, items & 1u))) break;
+        const int n = *reinterpret_cast<volatile int*>(&item_s.n);
+        if (n == 0 || !(ok = mbar_wait(c, full + 8u * s, ph))) break;
         tc_fence_after();
         if (TWO) {
           if (elect_one()) {
@@ -472,19 +551,17 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
           }
           for (int i = 0; i < n && ok; ++i) {
             const int t = i & 1;
-            const uint32_t acc = WIDE ? 0u : (uint32_t)t;
-            const bool first = WIDE ? i == 0 : i < 2;
             if (!(ok = mbar_wait(c, full + 8u * s, ph)) || !(ok = mbar_wait(c, p_full + 8u * t, np[t] & 1u))) break;
             ++np[t];
-            if (first) {
-              if (no[acc] > 0 && !(ok = mbar_wait(c, o_free + 8u * acc, (no[acc] - 1) & 1u))) break;
-              ++no[acc];
+            if (i == 0) {
+              if (no[0] > 0 && !(ok = mbar_wait(c, o_free, (no[0] - 1) & 1u))) break;
+              ++no[0];
             }
             tc_fence_after();
             if (elect_one()) {
-              issue_pv(t, s, tmem_o + 128u * acc, first);
+              issue_pv(t, s, tmem_o, i == 0);
               umma_commit(empty + 8u * s);
-              if (WIDE || i + 2 >= n) umma_commit(o_done + 8u * t);
+              umma_commit(o_done + 8u * t);
             }
             __syncwarp();
             step();
@@ -501,23 +578,27 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
     }
   } else {
     // ---------------- softmax: a row a thread.  After a wait that ran out a warp goes on without waiting, through the same named barriers as its partners.
-    if (!WIDE) seq_regs_inc<SEQ_REGS_SOFTMAX>();
+    if (TWO) seq_regs_inc<SEQ_REGS_SOFTMAX>();
     const int t = warp >> 2, row = (int)threadIdx.x & 127, tt = row / a.fold, hh = row - tt * a.fold;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     bool ok = true;
-    uint32_t ns[2] = {0, 0}, nd[2] = {0, 0}, ring0 = 0, items = 0;      // blocks of a slot, results, ring places and items so far
-    w.begin(a, start_s, tokens, BN);
-    for (; w.left > 0; w.next(a, tokens, BN), ++items) {
-      const int n = w.b1 - w.b0, token = w.first + (TWO ? t * a.tokens : 0) + tt, head = w.head + hh;
-      const bool valid = tt < a.tokens && token < w.q.nq && hh < w.heads;
-      const int p = w.q.nk - w.q.nq + token;
-      SeqSeen seen = seq_seen(p, w.q.nk, w.q.prefix, a.causal, a.window);
+    uint32_t ns[2] = {0, 0}, ring0 = 0, items = 0;      // blocks of a tile of scores, ring places and items so far
+    for (; ok; ++items) {
+      if (!(ok = mbar_wait(c, q_full, items & 1u))) break;
+      __syncwarp();
+      const SeqItem w = item_s;
+      arrive_warp(q_empty, lane);
+      if (w.n == 0) break;
+      const int n = w.n, token = w.first + (TWO ? t * a.tokens : 0) + tt, head = w.head + hh;
+      const bool valid = tt < a.tokens && token < w.nq && hh < w.heads;
+      const int p = w.nk - w.nq + token;
+      SeqSeen seen = seq_seen(p, w.nk, w.prefix, a.causal, a.window);
       if (!valid) { seen.hi = INT_MAX / 2; seen.lo = 0; }              // (nobody stores it: nothing to mask)
       const float slope = EXTRA && a.slopes && valid ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
       float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll 1
-      for (int i = ALT ? t : 0; i < n; i += ALT ? 2 : 1) {
-        const int slot = TWO ? t : i & 1, c0 = seq_block(w.blocks, w.b0 + i) * BN;
+      for (int i = 0; i < n; ++i) {
+        const int slot = TWO ? t : i & 1, c0 = seq_block(SeqBlocks{w.na, w.lo, 0}, w.b0 + i) * BN;
         const uint32_t ts = tmem + lanes + (uint32_t)(BN * slot);
         if (ok) ok = mbar_wait(c, s_full + 8u * slot, ns[slot] & 1u);
         __syncwarp();
@@ -542,10 +623,10 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
           }
           sl2 = 1.0f;
         }
-        if (__any_sync(0xffffffffu, c0 + BN > seen.hi || (c0 < seen.lo && c0 + BN > w.q.prefix))) {
+        if (__any_sync(0xffffffffu, c0 + BN > seen.hi || (c0 < seen.lo && c0 + BN > w.prefix))) {
 #pragma unroll
           for (int k = 0; k < BN / 32; ++k) {
-            const uint32_t bits = seq_mask_word(seen.hi - c0, seen.lo - c0, w.q.prefix - c0, k);
+            const uint32_t bits = seq_mask_word(seen.hi - c0, seen.lo - c0, w.prefix - c0, k);
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (!(bits >> j & 1u)) sr[32 * k + j] = 0xFF800000u;
@@ -553,18 +634,17 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
         }
         float alpha;
         seq_softmax<BN>(sr, sl2, m_run, l_run, alpha);
-        const bool begun = ALT ? i >= 2 : i > 0;
-        if (begun && __any_sync(0xffffffffu, alpha != 1.0f)) {
-          if (WIDE && ok) ok = mbar_wait(c, o_done + 8u * ((i - 1) & 1), (ns[(i - 1) & 1] - 1) & 1u);
+        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
+          if (!TWO && ok) ok = mbar_wait(c, o_done + 8u * ((i - 1) & 1), (ns[(i - 1) & 1] - 1) & 1u);
           __syncwarp();
           tc_fence_after();
-          attn_rescale(tmem_o + lanes + (TWO || ALT ? 128u * t : 0u), hdc, alpha);
+          attn_rescale(tmem_o + lanes + (TWO ? 128u * t : 0u), hdc, alpha);
         }
         // Rows of V behind the last key (of other sequences, or what a page held before) may be anything, and 0 x inf is NaN: they become zeros.
-        if ((TWO ? t == 0 : true) && w.q.nk - c0 < BN) {
+        if ((TWO ? t == 0 : true) && w.nk - c0 < BN) {
           const uint32_t place = ring0 + (uint32_t)(TWO ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1)), stage = place % (uint32_t)NS;
           if (ok) ok = mbar_wait(c, full + 8u * stage, place / (uint32_t)NS & 1u);
-          const int from = max(w.q.nk - c0, 0);
+          const int from = max(w.nk - c0, 0);
           char* const v0 = smem_dyn + (ring + stage * stage_bytes - smem_u32(smem_dyn));
           for (int x = from * 8 + row; x < BN * 8; x += 128)
             for (int b = 0; b < nbox; ++b) *reinterpret_cast<uint4*>(v0 + b * (BN * 128) + x * 16) = make_uint4(0, 0, 0, 0);
@@ -579,87 +659,81 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
       }
       ring0 += 2u * (uint32_t)n;
       // ---------------- the row's result
-      const bool whole = w.b0 == 0 && w.b1 == w.blocks.n, used = ALT ? t < n : true;
-      if (used) {
-        const int slot = WIDE ? (n - 1) & 1 : t;
-        const uint32_t count = WIDE ? ns[slot] - 1 : nd[t]++;
+      const bool whole = w.part < 0;
+      {
+        const int slot = TWO ? t : (n - 1) & 1;
+        const uint32_t count = TWO ? items : ns[slot] - 1;
         if (ok) ok = mbar_wait(c, o_done + 8u * slot, count & 1u);
       }
       __syncwarp();
       tc_fence_after();
-      float f[2] = {1.0f, 0.f};               // weights of the two accumulators
-      bool both = false;
-      const float unit = EXTRA ? 1.0f : a.scale_log2;
-      m_run *= unit;                          // (log2 units from here on; -inf stays, scale > 0)
-      if (ALT) {
-        ml_s[items & 1][t][row] = make_float2(m_run, l_run);
-        tc_fence_before();
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        tc_fence_after();
-        both = n > 1;
-        const float2 x = ml_s[items & 1][0][row], y = both ? ml_s[items & 1][1][row] : make_float2(-INFINITY, 0.f);
-        m_run = fmaxf(x.x, y.x);
-        f[0] = x.x == -INFINITY ? (x.y == 0.f ? 0.f : x.y) : exp2_fast(x.x - m_run);
-        f[1] = y.x == -INFINITY ? (y.y == 0.f ? 0.f : y.y) : exp2_fast(y.x - m_run);
-        l_run = f[0] * x.y;
-        if (both) l_run = fmaf(f[1], y.y, l_run);
-      }
-      float bad = 0.f;
+      m_run *= EXTRA ? 1.0f : a.scale_log2;   // (log2 units from here on; -inf stays, scale > 0)
       const float inv = l_run == 0.f ? (seen.hi > 0 ? NAN : 0.f) : 1.0f / l_run;
-      unsigned short* const o = a.out + (int64_t)(w.q.q0 + token) * a.ld_out + head * a.hd;
       const int at = (TWO ? t * SEQ_ROWS : 0) + row;
-      float* const part = whole ? nullptr : seq_part(a, MODE, (int)blockIdx.x, w.b0 == 0 ? 1 : 0);
-      const int half = (hdc / 16 + 1) / 2 * 16, lo = ALT && t == 1 ? half : 0, hi = ALT && t == 0 ? half : hdc;
+      float* const part = whole ? nullptr : seq_part(a, MODE, (int)blockIdx.x, w.part);
+      // A row a lane and 32 columns at a time, stored 32 bytes an instruction.  (A warp a scheduler pays for instructions here, not for the memory: fragments
+      // over quads, with their exchanges, took 680 cycles for 512 values, sixteen columns at a time in 16-byte stores 400.)
+      unsigned short* const o = a.out + (int64_t)(w.q0 + token) * a.ld_out + head * a.hd;
+      const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ld_out * 2) | (uintptr_t)(a.hd * 2)) & 31) == 0;
+      const uint32_t to = tmem_o + lanes + (TWO ? 128u * t : 0u);
+      uint64_t sum = 0ull;                    // of all values: not finite if one is not
+      const uint64_t by = whole ? pack2(inv, inv) : pack2(1.0f, 1.0f);
 #pragma unroll 1
-      for (int col = lo; col < hi; col += 16) {
-        float v[16];
-        tmem_ld16(tmem_o + lanes + (TWO ? 128u * t : 0u) + (uint32_t)col, v);
-        if (ALT) {
-          float u[16];
-          if (both) tmem_ld16(tmem_o + lanes + 128u + (uint32_t)col, u);
+      for (int col = 0; col < hdc; col += 32) {
+        uint32_t v[32];
+        tmem_ld32_nowait(to + (uint32_t)col, v);
+        tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] = both ? fmaf(f[1], u[j], f[0] * v[j]) : f[0] * v[j];
-        }
-        if (whole) {
+        for (int k = 0; k < 32; k += 16) {
+          if (col + k >= hdc) break;
+          uint64_t y[8];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) { v[j] = inv == 0.f ? 0.f : v[j] * inv; bad = fmaf(v[j], 0.f, bad); }
-          if (valid) seq_put(o + col, v, a.hd - col);
-        } else {
+          for (int j = 0; j < 8; ++j) {
+            y[j] = mul2(pack2(__uint_as_float(v[k + 2 * j]), __uint_as_float(v[k + 2 * j + 1])), by);
+            sum = add2(sum, y[j]);
+          }
+          if (whole) {
+            uint32_t x[8];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) bad = fmaf(v[j], 0.f, bad);
-          if (valid) {
+            for (int j = 0; j < 8; ++j) { float e, f; unpack2(y[j], e, f); x[j] = pack_bf16(e, f); }
+            if (valid) {
+              if (wide) {
+                st_global_32(o + col + k, x);
+              } else {
+                *reinterpret_cast<uint4*>(o + col + k) = make_uint4(x[0], x[1], x[2], x[3]);
+                if (col + k + 8 < a.hd) *reinterpret_cast<uint4*>(o + col + k + 8) = make_uint4(x[4], x[5], x[6], x[7]);
+              }
+            }
+          } else if (valid) {
+            uint32_t x[16];
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(part + at * hdc + col + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < 8; ++j) { float e, f; unpack2(y[j], e, f); x[2 * j] = __float_as_uint(e); x[2 * j + 1] = __float_as_uint(f); }
+            st_global_32(part + at * hdc + col + k, x);
+            st_global_32(part + at * hdc + col + k + 8, x + 8);
           }
         }
       }
-      if (!whole && valid && (!ALT || t == 0)) seq_part_ml(a, MODE, part)[at] = make_float2(m_run, l_run);
+      float s0, s1;
+      unpack2(sum, s0, s1);
+      unsigned again = __ballot_sync(0xffffffffu, valid && !(fabsf(s0 + s1) <= 3e38f));      // rows that are not finite
+      if (!whole && valid) seq_part_ml(a, MODE, part)[at] = make_float2(m_run, l_run);
       tc_fence_before();
-      if (ALT) {
-        arrive_warp(o_free, lane);
-        if (both) arrive_warp(o_free + 8u, lane);
-      } else {
-        arrive_warp(o_free + 8u * (TWO ? t : 0), lane);
-      }
-      if (threadIdx.x == 0 && !whole && w.b0 == 0) {
-        const int64_t end = start_s.end - w.left + w.blocks.n;
-        *record = SeqRecord{seq_owner(start_s.total, start_s.n, end - 1) - (int)blockIdx.x + 1, w.s, w.unit, w.first};
-      }
+      arrive_warp(o_free + 8u * (TWO ? t : 0), lane);
       // Rows that are not finite, once more from the keys they see alone.
-      unsigned again = __ballot_sync(0xffffffffu, valid && seen.hi > 0 && bad != 0.f);
       while (again) {
         const int src = __ffs(again) - 1;
         again &= again - 1;
         const int r_token = __shfl_sync(0xffffffffu, token, src), r_head = __shfl_sync(0xffffffffu, head, src), r_at = __shfl_sync(0xffffffffu, at, src);
         const float r_m = __shfl_sync(0xffffffffu, m_run, src);
+        const bool r_sees = __shfl_sync(0xffffffffu, seen.hi, src) > 0;
         SeqRow r;
-        seq_row_alone(a, w.q, w.s, w.blocks, w.b0, w.b1, BN, r_token, r_head, w.kvh, r);
-        if (8 * lane < a.hd && 8 * lane >= lo && 8 * lane < hi) {      // (a warpgroup's own columns)
+        seq_row_alone(a, w, BN, r_token, r_head, r);
+        if (8 * lane < a.hd) {
           if (whole) {
-            const float i_ = r.l == 0.f ? NAN : 1.0f / r.l;
+            const float i_ = r.l != 0.f ? 1.0f / r.l : (r_sees ? NAN : 0.f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) r.acc[j] *= i_;
-            seq_put(a.out + (int64_t)(w.q.q0 + r_token) * a.ld_out + r_head * a.hd + 8 * lane, r.acc, 8);
+            seq_put(a.out + (int64_t)(w.q0 + r_token) * a.ld_out + r_head * a.hd + 8 * lane, r.acc, 8);
           } else {                             // (relative to the maximum that the row's sum, which is as it was, is relative to)
             const float as = r.m == -INFINITY ? 0.f : exp2_fast(r.m - r_m);
 #pragma unroll
@@ -673,7 +747,7 @@ __global__ void __launch_bounds__(MODE == SEQ_WIDE ? 256 : 384, 1) vla_op_sequen
     }
   }
   __syncthreads();
-  if (warp == SOFT + 1) tmem_dealloc(tmem, 512);
+  if (warp == SOFT + 1) tmem_dealloc(tmem, COLS);
   if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(&failed_s) != 0u) *err = (unsigned)DEV_ERR_WAIT_MBAR;
 }
 
@@ -684,10 +758,10 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
   op_let_next_start();
   const int share = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, hdc = seq_cols(a.hd);
   const int4 got = __ldcg(reinterpret_cast<const int4*>(a.scratch + SEQ_HEADER + share * SEQ_RECORD));
-  const int parts = got.x, s = got.y, unit = got.z, first = got.w;
+  const int parts = got.x, s = got.y, head0 = got.z, first = got.w;
   if (parts <= 0) return;
   const Seq q = seq_load(a, s);
-  const int kvh = unit / a.per_group, in = unit - kvh * a.per_group, head0 = kvh * a.group + in * a.fold, heads = min(a.fold, a.group - in * a.fold);
+  const int heads = min(a.fold, a.group - head0 % a.group);
   for (int r = (int)blockIdx.y * SEQ_JOIN_ROWS + warp; r < min((int)(blockIdx.y + 1) * SEQ_JOIN_ROWS, seq_item_rows(mode)); r += SEQ_JOIN_THREADS / 32) {
     const int tile = r / SEQ_ROWS, rr = r % SEQ_ROWS, tt = rr / a.fold, hh = rr - tt * a.fold, token = first + tile * a.tokens + tt;
     if (tt >= a.tokens || token >= q.nq || hh >= heads) continue;

@@ -7,17 +7,16 @@
 namespace vla {
 
 // What the kernels need to know of a device, looked up on the first call made with it current.
-struct SeqDevice { int ctas = 0; };
+struct SeqDevice { int sms = 0; };
 static bool seq_look_up(int dev, SeqDevice* d) {
-  if (cudaDeviceGetAttribute(&d->ctas, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return false;
-  d->ctas = seq_min(d->ctas, SEQ_MAX_CTAS);
+  if (cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return false;
   const auto ready = [](auto* kernel, int mode) {      // (what the warpgroups that raise their registers ask for has to be there)
     cudaFuncAttributes fa;
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, seq_smem(mode)) == cudaSuccess && cudaFuncGetAttributes(&fa, kernel) == cudaSuccess &&
-           (mode == SEQ_WIDE || fa.numRegs * 384 >= 128 * SEQ_REGS_SERVICE + 256 * SEQ_REGS_SOFTMAX);
+           (mode != SEQ_TWO || fa.numRegs * 384 >= 128 * SEQ_REGS_SERVICE + 256 * SEQ_REGS_SOFTMAX);
   };
   return ready(vla_op_sequences_kernel<SEQ_TWO, false>, SEQ_TWO) && ready(vla_op_sequences_kernel<SEQ_TWO, true>, SEQ_TWO) &&
-         ready(vla_op_sequences_kernel<SEQ_ALTERNATE, false>, SEQ_ALTERNATE) && ready(vla_op_sequences_kernel<SEQ_ALTERNATE, true>, SEQ_ALTERNATE) &&
+         ready(vla_op_sequences_kernel<SEQ_ONE, false>, SEQ_ONE) && ready(vla_op_sequences_kernel<SEQ_ONE, true>, SEQ_ONE) &&
          ready(vla_op_sequences_kernel<SEQ_WIDE, false>, SEQ_WIDE) && ready(vla_op_sequences_kernel<SEQ_WIDE, true>, SEQ_WIDE);
 }
 static bool seq_device(SeqDevice* d) {
@@ -47,18 +46,24 @@ static bool seq_rows_ok(const void* p, int64_t ld, int64_t least) { return p && 
 
 static int seq_run(SeqArgs& a, float scale, float cap, void* scratch, size_t scratch_bytes, cudaStream_t s) {
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || (int64_t)scratch_bytes < seq_scratch_bytes(a.hd)) return VLA_ERR_NOMEM;
-  SeqDevice dev;
-  if (!seq_device(&dev)) return VLA_ERR_CUDA;
   const SeqFold f = seq_fold(a.hq, a.hkv);
   a.group = f.group; a.fold = f.fold; a.per_group = f.per_group; a.tokens = f.tokens;
   a.scratch = static_cast<char*>(scratch);
   a.scale_log2 = scale * 1.44269504f;
   a.capped = cap > 0.f ? 1 : 0;
   a.cap_in = cap > 0.f ? scale / cap : 0.f; a.cap_log2 = cap * 1.44269504f;
-  const int mode = seq_mode(a.tq, a.seqs, f.fold, a.hd), bn = mode == SEQ_WIDE ? 64 : 128, nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
+  const int mode = seq_mode(a.tq, a.seqs, f.fold, a.hd), bn
+   = seq_bn(mode), nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
+  // (blocks of one head of all sequences, at most, counted in 32 bits)
+  const int64_t tokens = tiles * f.tokens, keys = a.offsets_k ? a.tk : (int64_t)a.max_pages * a.page_size;
+  if ((a.tq / tokens + a.seqs) * (keys / bn + 1 + seq_item_ticks(mode)) > INT32_MAX) return VLA_ERR_INVALID;
+  SeqDevice dev;
+  if (!seq_device(&dev)) return VLA_ERR_CUDA;
+  const int shares = seq_shares(mode, dev.sms);
   a.chunk = bn;
   if (!a.offsets_k)
     while (a.page_size % a.chunk) a.chunk /= 2;                       // (page sizes are multiples of 8)
+  if (!a.offsets_k) seq_divisor(a.page_size, &a.page_magic, &a.page_shift);
   const int stage = nbox * bn * 128;
   a.stages = seq_min((seq_smem(mode) - 1024 - tiles * nbox * SEQ_ROWS * 128) / stage, SEQ_MAX_STAGES);
   SeqMaps maps;
@@ -70,14 +75,14 @@ static int seq_run(SeqArgs& a, float scale, float cap, void* scratch, size_t scr
   if (!seq_encode(&maps.m[0], a.q, 3, qd, qs, qb) || !seq_encode(&maps.m[1], a.k, 4, kd, ks, kb) || !seq_encode(&maps.m[2], a.v, 4, kd, vs, kb)) return VLA_ERR_CUDA;
   const bool extra = a.capped || a.slopes;
   const auto kernel = mode == SEQ_TWO ? (extra ? vla_op_sequences_kernel<SEQ_TWO, true> : vla_op_sequences_kernel<SEQ_TWO, false>)
-                                      : (mode == SEQ_ALTERNATE ? (extra ? vla_op_sequences_kernel<SEQ_ALTERNATE, true> : vla_op_sequences_kernel<SEQ_ALTERNATE, false>)
+                                      : (mode == SEQ_ONE ? (extra ? vla_op_sequences_kernel<SEQ_ONE, true> : vla_op_sequences_kernel<SEQ_ONE, false>)
                                                                : (extra ? vla_op_sequences_kernel<SEQ_WIDE, true> : vla_op_sequences_kernel<SEQ_WIDE, false>));
-  const int rc = op_launch(kernel, dev.ctas, mode == SEQ_WIDE ? 256 : 384, seq_smem(mode), 1, s, a, maps, op_fault());
+  const int rc = op_launch(kernel, shares, seq_threads(mode), seq_smem(mode), 1, s, a, maps, op_fault());
   if (rc != VLA_OK) return rc;
   // (rows that an item can have: those of its tiles, and those of all tokens)
   const int64_t rows = (int64_t)a.tq * a.fold;
   const int most = rows < seq_item_rows(mode) ? (int)rows : seq_item_rows(mode);
-  return op_launch_2d(vla_op_sequences_join_kernel, dev.ctas, (most + SEQ_JOIN_ROWS - 1) / SEQ_JOIN_ROWS, SEQ_JOIN_THREADS, s, a, mode);
+  return op_launch_2d(vla_op_sequences_join_kernel, shares, (most + SEQ_JOIN_ROWS - 1) / SEQ_JOIN_ROWS, SEQ_JOIN_THREADS, s, a, mode);
 }
 
 }  // namespace vla

@@ -1,7 +1,7 @@
 // How attention over several sequences (op_sequences.cuh) is cut into work: plain arithmetic, compiled for the host in the CPU tests too.
 //
 // An item is one sequence x `tokens` of its new tokens x the query heads of a unit, over the key blocks that any of its rows sees.  Items follow one
-// another by sequence, unit and tokens; their blocks, numbered through, are dealt out in equal shares to the CTAs, whatever the lengths (which only
+// another by sequence, unit and tokens; their blocks are dealt out in equal shares to the CTAs, whatever the lengths (which only
 // the GPU knows).  A CTA's share may begin and end inside an item; the parts of such an item are put together afterwards.
 #pragma once
 #include <stdint.h>
@@ -15,7 +15,7 @@
 namespace vla {
 
 constexpr int SEQ_ROWS = 128;            // rows of a tile (MMA M): tokens x query heads that share a key head
-constexpr int SEQ_MAX_CTAS = 160;        // shares at most; the scratch memory is made for as many
+constexpr int SEQ_MAX_SHARES = 320;      // shares at most; the scratch memory is made for as many
 constexpr int SEQ_HEADER = 256;          // bytes in front of the scratch memory: error word
 constexpr int SEQ_RECORD = 32;           // bytes of a share's record
 
@@ -57,29 +57,56 @@ SEQ_HD SeqBlocks seq_blocks(int nq, int nk, int prefix, int first, int tokens, i
 }
 SEQ_HD int seq_block(const SeqBlocks& b, int i) { return i < b.na ? i : b.lo + (i - b.na); }
 
-// Shares: CTA c of n has the blocks [total c / n, total (c + 1) / n).  (total below 2^52, n at most SEQ_MAX_CTAS)
-SEQ_HD int64_t seq_share(int64_t total, int n, int c) { return (int64_t)((uint64_t)total * (uint64_t)c / (uint64_t)n); }
-// The CTA whose share holds block `at`.
-SEQ_HD int seq_owner(int64_t total, int n, int64_t at) {
-  int c = (int)((uint64_t)at * (uint64_t)n / (uint64_t)total);
-  while (c + 1 < n && seq_share(total, n, c + 1) <= at) ++c;
-  return c;
+// Shares are counted in ticks: one a block, and some for an item's beginning and end, in front of its first block (seq_item_ticks).  Share c of n has the
+// ticks [begin, end) below; of an item of which it has the ticks [t0, t1) it does the blocks [t0 - w, t1 - w), none below 0.
+struct SeqShares { int64_t total; int n; int64_t each, more; };      // the first `more` of them have one tick more than `each`
+SEQ_HD int64_t seq_div(int64_t a, int64_t b) { return ((uint64_t)(a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b; }      // (a fourth of the time)
+SEQ_HD SeqShares seq_shares_of(int64_t total, int most) {
+  SeqShares s;
+  s.total = total;
+  s.n = total < most ? (int)total : most;
+  s.each = s.n > 0 ? seq_div(total, s.n) : 0;
+  s.more = total - s.each * s.n;
+  return s;
+}
+SEQ_HD int64_t seq_share(const SeqShares& s, int c) { return s.each * c + (c < s.more ? c : s.more); }
+// The share that has tick `at`.
+SEQ_HD int seq_owner(const SeqShares& s, int64_t at) {
+  const int64_t bound = s.more * (s.each + 1);
+  return (int)(at < bound ? seq_div(at, s.each + 1) : s.more + seq_div(at - bound, s.each));
+}
+// Whether items stay whole: a share then has those whose first tick is its.  Where the longest is short beside a share, cutting gains less than
+// the parts' way through memory costs.
+SEQ_HD bool seq_whole(const SeqShares& s, int longest, int w) { return longest <= w + 2 || 4 * (int64_t)longest <= s.each; }
+
+// x / d = x * magic >> shift for 0 <= x < 2^31, d from 2 to 2^30: with 2^(l-1) < d <= 2^l, magic = 2^(31+l) / d rounded up is below 2^32 and too large by less
+// than 1, which makes x * magic / 2^(31+l) too large by less than 2^-l <= 1 / d.
+inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
+  uint32_t l = 1;
+  while (l < 30 && (1 << l) < d) ++l;
+  *magic = (uint32_t)((((uint64_t)1 << (31 + l)) + (uint64_t)d - 1) / (uint64_t)d);
+  *shift = 31 + l;
 }
 
-// Shapes of the kernel.  Two: two tiles of 128 rows that share their key blocks (long sequences).  Alternate: one tile, whose even and odd blocks go
-// to one warpgroup each (few rows).  Wide: one tile and one warpgroup, heads wider than 128.
-enum { SEQ_TWO = 0, SEQ_ALTERNATE = 1, SEQ_WIDE = 2 };
+// Shapes of the kernel.  Two: two tiles of 128 rows that share their blocks of 128 keys, an SM to a CTA (long sequences).  One: a tile, blocks of 64 keys, two
+// CTAs an SM.  Wide: the same for heads wider than 128, an SM to a CTA.
+enum { SEQ_TWO = 0, SEQ_ONE = 1, SEQ_WIDE = 2 };
 inline int seq_mode(int64_t tq, int seqs, int fold, int hd) {
   if (hd > 128) return SEQ_WIDE;
-  return tq * fold > (int64_t)seqs * 160 ? SEQ_TWO : SEQ_ALTERNATE;
+  return tq * fold > (int64_t)seqs * 160 ? SEQ_TWO : SEQ_ONE;
 }
+SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
+// What an item takes beside its blocks, in blocks: its first loads, the last block's chain, the result.
+SEQ_HD constexpr int seq_item_ticks(int mode) { return mode == SEQ_TWO ? 2 : 3; }
 SEQ_HD int seq_item_rows(int mode) { return mode == SEQ_TWO ? 2 * SEQ_ROWS : SEQ_ROWS; }
 SEQ_HD int seq_cols(int hd) { return (hd + 15) / 16 * 16; }      // columns of the result's accumulator
+inline int seq_shares(int mode, int sms) { return mode == SEQ_ONE ? seq_min(2 * sms, SEQ_MAX_SHARES) : seq_min(sms, SEQ_MAX_SHARES / 2); }
+// Shared memory for tiles and stages, with 1 KB to begin on a boundary; the rest of the SM's 227 KB (or half of it) is for what is declared in the kernels.
+SEQ_HD int seq_smem(int mode) { return (mode == SEQ_ONE ? 110 : 225) * 1024; }
 // Scratch: header, records, two parts of a share.  The same for every call with this head width.
-inline int64_t seq_part_floats(int mode, int hd) { return (int64_t)seq_item_rows(mode) * (seq_cols(hd) + 2); }
+SEQ_HD int64_t seq_part_floats(int mode, int hd) { return (int64_t)seq_item_rows(mode) * (seq_cols(hd) + 2); }
 inline int64_t seq_scratch_bytes(int hd) {
-  const int64_t part = hd > 128 ? seq_part_floats(SEQ_WIDE, hd) : seq_part_floats(SEQ_TWO, hd);
-  return SEQ_HEADER + (int64_t)SEQ_MAX_CTAS * SEQ_RECORD + 2 * SEQ_MAX_CTAS * part * 4;
+  return SEQ_HEADER + (int64_t)SEQ_MAX_SHARES * SEQ_RECORD + 2 * (int64_t)SEQ_MAX_SHARES * (hd > 128 ? seq_part_floats(SEQ_WIDE, hd) / 2 : seq_part_floats(SEQ_ONE, hd)) * 4;
 }
 
 }  // namespace vla
