@@ -348,29 +348,43 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
  * out overlaps no input.  scratch: DEVICE, 256-byte aligned, vla_op_attention_sequences_scratch_bytes(hd) or more; its first word is the call's
  * error word, its contents matter to nobody afterwards, and calls that share it must not overlap on the GPU (two captured graphs among them). */
 int vla_op_attention_sequences_scratch_bytes(int32_t hd, size_t* out_bytes);
-int vla_op_attention_packed(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* out,
-                            int64_t ld_out, const int32_t* offsets_q, const int32_t* offsets_k, int32_t seqs, int32_t tq,
-                            int32_t tk, int32_t hq, int32_t hkv, int32_t hd, float scale, int32_t causal, const int32_t* prefix,
-                            int32_t window, float cap, const float* slopes, void* scratch, size_t scratch_bytes, void* stream);
+typedef struct vla_attention_args {
+  const void *q, *k, *v;                     /* k, v: rows of the packed sequences, or k_cache and v_cache */
+  void* out;
+  int64_t ld_q, ld_k, ld_v, ld_out;          /* elements from row to row; ld_k and ld_v: of the cache's pages too */
+  int64_t page_k, page_v;                    /* paged: elements from page to page */
+  const int32_t *offsets_q, *offsets_k;      /* offsets_k: packed */
+  const int32_t *lengths, *pages;            /* paged */
+  const int32_t* prefix;                     /* or NULL */
+  const float* slopes;                       /* or NULL */
+  void* scratch;
+  size_t scratch_bytes;
+  int32_t seqs, tq, tk;                      /* tk: packed */
+  int32_t n_pages, page_size, max_pages;     /* paged */
+  int32_t hq, hkv, hd, causal, window;
+  float scale, cap;
+  int32_t reserved;                          /* 0 */
+} vla_attention_args;
+int vla_op_attention_packed(const vla_attention_args* args, void* stream);
 
 /* The same over a paged cache: sequence s has lengths[s] tokens, the new ones (its rows of q) last, and token j's key and value are row
- * j % page_size of page pages[s * max_pages + j / page_size] of k_cache and v_cache [n_pages, page_size, hkv*hd], rows row_* and pages page_* elements
+ * j % page_size of page pages[s * max_pages + j / page_size] of k_cache and v_cache [n_pages, page_size, hkv*hd], rows ld_* and pages page_* elements
  * apart.  page_size a multiple of 8; max_pages * page_size at most 2^30; lengths beyond that many tokens count as that many.  A page that does not
  * exist (an entry below 0 or from n_pages on) reads as zeros; entries behind a sequence's length are not looked at, nor rows behind it. */
-int vla_op_attention_paged(const void* q, int64_t ld_q, const void* k_cache, int64_t row_k, int64_t page_k, const void* v_cache,
-                           int64_t row_v, int64_t page_v, void* out, int64_t ld_out, const int32_t* pages, const int32_t* lengths,
-                           const int32_t* offsets, int32_t seqs, int32_t tq, int32_t n_pages, int32_t page_size,
-                           int32_t max_pages, int32_t hq, int32_t hkv, int32_t hd, float scale, int32_t causal,
-                           const int32_t* prefix, int32_t window, float cap, const float* slopes, void* scratch,
-                           size_t scratch_bytes, void* stream);
+int vla_op_attention_paged(const vla_attention_args* args, void* stream);
 
 /* New rows of such a cache: rows offsets[s] <= i < offsets[s + 1] of k and v [t, width] (width = hkv*hd, a multiple of 8) become tokens lengths[s] -
  * (offsets[s + 1] - i) of sequence s.  lengths count the new tokens.  A row whose token is below 0 or behind the table, or on a page that does
  * not exist, is not written; two rows for one place are the caller's mistake.  Any page_size.  Strides and alignment as above. */
-int vla_op_cache_store(const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* k_cache, int64_t row_k, int64_t page_k,
-                       void* v_cache, int64_t row_v, int64_t page_v, const int32_t* pages, const int32_t* lengths,
-                       const int32_t* offsets, int32_t seqs, int32_t t, int32_t n_pages, int32_t page_size, int32_t max_pages,
-                       int32_t width, void* stream);
+typedef struct vla_cache_store_args {
+  const void *k, *v;
+  void *k_cache, *v_cache;
+  int64_t ld_k, ld_v;                        /* elements from row to row of k and v */
+  int64_t row_k, page_k, row_v, page_v;      /* of the cache: from row to row, from page to page */
+  const int32_t *pages, *lengths, *offsets;
+  int32_t seqs, t, n_pages, page_size, max_pages, width;
+} vla_cache_store_args;
+int vla_op_cache_store(const vla_cache_store_args* args, void* stream);
 
 /* Every device-side wait of the operators is bounded (2 s by default, each of them: a call may take longer); a wait that
  * runs out makes the kernel set the call's error word and return, leaving garbage in the output.  vla_op_status waits for `stream` to drain and

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -119,11 +120,8 @@ def load_library() -> C.CDLL:
     lib.vla_op_qk_norm_rope.argtypes = ([C.c_void_p] * 2 + [C.c_int32] + [C.c_int64] * 2 + [C.c_void_p] * 2 + [C.c_int64] * 2 + [C.c_int32] * 4 +
                                         [C.c_void_p] * 2 + [C.c_float, C.c_void_p] + [C.c_int32] * 2 + [C.c_float, C.c_int32, C.c_void_p])
     lib.vla_op_attention_sequences_scratch_bytes.argtypes = [C.c_int32, P(C.c_size_t)]
-    lib.vla_op_attention_packed.argtypes = ([C.c_void_p, C.c_int64] * 4 + [C.c_void_p] * 2 + [C.c_int32] * 6 + [C.c_float, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_void_p] +
-                                            [C.c_void_p, C.c_size_t, C.c_void_p])
-    lib.vla_op_attention_paged.argtypes = ([C.c_void_p, C.c_int64] + [C.c_void_p, C.c_int64, C.c_int64] * 2 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 3 + [C.c_int32] * 8 +
-                                           [C.c_float, C.c_int32, C.c_void_p, C.c_int32, C.c_float, C.c_void_p] + [C.c_void_p, C.c_size_t, C.c_void_p])
-    lib.vla_op_cache_store.argtypes = [C.c_void_p, C.c_int64] * 2 + [C.c_void_p, C.c_int64, C.c_int64] * 2 + [C.c_void_p] * 3 + [C.c_int32] * 6 + [C.c_void_p]
+    for fn in (lib.vla_op_attention_packed, lib.vla_op_attention_paged, lib.vla_op_cache_store):
+        fn.argtypes = [C.c_char_p, C.c_void_p]                                  # (a struct's bytes: thirty arguments one by one took 3 us more)
     lib.vla_last_error.argtypes = [C.c_void_p]
     lib.vla_last_error.restype = C.c_char_p
     lib.vla_destroy.argtypes = [C.c_void_p]
@@ -703,43 +701,70 @@ def op_attention_sequences_scratch_bytes(hd) -> int:
     return out.value
 
 
-def _rows(name, what, x, rows, width):
+def _offsets(name, offsets, others):
+    """The number of sequences, with the devices of all tensors looked at."""
+    import torch
+    seqs = offsets.shape[0] - 1 if offsets.dim() == 1 else 0
+    if seqs < 1 or offsets.dtype != torch.int32 or not offsets.is_contiguous() or _elsewhere(offsets, *others):
+        _refuse(name, "offsets is contiguous int32 [seqs + 1], on the current CUDA device like all else")
+    return seqs
+
+
+def _row_step(name, what, x, rows, width):
     """Elements from one row of x [rows, width] (bf16) to the next."""
     import torch
-    if x.dtype != torch.bfloat16 or x.shape != (rows, width) or x.stride(1) != 1:
-        _refuse(name, f"{what}, rows in one piece")
-    return x.stride(0) if rows > 1 else width                       # (the stride of one row says nothing)
+    if x.dtype != torch.bfloat16 or x.shape != (rows, width):
+        _refuse(name, what)
+    ld, one = x.stride()
+    if one != 1:
+        _refuse(name, what + ", rows in one piece")
+    return ld if rows > 1 else width                                # (the stride of one row says nothing)
 
 
-def _counts32(name, what, x, n):
+def _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream):
+    """What the two attentions below have in common: (tq, ld_q, out, ld_out, scratch, its bytes, pointers of prefix and slopes, scale)."""
     import torch
-    if x is not None and (x.shape != (n,) or x.dtype != torch.int32 or not x.is_contiguous()):
-        _refuse(name, f"{what} is contiguous int32, [{n}]")
-    return None if x is None else x.data_ptr()
-
-
-def _sequences(name, q, offsets, hq, hkv, hd, prefix, slopes, scale, out, scratch, stream, others):
-    """What the two attentions below have in common: (tq, seqs, ld_q, out, ld_out, scale, scratch and the pointers of prefix and slopes)."""
-    import torch
-    if q.dim() != 2 or offsets.dim() != 1 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8 or (hq * hd) >> 31 or _elsewhere(q, offsets, prefix, slopes, out, scratch, *others):
-        _refuse(name, "q is a matrix on the current CUDA device, like all else; hd a multiple of 8, at most 256")
-    tq, seqs = q.shape[0], offsets.shape[0] - 1
-    if tq < 1 or tq >> 31 or seqs < 1:
-        _refuse(name, "at least one row and one sequence, below 2^31 rows")
-    ld_q = _rows(name, "q is bf16 [tq, hq*hd]", q, tq, hq * hd)
-    _counts32(name, "offsets", offsets, seqs + 1)
-    if slopes is not None and (slopes.shape != (hq,) or slopes.dtype != torch.float32 or not slopes.is_contiguous()):
-        _refuse(name, "slopes is contiguous fp32, [hq]")
+    if q.dim() != 2 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8:
+        _refuse(name, "q is a matrix; hd a multiple of 8, at most 256")
+    tq, width = q.shape[0], hq * hd
+    if tq < 1 or (tq | width | hkv * hd) >> 31 or window >> 31:
+        _refuse(name, "at least one row, below 2^31 of them, window a number from 0 to 2^31 - 1")
+    ld_q = _row_step(name, "q is bf16 [tq, hq*hd]", q, tq, width)
+    p_prefix = p_slopes = 0
+    if prefix is not None:
+        if prefix.shape != (seqs,) or prefix.dtype != torch.int32 or not prefix.is_contiguous():
+            _refuse(name, "prefix is contiguous int32, [seqs]")
+        p_prefix = prefix.data_ptr()
+    if slopes is not None:
+        if slopes.shape != (hq,) or slopes.dtype != torch.float32 or not slopes.is_contiguous():
+            _refuse(name, "slopes is contiguous fp32, [hq]")
+        p_slopes = slopes.data_ptr()
     if out is None:
-        out, ld_out = _new(stream, (tq, hq * hd), torch.bfloat16, q), hq * hd
+        out, ld_out = _new(stream, (tq, width), torch.bfloat16, q), width
     else:
-        ld_out = _rows(name, "out is bf16 [tq, hq*hd]", out, tq, hq * hd)
-    if scratch is None:
-        scratch = _new(stream, (op_attention_sequences_scratch_bytes(hd),), torch.uint8, q)     # (goes back to its stream's memory when the call returns)
+        ld_out = _row_step(name, "out is bf16 [tq, hq*hd]", out, tq, width)
+    if scratch is None:                                             # (goes back to its stream's memory when the call returns)
+        scratch, size = _scratch(stream, hd, q)
     elif scratch.dtype != torch.uint8 or not scratch.is_contiguous():
         _refuse(name, "scratch is contiguous uint8")
-    return (tq, seqs, ld_q, out, ld_out, hd ** -0.5 if scale is None else scale, scratch, _counts32(name, "prefix", prefix, seqs),
-            None if slopes is None else slopes.data_ptr())
+    else:
+        size = scratch.numel()
+    return tq, ld_q, out, ld_out, scratch, size, p_prefix, p_slopes, hd ** -0.5 if scale is None else scale
+
+
+_scratch_sizes = {}
+
+
+def _scratch(stream, hd, like):
+    import torch
+    size = _scratch_sizes.get(hd)
+    if size is None:
+        size = _scratch_sizes[hd] = op_attention_sequences_scratch_bytes(hd)
+    return _new(stream, (size,), torch.uint8, like), size
+
+
+_ATTENTION_ARGS = struct.Struct("=18Q11i2fi")                        # vla_attention_args
+_CACHE_STORE_ARGS = struct.Struct("=13Q6i")                          # vla_cache_store_args
 
 
 def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=False, prefix=None, window=0, cap=0.0, slopes=None, scale=None, out=None,
@@ -750,45 +775,46 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
     cap tanh(s / cap); slopes fp32 [hq]: a score loses slopes[h] times the distance.  scale None: 1 / sqrt(hd).  Returns out [tq, hq*hd] bf16; rows that no
     sequence has are left as they were in ``out`` (without one: undefined), rows that see no key are zeros (see vla_op_attention_packed)."""
     name = "op_attention_packed"
-    tq, seqs, ld_q, out, ld_out, scale, scratch, p_prefix, p_slopes = _sequences(name, q, offsets, hq, hkv, hd, prefix, slopes, scale, out, scratch, stream, (k, v, offsets_k))
+    seqs = _offsets(name, offsets, (q, k, v, offsets_k, prefix, slopes, out, scratch))
+    tq, ld_q, out, ld_out, scratch, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     tk = k.shape[0]
     if offsets_k is None:
         offsets_k = offsets
         if tk != tq:
             _refuse(name, "without offsets_k, k and v have q's rows")
-    if k.dim() != 2 or v.dim() != 2 or tk < 1 or tk >> 31 or (hkv * hd) >> 31:
-        _refuse(name, "k and v are matrices of at least one row, below 2^31 of them")
-    ld_k, ld_v = _rows(name, "k is bf16 [tk, hkv*hd]", k, tk, hkv * hd), _rows(name, "v is bf16 [tk, hkv*hd]", v, tk, hkv * hd)
-    rc = (_lib or load_library()).vla_op_attention_packed(
-        q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, out.data_ptr(), ld_out, offsets.data_ptr(), _counts32(name, "offsets_k", offsets_k, seqs + 1), seqs, tq, tk,
-        hq, hkv, hd, scale, int(causal), p_prefix, _c32(name, window), cap, p_slopes, scratch.data_ptr(), scratch.numel(), _stream_ptr(stream))
+    elif offsets_k.shape != (seqs + 1,) or offsets_k.dtype != offsets.dtype or not offsets_k.is_contiguous():
+        _refuse(name, "offsets_k is contiguous int32, [seqs + 1]")
+    if tk < 1 or tk >> 31:
+        _refuse(name, "k and v have at least one row, below 2^31 of them")
+    ld_k, ld_v = _row_step(name, "k is bf16 [tk, hkv*hd]", k, tk, hkv * hd), _row_step(name, "v is bf16 [tk, hkv*hd]", v, tk, hkv * hd)
+    args = _ATTENTION_ARGS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, 0, 0, offsets.data_ptr(), offsets_k.data_ptr(), 0, 0,
+                                p_prefix, p_slopes, scratch.data_ptr(), size, seqs, tq, tk, 0, 0, 0, hq, hkv, hd, 1 if causal else 0, window, scale, cap, 0)
+    rc = (_lib or load_library()).vla_op_attention_packed(args, _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_attention_packed failed")
     return out
 
 
-def _c32(name, x):
-    if x >> 31:
-        _refuse(name, "window is a number from 0 to 2^31 - 1")
-    return x
-
-
 def _cache(name, k_cache, v_cache, pages, lengths, seqs, width):
     """Sizes and strides of a cache's two tensors: (n_pages, page_size, max_pages, row_k, page_k, row_v, page_v)."""
     import torch
-    if k_cache.dim() != 3 or v_cache.shape != k_cache.shape or k_cache.shape[2] != width or k_cache.dtype != torch.bfloat16 or v_cache.dtype != torch.bfloat16:
+    shape, bf16, i32 = k_cache.shape, torch.bfloat16, torch.int32
+    if len(shape) != 3 or shape[2] != width or v_cache.shape != shape or k_cache.dtype != bf16 or v_cache.dtype != bf16:
         _refuse(name, "k_cache and v_cache are bf16 [n_pages, page_size, hkv*hd]")
-    n, size = k_cache.shape[:2]
-    if k_cache.stride(2) != 1 or v_cache.stride(2) != 1 or n < 1 or size < 1 or n >> 31 or size >> 31:
+    n, size, _ = shape
+    (page_k, row_k, one_k), (page_v, row_v, one_v) = k_cache.stride(), v_cache.stride()
+    if one_k != 1 or one_v != 1 or n < 1 or size < 1 or (n | size) >> 31:
         _refuse(name, "the caches' rows are in one piece, at least one page of at least one row, below 2^31 of either")
-    if pages.dim() != 2 or pages.shape[0] != seqs or pages.shape[1] < 1 or pages.dtype != torch.int32 or not pages.is_contiguous() or pages.shape[1] >> 31:
-        _refuse(name, "pages is contiguous int32, [seqs, max_pages]")
-    _counts32(name, "lengths", lengths, seqs)
-    at = []
-    for x in (k_cache, v_cache):                                    # (the stride of a single row or page says nothing)
-        row = x.stride(1) if size > 1 else width
-        at += [row, x.stride(0) if n > 1 else size * row]
-    return n, size, pages.shape[1], at[0], at[1], at[2], at[3]
+    if size == 1:                                                   # (the stride of a single row or page says nothing)
+        row_k = row_v = width
+    if n == 1:
+        page_k, page_v = size * row_k, size * row_v
+    if pages.dim() != 2 or pages.dtype != i32 or not pages.is_contiguous() or lengths.shape != (seqs,) or lengths.dtype != i32 or not lengths.is_contiguous():
+        _refuse(name, "pages [seqs, max_pages] and lengths [seqs] are contiguous int32")
+    rows, most = pages.shape
+    if rows != seqs or most < 1 or most >> 31:
+        _refuse(name, "pages has a row of at least one entry for each sequence")
+    return n, size, most, row_k, page_k, row_v, page_v
 
 
 def op_attention_paged(q, k_cache, v_cache, pages, lengths, offsets, hq, hkv, hd, causal=True, prefix=None, window=0, cap=0.0, slopes=None, scale=None, out=None,
@@ -798,12 +824,13 @@ def op_attention_paged(q, k_cache, v_cache, pages, lengths, offsets, hq, hkv, hd
     page_size a multiple of 8; pages int32 [seqs, max_pages], lengths int32 [seqs], offsets int32 [seqs + 1], all on the GPU; entries of ``pages`` behind a
     sequence's length are not looked at (see vla_op_attention_paged)."""
     name = "op_attention_paged"
-    tq, seqs, ld_q, out, ld_out, scale, scratch, p_prefix, p_slopes = _sequences(name, q, offsets, hq, hkv, hd, prefix, slopes, scale, out, scratch, stream,
-                                                                                  (k_cache, v_cache, pages, lengths))
-    n, size, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, hkv * hd)
-    rc = (_lib or load_library()).vla_op_attention_paged(
-        q.data_ptr(), ld_q, k_cache.data_ptr(), row_k, page_k, v_cache.data_ptr(), row_v, page_v, out.data_ptr(), ld_out, pages.data_ptr(), lengths.data_ptr(), offsets.data_ptr(),
-        seqs, tq, n, size, most, hq, hkv, hd, scale, int(causal), p_prefix, _c32(name, window), cap, p_slopes, scratch.data_ptr(), scratch.numel(), _stream_ptr(stream))
+    seqs = _offsets(name, offsets, (q, k_cache, v_cache, pages, lengths, prefix, slopes, out, scratch))
+    tq, ld_q, out, ld_out, scratch, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
+    n, page, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, hkv * hd)
+    args = _ATTENTION_ARGS.pack(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), ld_q, row_k, row_v, ld_out, page_k, page_v, offsets.data_ptr(), 0,
+                                lengths.data_ptr(), pages.data_ptr(), p_prefix, p_slopes, scratch.data_ptr(), size, seqs, tq, 0, n, page, most, hq, hkv, hd, 1 if causal else 0,
+                                window, scale, cap, 0)
+    rc = (_lib or load_library()).vla_op_attention_paged(args, _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_attention_paged failed")
     return out
@@ -814,16 +841,17 @@ def op_cache_store(k, v, k_cache, v_cache, pages, lengths, offsets, stream=None)
     apart) become the last ones of lengths[s] tokens.  Rows whose place is in front of the first token, behind the table or on a page that does not exist
     are left out (see vla_op_cache_store)."""
     name = "op_cache_store"
-    if k.dim() != 2 or v.dim() != 2 or offsets.dim() != 1 or _elsewhere(k, v, k_cache, v_cache, pages, lengths, offsets):
-        _refuse(name, "k and v are matrices on the current CUDA device, like all else")
-    (t, width), seqs = k.shape, offsets.shape[0] - 1
-    if t < 1 or (t | width) >> 31 or seqs < 1:
-        _refuse(name, "at least one row and one sequence, below 2^31 rows")
-    ld_k, ld_v = _rows(name, "k is bf16 [t, hkv*hd]", k, t, width), _rows(name, "v is bf16 [t, hkv*hd]", v, t, width)
-    _counts32(name, "offsets", offsets, seqs + 1)
+    seqs = _offsets(name, offsets, (k, v, k_cache, v_cache, pages, lengths))
+    if k.dim() != 2:
+        _refuse(name, "k and v are matrices")
+    t, width = k.shape
+    if t < 1 or (t | width) >> 31:
+        _refuse(name, "at least one row, below 2^31 of them")
+    ld_k, ld_v = _row_step(name, "k is bf16 [t, hkv*hd]", k, t, width), _row_step(name, "v is bf16 [t, hkv*hd]", v, t, width)
     n, size, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, width)
-    rc = (_lib or load_library()).vla_op_cache_store(k.data_ptr(), ld_k, v.data_ptr(), ld_v, k_cache.data_ptr(), row_k, page_k, v_cache.data_ptr(), row_v, page_v, pages.data_ptr(),
-                                                     lengths.data_ptr(), offsets.data_ptr(), seqs, t, n, size, most, width, _stream_ptr(stream))
+    args = _CACHE_STORE_ARGS.pack(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), ld_k, ld_v, row_k, page_k, row_v, page_v, pages.data_ptr(), lengths.data_ptr(),
+                                  offsets.data_ptr(), seqs, t, n, size, most, width)
+    rc = (_lib or load_library()).vla_op_cache_store(args, _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_cache_store failed")
 

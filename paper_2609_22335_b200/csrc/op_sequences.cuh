@@ -41,7 +41,8 @@ struct SeqArgs {
 struct SeqMaps {
   alignas(64) CUtensorMap m[3];                // Q {hd, hq, tq}; K, V {hd, hkv, rows of a page, pages}
 };
-struct SeqRecord { int parts, s, head, first; };      // of an item that begins in this share and ends in a later one; parts = 0: none
+// Of an item that begins in this share and ends in a later one: shares that have parts of it (0: there is none), and what its rows are.
+struct __align__(16) SeqRecord { int parts, first, head, heads, q0, nq, nk, prefix; };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, uint32_t bar, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -110,9 +111,9 @@ __device__ __forceinline__ int seq_ticks32(const SeqArgs& a, const Seq& x, int f
 // The share's first item (of unit, sequence s, tokens from `first` on), its first tick of it, and where the share ends.
 struct SeqStart { SeqShares shares; int64_t left; int s, unit, first, tick; bool whole; Seq q; };
 // One warp: where share `c` begins.  A sequence a lane; those of several items are summed by all lanes together, one after another.
-__device__ __forceinline__ SeqStart seq_start(const SeqArgs& a, int tokens, int bn, int w, int most, int c, int lane) {
+__device__ __forceinline__ SeqStart seq_start(const SeqArgs& a, int tokens, int bn, int w, int join, int most, int c, int lane) {
   const int units = a.hkv * a.per_group;
-  int all = 0, longest = 0, own = 0;           // ticks of one unit; the most of an item; of this lane's sequence
+  int all = 0, items = 0, longest = 0, own = 0;      // ticks and items of one unit; the most ticks of an item; ticks of this lane's sequence
   Seq q = {0, 0, 0, 0, 0};
   auto count = [&](int s0) {
     q = {0, 0, 0, 0, 0};
@@ -145,13 +146,14 @@ __device__ __forceinline__ SeqStart seq_start(const SeqArgs& a, int tokens, int 
   for (int s0 = 0; s0 < a.seqs; s0 += 32) {
     count(s0);
     all += __reduce_add_sync(0xffffffffu, own);
+    items += __reduce_add_sync(0xffffffffu, (q.nq + tokens - 1) / tokens);
   }
   longest = __reduce_max_sync(0xffffffffu, longest);
   SeqStart r;
   r.shares = seq_shares_of((int64_t)all * units, most);
   r.left = 0;
   if (c >= r.shares.n) return r;
-  r.whole = seq_whole(r.shares, longest, w);
+  r.whole = seq_whole(r.shares, (int64_t)items * units, longest, join);
   const int64_t begin = seq_share(r.shares, c);
   r.left = seq_share(r.shares, c + 1) - begin;
   r.unit = (int)seq_div(begin, all);
@@ -340,11 +342,10 @@ __device__ __forceinline__ void seq_put(unsigned short* o, const float* v, int c
   *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
   if (cols >= 16) *reinterpret_cast<uint4*>(o + 8) = make_uint4(pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]), pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
 }
+// Part `which` (1: of the item that the share begins and does not end, 0: of the one that began before) of a share: rows of seq_row_floats, the row's
+// maximum (log2 units) and sum behind its columns.
 __device__ __forceinline__ float* seq_part(const SeqArgs& a, int mode, int share, int which) {
   return reinterpret_cast<float*>(a.scratch + SEQ_HEADER + SEQ_MAX_SHARES * SEQ_RECORD) + (2 * share + which) * seq_part_floats(mode, a.hd);
-}
-__device__ __forceinline__ float2* seq_part_ml(const SeqArgs& a, int mode, float* part) {
-  return reinterpret_cast<float2*>(part + (int64_t)seq_item_rows(mode) * seq_cols(a.hd));
 }
 
 constexpr int seq_threads(int mode) { return mode == SEQ_TWO ? 384 : 192; }
@@ -398,7 +399,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       // ---------------- loads.  A block of keys is one box of a head's columns, or a box for each piece of a page, issued side by side by the lanes.
       uint32_t s = 0, ph = 1u, items = 0;
       const int chunks = BN / a.chunk;
-      const SeqStart st = seq_start(a, tokens, BN, W, (int)gridDim.x, (int)blockIdx.x, lane);
+      const SeqStart st = seq_start(a, tokens, BN, W, seq_join_ticks(MODE), (int)gridDim.x, (int)blockIdx.x, lane);
       SeqWalk walk = {st.left, st.s, st.unit, st.first, st.tick, st.q};
       if (st.whole && st.tick > 0) walk.take(a, true, tokens, BN, W);      // (that item is the share's before)
       for (;; ++items) {
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
                   tma_load_3d(Qs + (uint32_t)t * tile_bytes + (uint32_t)b * (SEQ_ROWS * 128), &maps.m[0], q_full, b * 64, w.head, w.q0 + w.first + t * a.tokens);
               if (w.part == 1) {               // (the item's last tick lies behind the share's end by as many as its blocks that are left)
                 const int64_t last = seq_share(st.shares, (int)blockIdx.x + 1) + w.blocks - n - 1;
-                *record = SeqRecord{seq_owner(st.shares, last) - (int)blockIdx.x + 1, w.s, w.head, w.first};
+                *record = SeqRecord{seq_owner(st.shares, last) - (int)blockIdx.x + 1, w.first, w.head, w.heads, w.q0, w.nq, w.nk, w.prefix};
               }
             }
           }
@@ -671,6 +672,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       const float inv = l_run == 0.f ? (seen.hi > 0 ? NAN : 0.f) : 1.0f / l_run;
       const int at = (TWO ? t * SEQ_ROWS : 0) + row;
       float* const part = whole ? nullptr : seq_part(a, MODE, (int)blockIdx.x, w.part);
+      float* const part_row = part + at * seq_row_floats(a.hd);
       // A row a lane and 32 columns at a time, stored 32 bytes an instruction.  (A warp a scheduler pays for instructions here, not for the memory: fragments
       // over quads, with their exchanges, took 680 cycles for 512 values, sixteen columns at a time in 16-byte stores 400.)
       unsigned short* const o = a.out + (int64_t)(w.q0 + token) * a.ld_out + head * a.hd;
@@ -708,15 +710,15 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
             uint32_t x[16];
 #pragma unroll
             for (int j = 0; j < 8; ++j) { float e, f; unpack2(y[j], e, f); x[2 * j] = __float_as_uint(e); x[2 * j + 1] = __float_as_uint(f); }
-            st_global_32(part + at * hdc + col + k, x);
-            st_global_32(part + at * hdc + col + k + 8, x + 8);
+            st_global_32(part_row + col + k, x);
+            st_global_32(part_row + col + k + 8, x + 8);
           }
         }
       }
       float s0, s1;
       unpack2(sum, s0, s1);
       unsigned again = __ballot_sync(0xffffffffu, valid && !(fabsf(s0 + s1) <= 3e38f));      // rows that are not finite
-      if (!whole && valid) seq_part_ml(a, MODE, part)[at] = make_float2(m_run, l_run);
+      if (!whole && valid) *reinterpret_cast<float2*>(part_row + hdc) = make_float2(m_run, l_run);
       tc_fence_before();
       arrive_warp(o_free + 8u * (TWO ? t : 0), lane);
       // Rows that are not finite, once more from the keys they see alone.
@@ -738,7 +740,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
             const float as = r.m == -INFINITY ? 0.f : exp2_fast(r.m - r_m);
 #pragma unroll
             for (int j = 0; j < 8; ++j) r.acc[j] *= as;
-            float4* const x = reinterpret_cast<float4*>(part + r_at * hdc + 8 * lane);
+            float4* const x = reinterpret_cast<float4*>(part + r_at * seq_row_floats(a.hd) + 8 * lane);
             x[0] = make_float4(r.acc[0], r.acc[1], r.acc[2], r.acc[3]);
             x[1] = make_float4(r.acc[4], r.acc[5], r.acc[6], r.acc[7]);
           }
@@ -751,46 +753,95 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(&failed_s) != 0u) *err = (unsigned)DEV_ERR_WAIT_MBAR;
 }
 
-// Parts of the items that were cut, put together: a block for each share that begins such an item and for 32 of its rows, a warp a row.
-constexpr int SEQ_JOIN_THREADS = 256, SEQ_JOIN_ROWS = 32;
+// Parts of the items that were cut, put together: a warp a row, or four where there are many parts, each with every fourth part.  Bound by the way to the L2
+// cache and back (0.4 us) and by fetching the instructions, so four parts' columns, four a lane, with their maxima and sums are asked for at once and the
+// code is short.
+constexpr int SEQ_JOIN_THREADS = 128, SEQ_JOIN_WARPS = SEQ_JOIN_THREADS / 32;
+template <bool WIDE>
 __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel(const __grid_constant__ SeqArgs a, int mode) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   op_let_next_start();
-  const int share = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, hdc = seq_cols(a.hd);
-  const int4 got = __ldcg(reinterpret_cast<const int4*>(a.scratch + SEQ_HEADER + share * SEQ_RECORD));
-  const int parts = got.x, s = got.y, head0 = got.z, first = got.w;
+  const int share = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, hdc = seq_cols(a.hd), stride = seq_row_floats(a.hd);
+  const int4* const rec = reinterpret_cast<const int4*>(a.scratch + SEQ_HEADER + share * SEQ_RECORD);
+  const int4 x = __ldcg(rec), y = __ldcg(rec + 1);
+  const int parts = x.x, first = x.y, head0 = x.z, heads = x.w, q0 = y.x, nq = y.y, nk = y.z, prefix = y.w;
   if (parts <= 0) return;
-  const Seq q = seq_load(a, s);
-  const int heads = min(a.fold, a.group - head0 % a.group);
-  for (int r = (int)blockIdx.y * SEQ_JOIN_ROWS + warp; r < min((int)(blockIdx.y + 1) * SEQ_JOIN_ROWS, seq_item_rows(mode)); r += SEQ_JOIN_THREADS / 32) {
+  constexpr int AHEAD = 4, HALVES = WIDE ? 2 : 1, COLS = 4 * HALVES;
+  __shared__ float met_s[SEQ_JOIN_WARPS][COLS + 2][32];
+  const int ways = parts > AHEAD ? SEQ_JOIN_WARPS : 1, mine = ways == 1 ? 0 : warp, rows = SEQ_JOIN_WARPS / ways;      // warps of a row; rows at once
+  const int64_t step = 2 * seq_part_floats(mode, a.hd);
+  const float* const base = seq_part(a, mode, share, 0);
+  const int left = nq - first, last = left > a.tokens ? SEQ_ROWS + min(left - a.tokens, a.tokens) * a.fold : left * a.fold;      // (of one tile: all of it)
+#pragma unroll 1
+  for (int r0 = (int)blockIdx.y * rows; r0 < min(last, seq_item_rows(mode)); r0 += (int)gridDim.y * rows) {
+    const int r = r0 + (ways == 1 ? warp : 0);
     const int tile = r / SEQ_ROWS, rr = r % SEQ_ROWS, tt = rr / a.fold, hh = rr - tt * a.fold, token = first + tile * a.tokens + tt;
-    if (tt >= a.tokens || token >= q.nq || hh >= heads) continue;
-    float m = -INFINITY;
-    for (int k = lane; k < parts; k += 32) m = fmaxf(m, __ldcg(seq_part_ml(a, mode, seq_part(a, mode, share + k, k == 0 ? 1 : 0)) + r).x);
-    m = warp_max(m);
-    float acc[8], l = 0.f;
+    if (tt >= a.tokens || token >= nq || hh >= heads) continue;      // (the same for all warps of a row)
+    float m = -INFINITY, l = 0.f, acc[COLS];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-#pragma unroll 4
-    for (int k = 0; k < parts; ++k) {
-      float* const part = seq_part(a, mode, share + k, k == 0 ? 1 : 0);
-      const float2 ml = __ldcg(seq_part_ml(a, mode, part) + r);
-      const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : ml.y) : exp2_fast(ml.x - m);
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-      if (8 * lane < hdc) {
-        x = __ldcg(reinterpret_cast<const float4*>(part + r * hdc + 8 * lane));
-        y = __ldcg(reinterpret_cast<const float4*>(part + r * hdc + 8 * lane + 4));
+    for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
+    const float* const at = base + (int64_t)r * stride;
+#pragma unroll 1
+    for (int k = mine; k < parts; k += AHEAD * ways) {
+      float2 ml[AHEAD];
+      float4 o[AHEAD][HALVES];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int part = k + u * ways;
+        const float* const p = at + (part == 0 ? step / 2 : part * step);
+        ml[u] = make_float2(-INFINITY, 0.f);
+        if (part < parts) ml[u] = __ldcg(reinterpret_cast<const float2*>(p + hdc));
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+          o[u][h] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (part < parts && 4 * lane + 128 * h < hdc) o[u][h] = __ldcg(reinterpret_cast<const float4*>(p + 4 * lane + 128 * h));
+        }
       }
-      if (f != 0.f) {
-        l = fmaf(f, ml.y, l);
-        acc[0] = fmaf(f, x.x, acc[0]); acc[1] = fmaf(f, x.y, acc[1]); acc[2] = fmaf(f, x.z, acc[2]); acc[3] = fmaf(f, x.w, acc[3]);
-        acc[4] = fmaf(f, y.x, acc[4]); acc[5] = fmaf(f, y.y, acc[5]); acc[6] = fmaf(f, y.z, acc[6]); acc[7] = fmaf(f, y.w, acc[7]);
+      const float top = fmaxf(m, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x))), keep = m == -INFINITY ? 0.f : exp2_fast(m - top);
+      l *= keep;
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) acc[j] *= keep;
+      m = top;
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const float f = ml[u].x == -INFINITY ? (ml[u].y == 0.f ? 0.f : ml[u].y) : exp2_fast(ml[u].x - top);      // (no maximum: no keys, or scores that are all NaN)
+        if (f == 0.f) continue;                // (a part without keys of this row: whatever lies there)
+        l = fmaf(f, ml[u].y, l);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+          acc[4 * h] = fmaf(f, o[u][h].x, acc[4 * h]); acc[4 * h + 1] = fmaf(f, o[u][h].y, acc[4 * h + 1]);
+          acc[4 * h + 2] = fmaf(f, o[u][h].z, acc[4 * h + 2]); acc[4 * h + 3] = fmaf(f, o[u][h].w, acc[4 * h + 3]);
+        }
       }
     }
-    const float inv = l == 0.f ? (seq_seen(q.nk - q.nq + token, q.nk, q.prefix, a.causal, a.window).hi > 0 ? NAN : 0.f) : 1.0f / l;
+    if (ways > 1) {                            // the four warps' shares meet, in their order
+      __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] *= inv;
-    if (8 * lane < a.hd) seq_put(a.out + (int64_t)(q.q0 + token) * a.ld_out + (head0 + hh) * a.hd + 8 * lane, acc, 8);
+      for (int j = 0; j < COLS; ++j) met_s[warp][j][lane] = acc[j];
+      met_s[warp][COLS][lane] = m; met_s[warp][COLS + 1][lane] = l;
+      __syncthreads();
+      if (warp != 0) continue;
+      float top = m;
+#pragma unroll
+      for (int i = 1; i < SEQ_JOIN_WARPS; ++i) top = fmaxf(top, met_s[i][COLS][lane]);
+      l = 0.f;
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < SEQ_JOIN_WARPS; ++i) {
+        const float x = met_s[i][COLS][lane], y = met_s[i][COLS + 1][lane], f = x == -INFINITY ? (y == 0.f ? 0.f : y) : exp2_fast(x - top);
+        if (f == 0.f) continue;
+        l = fmaf(f, y, l);
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) acc[j] = fmaf(f, met_s[i][j][lane], acc[j]);
+      }
+    }
+    const float inv = l == 0.f ? (seq_seen(nk - nq + token, nk, prefix, a.causal, a.window).hi > 0 ? NAN : 0.f) : 1.0f / l;
+    unsigned short* const out = a.out + (int64_t)(q0 + token) * a.ld_out + (head0 + hh) * a.hd;
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h)
+      if (4 * lane + 128 * h < a.hd)
+        *reinterpret_cast<uint2*>(out + 4 * lane + 128 * h) = make_uint2(pack_bf16(acc[4 * h] * inv, acc[4 * h + 1] * inv), pack_bf16(acc[4 * h + 2] * inv, acc[4 * h + 3] * inv));
   }
 }
 

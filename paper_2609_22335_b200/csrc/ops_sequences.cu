@@ -37,21 +37,37 @@ static bool seq_encode(CUtensorMap* out, const void* base, int rank, const int64
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static bool seq_shape_ok(int seqs, int tq, int hq, int hkv, int hd, float scale, int causal, const void* prefix, int window, float cap) {
-  return seqs >= 1 && seqs <= 1 << 20 && tq >= 1 && tq <= 1 << 30 && hkv >= 1 && hq >= hkv && hq % hkv == 0 && hq <= 65536 && hd >= 8 && hd <= 256 && hd % 8 == 0 &&
-         scale > 0.f && scale < 1e30f && window >= 0 && (causal || (window == 0 && !prefix)) && cap >= 0.f && cap < 1e30f;
-}
 // Rows `ld` elements apart that begin on 16 bytes.
 static bool seq_rows_ok(const void* p, int64_t ld, int64_t least) { return p && ld >= least && ld < (int64_t)1 << 38 && ld % 8 == 0 && op_aligned(16, {p}); }
+static bool seq_cache_ok(int n_pages, int page_size, int max_pages) {
+  return n_pages >= 1 && n_pages <= 1 << 30 && page_size >= 1 && page_size <= 1 << 20 && max_pages >= 1 && (int64_t)max_pages * page_size <= 1 << 30;
+}
+// What both attentions ask of their arguments.
+static bool seq_shape_ok(const vla_attention_args& x) {
+  if (x.seqs < 1 || x.seqs > 1 << 20 || x.tq < 1 || x.tq > 1 << 30 || x.hkv < 1 || x.hq < x.hkv || x.hq % x.hkv || x.hq > 65536 || x.hd < 8 || x.hd > 256 || x.hd % 8) return false;
+  if (!(x.scale > 0.f) || !(x.scale < 1e30f) || !(x.cap >= 0.f) || !(x.cap < 1e30f) || x.window < 0 || (!x.causal && (x.window || x.prefix)) || x.reserved) return false;
+  if (!seq_rows_ok(x.q, x.ld_q, (int64_t)x.hq * x.hd) || !seq_rows_ok(x.out, x.ld_out, (int64_t)x.hq * x.hd)) return false;
+  if (!seq_rows_ok(x.k, x.ld_k, (int64_t)x.hkv * x.hd) || !seq_rows_ok(x.v, x.ld_v, (int64_t)x.hkv * x.hd)) return false;
+  return x.offsets_q && op_aligned(4, {x.offsets_q, x.prefix, x.slopes});
+}
+static SeqArgs seq_args(const vla_attention_args& x) {
+  SeqArgs a = {};
+  a.offsets_q = x.offsets_q; a.prefix = x.prefix; a.slopes = x.slopes;
+  a.q = static_cast<const unsigned short*>(x.q); a.k = static_cast<const unsigned short*>(x.k); a.v = static_cast<const unsigned short*>(x.v);
+  a.out = static_cast<unsigned short*>(x.out);
+  a.ld_q = x.ld_q; a.ld_k = x.ld_k; a.ld_v = x.ld_v; a.ld_out = x.ld_out;
+  a.seqs = x.seqs; a.tq = x.tq; a.hq = x.hq; a.hkv = x.hkv; a.hd = x.hd; a.causal = x.causal ? 1 : 0; a.window = x.window;
+  return a;
+}
 
-static int seq_run(SeqArgs& a, float scale, float cap, void* scratch, size_t scratch_bytes, cudaStream_t s) {
-  if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || (int64_t)scratch_bytes < seq_scratch_bytes(a.hd)) return VLA_ERR_NOMEM;
+static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
+  if (!x.scratch || (reinterpret_cast<uintptr_t>(x.scratch) & 255) || (int64_t)x.scratch_bytes < seq_scratch_bytes(a.hd)) return VLA_ERR_NOMEM;
   const SeqFold f = seq_fold(a.hq, a.hkv);
   a.group = f.group; a.fold = f.fold; a.per_group = f.per_group; a.tokens = f.tokens;
-  a.scratch = static_cast<char*>(scratch);
-  a.scale_log2 = scale * 1.44269504f;
-  a.capped = cap > 0.f ? 1 : 0;
-  a.cap_in = cap > 0.f ? scale / cap : 0.f; a.cap_log2 = cap * 1.44269504f;
+  a.scratch = static_cast<char*>(x.scratch);
+  a.scale_log2 = x.scale * 1.44269504f;
+  a.capped = x.cap > 0.f ? 1 : 0;
+  a.cap_in = a.capped ? x.scale / x.cap : 0.f; a.cap_log2 = x.cap * 1.44269504f;
   const int mode = seq_mode(a.tq, a.seqs, f.fold, a.hd), bn
    = seq_bn(mode), nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
   // (blocks of one head of all sequences, at most, counted in 32 bits)
@@ -79,10 +95,10 @@ static int seq_run(SeqArgs& a, float scale, float cap, void* scratch, size_t scr
                                                                : (extra ? vla_op_sequences_kernel<SEQ_WIDE, true> : vla_op_sequences_kernel<SEQ_WIDE, false>));
   const int rc = op_launch(kernel, shares, seq_threads(mode), seq_smem(mode), 1, s, a, maps, op_fault());
   if (rc != VLA_OK) return rc;
-  // (rows that an item can have: those of its tiles, and those of all tokens)
+  // Rows that an item can have: those of its tiles, and those of all tokens; a warp each, or some one after another beyond sixteen blocks an SM.
   const int64_t rows = (int64_t)a.tq * a.fold;
-  const int most = rows < seq_item_rows(mode) ? (int)rows : seq_item_rows(mode);
-  return op_launch_2d(vla_op_sequences_join_kernel, shares, (most + SEQ_JOIN_ROWS - 1) / SEQ_JOIN_ROWS, SEQ_JOIN_THREADS, s, a, mode);
+  const int most = rows < seq_item_rows(mode) ? (int)rows : seq_item_rows(mode), blocks = seq_min(most, 16 * dev.sms / shares);
+  return op_launch_2d(mode == SEQ_WIDE ? vla_op_sequences_join_kernel<true> : vla_op_sequences_join_kernel<false>, shares, blocks, SEQ_JOIN_THREADS, s, a, mode);
 }
 
 }  // namespace vla
@@ -95,63 +111,43 @@ int vla_op_attention_sequences_scratch_bytes(int32_t hd, size_t* out_bytes) {
   return VLA_OK;
 }
 
-int vla_op_attention_packed(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* out, int64_t ld_out,
-                            const int32_t* offsets_q, const int32_t* offsets_k, int32_t seqs, int32_t tq, int32_t tk, int32_t hq, int32_t hkv,
-                            int32_t hd, float scale, int32_t causal, const int32_t* prefix, int32_t window, float cap, const float* slopes,
-                            void* scratch, size_t scratch_bytes, void* stream) {
+int vla_op_attention_packed(const vla_attention_args* args, void* stream) {
   using namespace vla;
-  if (!seq_shape_ok(seqs, tq, hq, hkv, hd, scale, causal, prefix, window, cap) || tk < 1 || tk > 1 << 30) return VLA_ERR_INVALID;
-  if (!seq_rows_ok(q, ld_q, (int64_t)hq * hd) || !seq_rows_ok(out, ld_out, (int64_t)hq * hd) || !seq_rows_ok(k, ld_k, (int64_t)hkv * hd) || !seq_rows_ok(v, ld_v, (int64_t)hkv * hd))
-    return VLA_ERR_INVALID;
-  if (!offsets_q || !offsets_k || !op_aligned(4, {offsets_q, offsets_k, prefix, slopes})) return VLA_ERR_INVALID;
-  SeqArgs a = {};
-  a.offsets_q = offsets_q; a.offsets_k = offsets_k; a.prefix = prefix; a.slopes = slopes;
-  a.q = static_cast<const unsigned short*>(q); a.k = static_cast<const unsigned short*>(k); a.v = static_cast<const unsigned short*>(v);
-  a.out = static_cast<unsigned short*>(out);
-  a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out;
-  a.seqs = seqs; a.tq = tq; a.tk = tk; a.hq = hq; a.hkv = hkv; a.hd = hd; a.causal = causal ? 1 : 0; a.window = window;
-  return seq_run(a, scale, cap, scratch, scratch_bytes, static_cast<cudaStream_t>(stream));
+  if (!args) return VLA_ERR_INVALID;
+  const vla_attention_args& x = *args;
+  if (!seq_shape_ok(x) || x.tk < 1 || x.tk > 1 << 30 || !x.offsets_k || !op_aligned(4, {x.offsets_k})) return VLA_ERR_INVALID;
+  SeqArgs a = seq_args(x);
+  a.offsets_k = x.offsets_k; a.tk = x.tk;
+  return seq_run(a, x, static_cast<cudaStream_t>(stream));
 }
 
-int vla_op_attention_paged(const void* q, int64_t ld_q, const void* k_cache, int64_t row_k, int64_t page_k, const void* v_cache, int64_t row_v,
-                           int64_t page_v, void* out, int64_t ld_out, const int32_t* pages, const int32_t* lengths, const int32_t* offsets,
-                           int32_t seqs, int32_t tq, int32_t n_pages, int32_t page_size, int32_t max_pages, int32_t hq, int32_t hkv, int32_t hd,
-                           float scale, int32_t causal, const int32_t* prefix, int32_t window, float cap, const float* slopes, void* scratch,
-                           size_t scratch_bytes, void* stream) {
+int vla_op_attention_paged(const vla_attention_args* args, void* stream) {
   using namespace vla;
-  if (!seq_shape_ok(seqs, tq, hq, hkv, hd, scale, causal, prefix, window, cap)) return VLA_ERR_INVALID;
-  if (n_pages < 1 || n_pages > 1 << 30 || page_size < 8 || page_size % 8 || page_size > 1 << 20 || max_pages < 1 || (int64_t)max_pages * page_size > 1 << 30) return VLA_ERR_INVALID;
-  if (!seq_rows_ok(q, ld_q, (int64_t)hq * hd) || !seq_rows_ok(out, ld_out, (int64_t)hq * hd) || !seq_rows_ok(k_cache, row_k, (int64_t)hkv * hd) ||
-      !seq_rows_ok(v_cache, row_v, (int64_t)hkv * hd) || !seq_rows_ok(k_cache, page_k, row_k) || !seq_rows_ok(v_cache, page_v, row_v))
-    return VLA_ERR_INVALID;
-  if (!pages || !lengths || !offsets || !op_aligned(4, {pages, lengths, offsets, prefix, slopes})) return VLA_ERR_INVALID;
-  SeqArgs a = {};
-  a.offsets_q = offsets; a.lengths = lengths; a.pages = pages; a.prefix = prefix; a.slopes = slopes;
-  a.q = static_cast<const unsigned short*>(q); a.k = static_cast<const unsigned short*>(k_cache); a.v = static_cast<const unsigned short*>(v_cache);
-  a.out = static_cast<unsigned short*>(out);
-  a.ld_q = ld_q; a.ld_k = row_k; a.page_k = page_k; a.ld_v = row_v; a.page_v = page_v; a.ld_out = ld_out;
-  a.seqs = seqs; a.tq = tq; a.n_pages = n_pages; a.page_size = page_size; a.max_pages = max_pages; a.hq = hq; a.hkv = hkv; a.hd = hd;
-  a.causal = causal ? 1 : 0; a.window = window;
-  return seq_run(a, scale, cap, scratch, scratch_bytes, static_cast<cudaStream_t>(stream));
+  if (!args) return VLA_ERR_INVALID;
+  const vla_attention_args& x = *args;
+  if (!seq_shape_ok(x) || !seq_cache_ok(x.n_pages, x.page_size, x.max_pages) || x.page_size < 8 || x.page_size % 8) return VLA_ERR_INVALID;
+  if (!seq_rows_ok(x.k, x.page_k, x.ld_k) || !seq_rows_ok(x.v, x.page_v, x.ld_v) || !x.pages || !x.lengths || !op_aligned(4, {x.pages, x.lengths})) return VLA_ERR_INVALID;
+  SeqArgs a = seq_args(x);
+  a.lengths = x.lengths; a.pages = x.pages; a.page_k = x.page_k; a.page_v = x.page_v;
+  a.n_pages = x.n_pages; a.page_size = x.page_size; a.max_pages = x.max_pages;
+  return seq_run(a, x, static_cast<cudaStream_t>(stream));
 }
 
-int vla_op_cache_store(const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* k_cache, int64_t row_k, int64_t page_k, void* v_cache,
-                       int64_t row_v, int64_t page_v, const int32_t* pages, const int32_t* lengths, const int32_t* offsets, int32_t seqs, int32_t t,
-                       int32_t n_pages, int32_t page_size, int32_t max_pages, int32_t width, void* stream) {
+int vla_op_cache_store(const vla_cache_store_args* args, void* stream) {
   using namespace vla;
-  if (seqs < 1 || seqs > 1 << 20 || t < 1 || t > 1 << 30 || n_pages < 1 || n_pages > 1 << 30 || page_size < 1 || page_size > 1 << 20 || max_pages < 1 ||
-      (int64_t)max_pages * page_size > 1 << 30 || width < 8 || width % 8 || width > 1 << 24)
-    return VLA_ERR_INVALID;
-  if (!seq_rows_ok(k, ld_k, width) || !seq_rows_ok(v, ld_v, width) || !seq_rows_ok(k_cache, row_k, width) || !seq_rows_ok(v_cache, row_v, width) ||
-      !seq_rows_ok(k_cache, page_k, row_k) || !seq_rows_ok(v_cache, page_v, row_v) || !pages || !lengths || !offsets || !op_aligned(4, {pages, lengths, offsets}))
+  if (!args) return VLA_ERR_INVALID;
+  const vla_cache_store_args& x = *args;
+  if (x.seqs < 1 || x.seqs > 1 << 20 || x.t < 1 || x.t > 1 << 30 || !seq_cache_ok(x.n_pages, x.page_size, x.max_pages) || x.width < 8 || x.width % 8 || x.width > 1 << 24) return VLA_ERR_INVALID;
+  if (!seq_rows_ok(x.k, x.ld_k, x.width) || !seq_rows_ok(x.v, x.ld_v, x.width) || !seq_rows_ok(x.k_cache, x.row_k, x.width) || !seq_rows_ok(x.v_cache, x.row_v, x.width) ||
+      !seq_rows_ok(x.k_cache, x.page_k, x.row_k) || !seq_rows_ok(x.v_cache, x.page_v, x.row_v) || !x.pages || !x.lengths || !x.offsets || !op_aligned(4, {x.pages, x.lengths, x.offsets}))
     return VLA_ERR_INVALID;
   StoreArgs g;
-  g.k = static_cast<const unsigned short*>(k); g.v = static_cast<const unsigned short*>(v);
-  g.k_cache = static_cast<unsigned short*>(k_cache); g.v_cache = static_cast<unsigned short*>(v_cache);
-  g.ld_k = ld_k; g.ld_v = ld_v; g.row_k = row_k; g.row_v = row_v; g.page_k = page_k; g.page_v = page_v;
-  g.pages = pages; g.lengths = lengths; g.offsets = offsets;
-  g.t = t; g.seqs = seqs; g.n_pages = n_pages; g.page_size = page_size; g.max_pages = max_pages; g.width = width;
-  return op_launch(vla_op_cache_store_kernel, (t - 1) / (STORE_THREADS / 32) + 1, STORE_THREADS, 0, 1, static_cast<cudaStream_t>(stream), g);
+  g.k = static_cast<const unsigned short*>(x.k); g.v = static_cast<const unsigned short*>(x.v);
+  g.k_cache = static_cast<unsigned short*>(x.k_cache); g.v_cache = static_cast<unsigned short*>(x.v_cache);
+  g.ld_k = x.ld_k; g.ld_v = x.ld_v; g.row_k = x.row_k; g.row_v = x.row_v; g.page_k = x.page_k; g.page_v = x.page_v;
+  g.pages = x.pages; g.lengths = x.lengths; g.offsets = x.offsets;
+  g.t = x.t; g.seqs = x.seqs; g.n_pages = x.n_pages; g.page_size = x.page_size; g.max_pages = x.max_pages; g.width = x.width;
+  return op_launch(vla_op_cache_store_kernel, (x.t - 1) / (STORE_THREADS / 32) + 1, STORE_THREADS, 0, 1, static_cast<cudaStream_t>(stream), g);
 }
 
 }  // extern "C"

@@ -75,10 +75,12 @@ SEQ_HD int seq_owner(const SeqShares& s, int64_t at) {
   const int64_t bound = s.more * (s.each + 1);
   return (int)(at < bound ? seq_div(at, s.each + 1) : s.more + seq_div(at - bound, s.each));
 }
-// Whether items stay whole: a share then has those whose first tick is its.  Where the longest is short beside a share, cutting gains less than
-// the parts' way through memory costs.
-SEQ_HD bool seq_whole(const SeqShares& s, int longest, int w) { return longest <= w + 2 || 4 * (int64_t)longest <= s.each; }
-
+// Whether items stay whole: a share then has those whose first tick is its.  Cut, a call takes a share and the join, whole as many items as the fullest share
+// has -- of one length that many times it, of several a share and most of the longest.  The join's time is that of some blocks.
+SEQ_HD bool seq_whole(const SeqShares& s, int64_t items, int longest, int join) {
+  const int64_t cut = s.each + join, fullest = seq_div(items + s.n - 1, s.n) * longest, mixed = s.each + longest - longest / 4;
+  return (fullest < mixed ? fullest : mixed) <= cut;
+}
 // x / d = x * magic >> shift for 0 <= x < 2^31, d from 2 to 2^30: with 2^(l-1) < d <= 2^l, magic = 2^(31+l) / d rounded up is below 2^32 and too large by less
 // than 1, which makes x * magic / 2^(31+l) too large by less than 2^-l <= 1 / d.
 inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
@@ -98,13 +100,15 @@ inline int seq_mode(int64_t tq, int seqs, int fold, int hd) {
 SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
 // What an item takes beside its blocks, in blocks: its first loads, the last block's chain, the result.
 SEQ_HD constexpr int seq_item_ticks(int mode) { return mode == SEQ_TWO ? 2 : 3; }
+SEQ_HD constexpr int seq_join_ticks(int mode) { return mode == SEQ_TWO ? 5 : 6; }
 SEQ_HD int seq_item_rows(int mode) { return mode == SEQ_TWO ? 2 * SEQ_ROWS : SEQ_ROWS; }
 SEQ_HD int seq_cols(int hd) { return (hd + 15) / 16 * 16; }      // columns of the result's accumulator
 inline int seq_shares(int mode, int sms) { return mode == SEQ_ONE ? seq_min(2 * sms, SEQ_MAX_SHARES) : seq_min(sms, SEQ_MAX_SHARES / 2); }
 // Shared memory for tiles and stages, with 1 KB to begin on a boundary; the rest of the SM's 227 KB (or half of it) is for what is declared in the kernels.
 SEQ_HD int seq_smem(int mode) { return (mode == SEQ_ONE ? 110 : 225) * 1024; }
 // Scratch: header, records, two parts of a share.  The same for every call with this head width.
-SEQ_HD int64_t seq_part_floats(int mode, int hd) { return (int64_t)seq_item_rows(mode) * (seq_cols(hd) + 2); }
+SEQ_HD int seq_row_floats(int hd) { return seq_cols(hd) + 8; }      // (rows begin on 32 bytes)
+SEQ_HD int64_t seq_part_floats(int mode, int hd) { return (int64_t)seq_item_rows(mode) * seq_row_floats(hd); }
 inline int64_t seq_scratch_bytes(int hd) {
   return SEQ_HEADER + (int64_t)SEQ_MAX_SHARES * SEQ_RECORD + 2 * (int64_t)SEQ_MAX_SHARES * (hd > 128 ? seq_part_floats(SEQ_WIDE, hd) / 2 : seq_part_floats(SEQ_ONE, hd)) * 4;
 }
