@@ -295,6 +295,17 @@ __device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, i
   }
 }
 
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_of(const uint32_t* v) { return pack2(__uint_as_float(v[0]), __uint_as_float(v[1])); }
+__device__ __forceinline__ void pair_to(uint32_t* v, uint64_t x) {
+  float a, b;
+  unpack2(x, a, b);
+  v[0] = __float_as_uint(a); v[1] = __float_as_uint(b);
+}
 // One block of a row's online softmax: BN scores in, BN / 2 pairs of bf16 probabilities out (front half of the registers).
 template <int BN>
 __device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_run, float& l_run, float& alpha) {
@@ -313,7 +324,7 @@ __device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_ru
 #pragma unroll
   for (int j = 0; j < BN; j += 2) {
     float p0, p1;
-    unpack2(fma2(pack2(__uint_as_float(sr[j]), __uint_as_float(sr[j + 1])), sl2_2, mb_2), p0, p1);
+    unpack2(fma2(pair_of(sr + j), sl2_2, mb_2), p0, p1);
     p0 = exp2_fast(p0); p1 = exp2_fast(p1);
     s2[(j >> 1) & 1] = add2(s2[(j >> 1) & 1], pack2(p0, p1));
     sr[j >> 1] = pack_bf16(p0, p1);
@@ -322,11 +333,6 @@ __device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_ru
   unpack2(add2(s2[0], s2[1]), x0, x1);
   l_run = l_run * alpha + (x0 + x1);
   m_run = mx;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
 }
 __device__ __forceinline__ void st_global_32(void* p, const uint32_t* v) {      // 32 bytes on their boundary
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -611,16 +617,44 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         float sl2 = a.scale_log2;
         if (EXTRA) {
           const float d = (float)(p - c0);
+          uint64_t by = pack2(a.scale_log2, a.scale_log2);
           if (a.capped) {
+            // cap tanh(x): an odd polynomial up to 1/2 (least largest relative error there, 1.3e-8), by powers and reciprocals where a score is beyond.
+            float top = 0.f;
 #pragma unroll
-            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(a.cap_log2 * seq_tanh(__uint_as_float(sr[j]) * a.cap_in));
-          } else {
+            for (int j = 0; j < BN; j += 2) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(sr[j])), fabsf(__uint_as_float(sr[j + 1]))));
+            if (__any_sync(0xffffffffu, !(top * a.cap_in <= 0.5f))) {
 #pragma unroll
-            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(__uint_as_float(sr[j]) * a.scale_log2);
+              for (int j = 0; j < BN; ++j) {
+                float e, r;                   // 1 - 2 / (1 + e^2x), off by 2^-23 of the cap
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__uint_as_float(sr[j]) * (a.cap_in * 2.885390082f)));
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+                sr[j] = __float_as_uint(fmaf(-2.0f, r, 1.0f));
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < BN; j += 2) {
+                const uint64_t x = mul2(pair_of(sr + j), pack2(a.cap_in, a.cap_in)), z = mul2(x, x);
+                uint64_t y = fma2(z, pack2(1.7135007306933403e-02f, 1.7135007306933403e-02f), pack2(-5.298607423901558e-02f, -5.298607423901558e-02f));
+                y = fma2(y, z, pack2(1.3324779272079468e-01f, 1.3324779272079468e-01f));
+                y = fma2(y, z, pack2(-3.333306908607483e-01f, -3.333306908607483e-01f));
+                pair_to(sr + j, mul2(fma2(y, z, pack2(1.0f, 1.0f)), x));
+              }
+            }
+            by = pack2(a.cap_log2, a.cap_log2);
           }
-          if (a.slopes) {
+          if (!a.slopes) {
 #pragma unroll
-            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(fmaf(-slope, fabsf(d - (float)j), __uint_as_float(sr[j])));
+            for (int j = 0; j < BN; j += 2) pair_to(sr + j, mul2(pair_of(sr + j), by));
+          } else if (__all_sync(0xffffffffu, d >= (float)BN)) {       // all keys on one side of all rows: the distance is linear
+            const uint64_t up = pack2(slope, slope), from = pack2(-slope * d, -slope * d);
+#pragma unroll
+            for (int j = 0; j < BN; j += 2) pair_to(sr + j, fma2(pair_of(sr + j), by, fma2(up, pack2((float)j, (float)(j + 1)), from)));
+          } else {
+            float one, two;
+            unpack2(by, one, two);
+#pragma unroll
+            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(fmaf(-slope, fabsf(d - (float)j), __uint_as_float(sr[j]) * one));
           }
           sl2 = 1.0f;
         }
