@@ -169,28 +169,43 @@ __device__ __forceinline__ void bias_load(const LinearArgs& g, float* b, int f, 
     }
   }
 }
+// What the addends need in front of a tile's accumulators: the first fragment of residual rows, and the others of this warp on their way to the L2 cache.  Without
+// it a layer of 50 x 2048 x 2048 waited 5 us for rows that nobody had asked for while the products ran.
+template <int VEC>
+__device__ __forceinline__ void residual_first(const LinearArgs& g, uint32_t* res, int lane, int row0, int rows, int n0, int lo, int hi) {
+  if (!g.residual || rows <= 0 || lo >= hi) return;
+  residual_load<VEC>(g, res, row0 + (lane >> 2), n0 + 32 * lo, lane & 3);
+  const int size = g.residual_f32 ? 4 : 2, bytes = (min(n0 + 32 * hi, g.n) - (n0 + 32 * lo)) * size;
+  if (lane < rows) {
+    const char* p = static_cast<const char*>(g.residual) + ((long long)(row0 + lane) * g.ld_residual + n0 + 32 * lo) * size;
+    for (int x = 0; x < bytes; x += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + x));
+  }
+}
 // This warp's share of a tile's columns: groups of 32, [lo, hi), for its 32 lanes.  `part` (split K): the other CTAs'
 // fragments of the same group, written by the threads that hold the same place.  `n_acc`: accumulators of the same columns,
-// `acc_stride` apart, that add up to the result.
+// `acc_stride` apart, that add up to the result.  `res`: see residual_first; the next fragment's rows are asked for as soon as one's are added.
 template <int ACT, int VEC, bool ADD>
-__device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, int lane, int row0, int rows, int n0, int lo, int hi, const float4* part,
+__device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, int lane, int row0, int rows, int n0, int lo, int hi, uint32_t* res, const float4* part,
                                             int n_part, int part_stride, int n_acc = 1, uint32_t acc_stride = 0) {
   const int q = lane & 3;
 #pragma unroll 1
   for (int h = 0; h < 2 && 16 * h < rows; ++h) {
     if (lo >= hi) break;
     const uint32_t th = tmem + ((uint32_t)(16 * h) << 16);
-    uint32_t nx[EPI], res[EPI];
+    uint32_t nx[EPI];
     const int row = row0 + 16 * h + (lane >> 2);
-    if (ADD && g.residual) residual_load<VEC>(g, res, row, n0 + 32 * lo, q);
-    tmem_ld_frag(th + 32u * (uint32_t)lo, nx);
+    if (!ADD) tmem_ld_frag(th + 32u * (uint32_t)lo, nx);
 #pragma unroll 1
     for (int c = lo; c < hi; ++c) {
-      float v[EPI];
+      float v[EPI], b[8];
+      if (ADD) {                               // (the registers go to the residual rows in flight, not to the next accumulators)
+        tmem_ld_frag(th + 32u * (uint32_t)c, nx);
+        if (g.bias) bias_load<VEC>(g, b, n0 + 32 * c, q);
+      }
       tmem_ld_wait();
 #pragma unroll
       for (int j = 0; j < EPI; ++j) v[j] = __uint_as_float(nx[j]);
-      tmem_ld_frag(th + 32u * (uint32_t)(c + 1 < hi ? c + 1 : c), nx);
+      if (!ADD) tmem_ld_frag(th + 32u * (uint32_t)(c + 1 < hi ? c + 1 : c), nx);
 #pragma unroll 1
       for (int r = 1; r < n_acc; ++r) {
         uint32_t t[EPI];
@@ -210,8 +225,6 @@ __device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, 
       }
       if (ADD) {
         if (g.bias) {
-          float b[8];
-          bias_load<VEC>(g, b, n0 + 32 * c, q);
 #pragma unroll
           for (int j = 0; j < EPI; ++j) v[j] += b[2 * (j >> 2) + (j & 1)];
         }
@@ -224,6 +237,7 @@ __device__ __forceinline__ void linear_rows(const LinearArgs& g, uint32_t tmem, 
         if (g.residual) {
           residual_add<VEC>(g, res, v, q);
           if (c + 1 < hi) residual_load<VEC>(g, res, row, n0 + 32 * (c + 1), q);
+          else if (h == 0 && rows > 16) residual_load<VEC>(g, res, row + 16, n0 + 32 * lo, q);
         }
       } else {
         activate<ACT, EPI>(v);
@@ -313,24 +327,36 @@ __global__ void __launch_bounds__(LIN_THREADS, 2) vla_op_linear_kernel(const __g
   const int quarter = warp & 3, half = warp >= 6 ? 1 : 0;             // (epilogue warps 2..9: a quarter of the lanes is fixed by warp % 4)
   const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
   const int groups = (g.bn + 31) / 32;
-  auto rows_of = [&](uint32_t acc, int t, int lo, int hi, const float4* part, int n_part, int part_stride) {
-    const int row0 = t % g.tiles_m * g.bm + 32 * quarter, rows = min(g.bm, g.m - t % g.tiles_m * g.bm) - 32 * quarter, n0 = t / g.tiles_m * g.bn;
-    LinearArgs gg = g;
+  uint32_t res[EPI];                                                  // (ADD alone)
+  auto place = [&](int t, int& row0, int& rows, int& n0, LinearArgs& gg) {
+    row0 = t % g.tiles_m * g.bm + 32 * quarter; rows = min(g.bm, g.m - t % g.tiles_m * g.bm) - 32 * quarter; n0 = t / g.tiles_m * g.bn;
     gg.m = row0 + max(rows, 0);                                       // (this tile's rows and features only)
     gg.n_end = min(g.n, n0 + g.bn);
-    if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
-    else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
-    else linear_rows<ACT_NONE, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, part, n_part, part_stride);
+  };
+  auto first_of = [&](int t, int lo, int hi) {
+    int row0, rows, n0;
+    LinearArgs gg = g;
+    place(t, row0, rows, n0, gg);
+    residual_first<VEC>(gg, res, lane, row0, rows, n0, lo, hi);
+  };
+  auto rows_of = [&](uint32_t acc, int t, int lo, int hi, const float4* part, int n_part, int part_stride) {
+    int row0, rows, n0;
+    LinearArgs gg = g;
+    place(t, row0, rows, n0, gg);
+    if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, res, part, n_part, part_stride);
+    else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, res, part, n_part, part_stride);
+    else linear_rows<ACT_NONE, VEC, ADD>(gg, acc + lanes, lane, row0, rows, n0, lo, hi, res, part, n_part, part_stride);
   };
   if (g.ks == 1) {
     if (warp >= 2) {
       uint32_t i = 0;
       for (int t = first_tile; t < g.tiles; t += step, ++i) {
         const uint32_t buf = n_acc == 2 ? i & 1u : 0u, use = n_acc == 2 ? i >> 1 : i;
+        const int mid = (groups + 1) / 2;
+        if (ADD) first_of(t, half ? mid : 0, half ? groups : mid);
         if (!mbar_wait(c, accf0 + 8u * buf, use & 1u)) break;
         __syncwarp();
         tc_fence_after();
-        const int mid = (groups + 1) / 2;
         rows_of(tmem + 128u * buf, t, half ? mid : 0, half ? groups : mid, nullptr, 0, 0);
         tc_fence_before();
         arrive_warp(acce0 + 8u * buf, lane);
@@ -339,6 +365,9 @@ __global__ void __launch_bounds__(LIN_THREADS, 2) vla_op_linear_kernel(const __g
   } else {
     // ---------------- split K: every CTA sends the columns of the others away, then finishes its own
     const int own = groups / g.ks, thread = 32 * quarter + lane, stride = own * 2 * 4 * 128;          // float4 of one source CTA
+    // the two warps of a quarter share the owned groups
+    const int lo = rank * own, mid = lo + (own + 1) / 2, hi = lo + own, b = half ? mid : lo, e = half ? hi : mid;
+    if (ADD && warp >= 2) first_of(first_tile, b, e);
     cluster_sync();                                                   // every CTA of the cluster has started
     if (warp >= 2) {
       mbar_wait(c, accf0, 0u);
@@ -369,9 +398,7 @@ __global__ void __launch_bounds__(LIN_THREADS, 2) vla_op_linear_kernel(const __g
     }
     cluster_sync();
     if (warp >= 2) {
-      // the two warps of a quarter share the owned groups
-      const int lo = rank * own, mid = lo + (own + 1) / 2, hi = lo + own, b = half ? mid : lo;
-      rows_of(tmem, first_tile, b, half ? hi : mid, reinterpret_cast<const float4*>(smem_raw) + (b - lo) * 2 * (4 * 128) + thread, g.ks - 1, stride);
+      rows_of(tmem, first_tile, b, e, reinterpret_cast<const float4*>(smem_raw) + (b - lo) * 2 * (4 * 128) + thread, g.ks - 1, stride);
     }
   }
   tc_fence_before();

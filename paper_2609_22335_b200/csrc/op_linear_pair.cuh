@@ -136,17 +136,19 @@ __global__ void __launch_bounds__(LIN_THREADS, 1) vla_op_linear_pair_kernel(cons
     uint32_t buf = 0, bph = 0u;
     for (int t = first_tile; t < g.tiles; t += step) {
       const uint32_t acc = tmem + set_cols * buf + lanes;
-      if (!mbar_wait(c, accf0 + 8u * buf, bph)) break;
-      __syncwarp();
-      tc_fence_after();
       const int cta_row = (2 * (t % g.tiles_m) + rank) * g.bm, row0 = cta_row + 32 * quarter, rows = min(g.bm, g.m - cta_row) - 32 * quarter;
       const int n0 = t / g.tiles_m * g.bn;
       LinearArgs gg = g;
       gg.m = row0 + max(rows, 0);                                     // (this tile's rows and features only)
       gg.n_end = min(g.n, n0 + g.bn);
-      if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
-      else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
-      else linear_rows<ACT_NONE, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
+      uint32_t res[EPI];                                              // (ADD alone)
+      if (ADD) residual_first<VEC>(gg, res, lane, row0, rows, n0, lo, hi);
+      if (!mbar_wait(c, accf0 + 8u * buf, bph)) break;
+      __syncwarp();
+      tc_fence_after();
+      if (g.act == ACT_GELU) linear_rows<ACT_GELU, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, res, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
+      else if (g.act == ACT_SILU) linear_rows<ACT_SILU, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, res, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
+      else linear_rows<ACT_NONE, VEC, ADD>(gg, acc, lane, row0, rows, n0, lo, hi, res, nullptr, 0, 0, PARTS ? parts : 1, part_cols);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(acce_leader + 8u * buf) : "memory");
