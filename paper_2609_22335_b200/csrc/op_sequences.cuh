@@ -307,12 +307,16 @@ __device__ __forceinline__ void pair_to(uint32_t* v, uint64_t x) {
   v[0] = __float_as_uint(a); v[1] = __float_as_uint(b);
 }
 // One block of a row's online softmax: BN scores in, BN / 2 pairs of bf16 probabilities out (front half of the registers).
+// `known`: the scores' largest absolute value, where the caller has it and they lie close together (else below 0): as good a reference as their maximum.
 template <int BN>
-__device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_run, float& l_run, float& alpha) {
-  float m4[4] = {m_run, __uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2])};
+__device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float known, float& m_run, float& l_run, float& alpha) {
+  float mx = fmaxf(m_run, known);
+  if (known < 0.f) {
+    float m4[4] = {m_run, __uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2])};
 #pragma unroll
-  for (int j = 3; j < BN - 1; j += 2) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
-  float mx = fmaxf(max3(m4[0], m4[1], m4[2]), fmaxf(m4[3], __uint_as_float(sr[BN - 1])));
+    for (int j = 3; j < BN - 1; j += 2) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
+    mx = fmaxf(max3(m4[0], m4[1], m4[2]), fmaxf(m4[3], __uint_as_float(sr[BN - 1])));
+  }
   alpha = 1.0f;
   if (m_run != -INFINITY) {
     if ((mx - m_run) * sl2 <= ATTN_RESCALE_LOG2) mx = m_run;
@@ -614,10 +618,10 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
 #pragma unroll
         for (int k = 0; k < BN; k += 32) tmem_ld32_nowait(ts + k, sr + k);
         tmem_ld_wait();
-        float sl2 = a.scale_log2;
+        float sl2 = a.scale_log2, known = -1.0f;
         if (EXTRA) {
           const float d = (float)(p - c0);
-          uint64_t by = pack2(a.scale_log2, a.scale_log2);
+          sl2 = a.capped ? a.cap_log2 : a.scale_log2;                  // what makes log2 units of the scores in the registers
           if (a.capped) {
             // cap tanh(x): an odd polynomial up to 1/2 (least largest relative error there, 1.3e-8), by powers and reciprocals where a score is beyond.
             float top = 0.f;
@@ -640,23 +644,23 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
                 y = fma2(y, z, pack2(-3.333306908607483e-01f, -3.333306908607483e-01f));
                 pair_to(sr + j, mul2(fma2(y, z, pack2(1.0f, 1.0f)), x));
               }
+              // All scores lie within half the cap of 0, 46 powers of e at a cap of 50: nobody need look for the maximum.
+              if (a.cap_log2 <= 100.0f) known = top * a.cap_in;
             }
-            by = pack2(a.cap_log2, a.cap_log2);
           }
-          if (!a.slopes) {
+          if (a.slopes) {
+            const uint64_t by = pack2(sl2, sl2);
+            if (__all_sync(0xffffffffu, d >= (float)BN)) {             // all keys on one side of all rows: the distance is linear
+              const uint64_t up = pack2(slope, slope), from = pack2(-slope * d, -slope * d);
 #pragma unroll
-            for (int j = 0; j < BN; j += 2) pair_to(sr + j, mul2(pair_of(sr + j), by));
-          } else if (__all_sync(0xffffffffu, d >= (float)BN)) {       // all keys on one side of all rows: the distance is linear
-            const uint64_t up = pack2(slope, slope), from = pack2(-slope * d, -slope * d);
+              for (int j = 0; j < BN; j += 2) pair_to(sr + j, fma2(pair_of(sr + j), by, fma2(up, pack2((float)j, (float)(j + 1)), from)));
+            } else {
 #pragma unroll
-            for (int j = 0; j < BN; j += 2) pair_to(sr + j, fma2(pair_of(sr + j), by, fma2(up, pack2((float)j, (float)(j + 1)), from)));
-          } else {
-            float one, two;
-            unpack2(by, one, two);
-#pragma unroll
-            for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(fmaf(-slope, fabsf(d - (float)j), __uint_as_float(sr[j]) * one));
+              for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(fmaf(-slope, fabsf(d - (float)j), __uint_as_float(sr[j]) * sl2));
+            }
+            sl2 = 1.0f;
+            known = -1.0f;
           }
-          sl2 = 1.0f;
         }
         if (__any_sync(0xffffffffu, c0 + BN > seen.hi || (c0 < seen.lo && c0 + BN > w.prefix))) {
 #pragma unroll
@@ -668,7 +672,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
           }
         }
         float alpha;
-        seq_softmax<BN>(sr, sl2, m_run, l_run, alpha);
+        seq_softmax<BN>(sr, sl2, known, m_run, l_run, alpha);
         if (i > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
           if (!TWO && ok) ok = mbar_wait(c, o_done + 8u * ((i - 1) & 1), (ns[(i - 1) & 1] - 1) & 1u);
           __syncwarp();
@@ -702,7 +706,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       }
       __syncwarp();
       tc_fence_after();
-      m_run *= EXTRA ? 1.0f : a.scale_log2;   // (log2 units from here on; -inf stays, scale > 0)
+      m_run *= EXTRA ? (a.slopes ? 1.0f : (a.capped ? a.cap_log2 : a.scale_log2)) : a.scale_log2;   // (log2 units from here on; -inf stays, scale > 0)
       const float inv = l_run == 0.f ? (seen.hi > 0 ? NAN : 0.f) : 1.0f / l_run;
       const int at = (TWO ? t * SEQ_ROWS : 0) + row;
       float* const part = whole ? nullptr : seq_part(a, MODE, (int)blockIdx.x, w.part);
