@@ -673,7 +673,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         }
         float alpha;
         seq_softmax<BN>(sr, sl2, known, m_run, l_run, alpha);
-        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.0f)) {
+        if (i > 0 && __any_sync(0xffffffffu, valid && alpha != 1.0f)) {      // (rows that nobody stores may be NaN)
           if (!TWO && ok) ok = mbar_wait(c, o_done + 8u * ((i - 1) & 1), (ns[(i - 1) & 1] - 1) & 1u);
           __syncwarp();
           tc_fence_after();
