@@ -139,6 +139,46 @@ def test_rows_whose_scores_are_far_apart():
         ref.check(run(30 * q, 10 * k, v, e, 4, 2, 64, causal=causal), ref.packed(30 * q, 10 * k, v, e, e, 4, 2, 64, causal=causal))
 
 
+def test_a_query_that_is_nan_is_its_rows_alone():
+    import torch
+    e = [0, 200, 333]
+    for hd in (64, 256):
+        q, k, v = make(333, 4, 2, hd, seed=15)
+        want = ref.packed(q, k, v, e, e, 4, 2, hd, causal=True)
+        q[77, 2 * hd + 3] = math.nan
+        got = run(q, k, v, e, 4, 2, hd, causal=True)
+        assert bool(got[77, 2 * hd:3 * hd].isnan().all())
+        got[77, 2 * hd:3 * hd] = want[0][2][77, 2 * hd:3 * hd].bfloat16()
+        ref.check(got, want)
+
+
+def test_thousands_of_sequences_none_at_all_and_windows_without_end():
+    import torch
+    lengths = [(7 * s) % 4 for s in range(3000)]
+    e = ends(lengths)
+    q, k, v = make(e[-1], 2, 1, 64, seed=16)
+    got, off = run(q, k, v, e, 2, 1, 64, causal=True), torch.tensor(e[:-1], device="cuda")
+    # (rows of up to three: the first of each is its own value, the second weighs two)
+    for n in range(1, 4):
+        first = off[torch.tensor([x == n for x in lengths], device="cuda")]
+        assert bool((got[first].view(-1, 2, 64) == v[first][:, None]).all())
+    picked = [s for s in range(0, 3000, 61)]
+    ref.check(got, [(e[s], e[s + 1], *ref.attend(q[e[s]:e[s + 1]], k[e[s]:e[s + 1]], v[e[s]:e[s + 1]], 2, 1, 64, causal=True)) for s in picked])
+    out = torch.full_like(q, 3.0)
+    assert bool((run(q, k, v, [0] * 5, 2, 1, 64, out=out) == 3).all())
+    for n, keys in ((50, 20), (300, 10)):                # more rows than keys: positions in front of the first one
+        q, k, v = make(n, 2, 1, 64, seed=17, keys=keys)
+        ref.check(run(q, k, v, [0, n], 2, 1, 64, ends_k=[0, keys], causal=True, window=(1 << 31) - 1, prefix=[3]), ref.packed(q, k, v, [0, n], [0, keys], 2, 1, 64, causal=True, prefix=[3]))
+
+
+def test_caps_from_tiny_to_none_to_speak_of():
+    e = [0, 150, 400]
+    q, k, v = make(400, 4, 2, 64, seed=18)
+    for cap in (1e-3, 0.5, 2.0, 5.0, 69.0, 70.0, 1e4, 1e20):
+        # (from 1e4 on the cap changes nothing that 32 bits show, and its share of the tolerance would hide everything)
+        ref.check(run(q, k, v, e, 4, 2, 64, causal=True, cap=cap), ref.packed(q, k, v, e, e, 4, 2, 64, causal=True, cap=0.0 if cap >= 1e4 else cap))
+
+
 def test_the_same_call_gives_the_same_bits_and_two_calls_at_once_do_not_meet():
     import torch
     from paper_2609_22335_b200 import api
