@@ -358,18 +358,6 @@ __device__ __forceinline__ float* seq_part(const SeqArgs& a, int mode, int share
   return reinterpret_cast<float*>(a.scratch + SEQ_HEADER + SEQ_MAX_SHARES * SEQ_RECORD) + (2 * share + which) * seq_part_floats(mode, a.hd);
 }
 
-#ifdef SEQ_TUNE
-__device__ long long g_tune[320][64];
-__device__ long long g_gt[4096][4];
-__device__ long long g_j[320][16];
-#define JT(i, dep) do { if (threadIdx.x == 0 && blockIdx.y == 0) { asm volatile("" :: "r"(__float_as_uint(dep)) : "memory"); g_j[blockIdx.x][i] = clock64(); } } while (0)
-__device__ unsigned g_seq;
-#define TUNE2(code) do { if (lane == 0 && tune_n < 31) { g_tune[blockIdx.x][32 + (++tune_n)] = clock64() * 16 + (code); g_tune[blockIdx.x][32] = tune_n; } } while (0)
-#define TUNE(code) do { if (threadIdx.x == 0 && tune_n < 31) { g_tune[blockIdx.x][++tune_n] = clock64() * 16 + (code); g_tune[blockIdx.x][0] = tune_n; } } while (0)
-#else
-#define TUNE(code)
-#define TUNE2(code)
-#endif
 constexpr int seq_threads(int mode) { return mode == SEQ_TWO ? 384 : 192; }
 // EXTRA: scores are capped or have a bias by distance.
 template <int MODE, bool EXTRA>
@@ -379,17 +367,10 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   constexpr int BN = TWO ? 128 : 64, SOFT = TWO ? 8 : 4;              // keys of a block; softmax warps
   constexpr uint32_t COLS = MODE == SEQ_ONE ? 256 : 512;              // tensor memory: two tiles of scores, then the results
   extern __shared__ char smem_dyn[];
-#ifdef SEQ_TUNE
-  if (threadIdx.x == 0) g_gt[blockIdx.x][0] = gtimer();
-#endif
   __shared__ __align__(8) uint64_t bars[2 * SEQ_MAX_STAGES + 10];
   __shared__ uint32_t tmem_base_s;
   __shared__ unsigned failed_s;
   __shared__ SeqItem item_s;
-#ifdef SEQ_TUNE
-  int tune_n = 0;
-#endif
-  TUNE(0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, NS = a.stages;
   const int nbox = (a.hd + 63) / 64, hdc = seq_cols(a.hd), tokens = (TWO ? 2 : 1) * a.tokens;
   const uint32_t full = smem_u32(bars), empty = full + 8 * SEQ_MAX_STAGES, s_full = empty + 8 * SEQ_MAX_STAGES, p_full = s_full + 16, o_done = p_full + 16,
@@ -410,9 +391,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   }
   if (threadIdx.x < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[threadIdx.x]) : "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-#ifdef SEQ_TUNE
-  if (threadIdx.x == 0) g_gt[blockIdx.x][1] = gtimer();
-#endif
   if (threadIdx.x == 0) {
     record->parts = 0;
     if (blockIdx.x == 0) *err = 0u;
@@ -422,7 +400,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   __syncthreads();
   op_let_next_start();
   tc_fence_after();
-  TUNE(3);
   const uint32_t tmem = tmem_base_s, tmem_o = tmem + 2 * BN;
 
   if (warp >= SOFT) {
@@ -432,20 +409,16 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       // ---------------- loads.  A block of keys is one box of a head's columns, or a box for each piece of a page, issued side by side by the lanes.
       uint32_t s = 0, ph = 1u, items = 0;
       const int chunks = BN / a.chunk;
-      TUNE2(1);
       const SeqStart st = seq_start(a, tokens, BN, W, seq_join_ticks(MODE), (int)gridDim.x, (int)blockIdx.x, lane);
-      TUNE2(2);
       SeqWalk walk = {st.left, st.s, st.unit, st.first, st.tick, st.q};
       if (st.whole && st.tick > 0) walk.take(a, true, tokens, BN, W);      // (that item is the share's before)
       for (;; ++items) {
         const SeqItem w = walk.take(a, st.whole, tokens, BN, W);
         const int n = w.n;
-        TUNE2(3);
         if (lane == 0) {
           ok = items == 0 || mbar_wait(c, q_empty, (items - 1) & 1u);      // Q's tiles are free, and everybody knows the item before
           if (ok) {
             item_s = w;
-            TUNE2(4);
             if (n == 0) {
               asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(q_full) : "memory");
             } else {
@@ -465,7 +438,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         }
         ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
         if (!ok || n == 0) break;
-        TUNE2(5);
         // The order in which the blocks' MMAs come: K0 V0 K1 V1 .. with two tiles, else K0 K1 V0 K2 V1 .. V(n-2) V(n-1).  A page's number is asked for a block ahead.
         struct Box { int which, z, page; };
         auto box = [&](int m) {
@@ -494,7 +466,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
           const Box x = next;
           if (m + 1 < 2 * n) next = box(m + 1);
           const uint32_t bar = full + 8u * s, dst = ring + s * stage_bytes + (uint32_t)(lane * a.chunk * 128);
-          TUNE2(6);
           ok = __all_sync(0xffffffffu, mbar_wait(c, empty + 8u * s, ph));
           if (!ok) break;
           if (lane == 0) mbar_expect_tx(bar, stage_bytes);
@@ -629,7 +600,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       const SeqItem w = item_s;
       arrive_warp(q_empty, lane);
       if (w.n == 0) break;
-      TUNE(1);
       const int n = w.n, token = w.first + (TWO ? t * a.tokens : 0) + tt, head = w.head + hh;
       const bool valid = tt < a.tokens && token < w.nq && hh < w.heads;
       const int p = w.nk - w.nq + token;
@@ -642,7 +612,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         const int slot = TWO ? t : i & 1, c0 = seq_block(SeqBlocks{w.na, w.lo, 0}, w.b0 + i) * BN;
         const uint32_t ts = tmem + lanes + (uint32_t)(BN * slot);
         if (ok) ok = mbar_wait(c, s_full + 8u * slot, ns[slot] & 1u);
-        TUNE(4);
         __syncwarp();
         tc_fence_after();
         uint32_t sr[BN];
@@ -725,7 +694,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         tmem_st_wait();
         tc_fence_before();
         arrive_warp(p_full + 8u * slot, lane);
-        TUNE(5);
         ++ns[slot];
       }
       ring0 += 2u * (uint32_t)n;
@@ -738,7 +706,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       }
       __syncwarp();
       tc_fence_after();
-      TUNE(6);
       m_run *= EXTRA ? (a.slopes ? 1.0f : (a.capped ? a.cap_log2 : a.scale_log2)) : a.scale_log2;   // (log2 units from here on; -inf stays, scale > 0)
       const float inv = l_run == 0.f ? (seen.hi > 0 ? NAN : 0.f) : 1.0f / l_run;
       const int at = (TWO ? t * SEQ_ROWS : 0) + row;
@@ -793,7 +760,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       if (!whole && valid) *reinterpret_cast<float2*>(part_row + hdc) = make_float2(m_run, l_run);
       tc_fence_before();
       arrive_warp(o_free + 8u * (TWO ? t : 0), lane);
-      TUNE(7);
       // Those rows once more, from the keys they see alone.
       while (again) {
         const int src = __ffs(again) - 1;
@@ -822,9 +788,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
     }
   }
   __syncthreads();
-#ifdef SEQ_TUNE
-  if (threadIdx.x == 0) g_gt[blockIdx.x][2] = gtimer();
-#endif
   if (warp == SOFT + 1) tmem_dealloc(tmem, COLS);
   if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(&failed_s) != 0u) *err = (unsigned)DEV_ERR_WAIT_MBAR;
 }
@@ -835,26 +798,13 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
 constexpr int SEQ_JOIN_THREADS = 128, SEQ_JOIN_WARPS = SEQ_JOIN_THREADS / 32;
 template <bool WIDE>
 __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel(const __grid_constant__ SeqArgs a, int mode) {
-#ifdef SEQ_TUNE
-  const int jb = 1024 + (int)blockIdx.x;
-  if (threadIdx.x == 0 && blockIdx.y == 0) g_gt[jb][0] = gtimer();
-#endif
   asm volatile("griddepcontrol.wait;" ::: "memory");
   op_let_next_start();
-#ifdef SEQ_TUNE
-  JT(0, 0.f);
-#endif
-#ifdef SEQ_TUNE
-  if (threadIdx.x == 0 && blockIdx.y == 0) g_gt[jb][1] = gtimer();
-#endif
   const int share = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, hdc = seq_cols(a.hd), stride = seq_row_floats(a.hd);
   const int4* const rec = reinterpret_cast<const int4*>(a.scratch + SEQ_HEADER + share * SEQ_RECORD);
   const int4 x = __ldcg(rec), y = __ldcg(rec + 1);
   const int parts = x.x, first = x.y, head0 = x.z, heads = x.w, q0 = y.x, nq = y.y, nk = y.z, prefix = y.w;
   if (parts <= 0) return;
-#ifdef SEQ_TUNE
-  JT(1, (float)parts);
-#endif
   constexpr int AHEAD = 4, HALVES = WIDE ? 2 : 1, COLS = 4 * HALVES;
   __shared__ float met_s[SEQ_JOIN_WARPS][COLS + 2][32];
   const int ways = parts > AHEAD ? SEQ_JOIN_WARPS : 1, mine = ways == 1 ? 0 : warp, rows = SEQ_JOIN_WARPS / ways;      // warps of a row; rows at once
@@ -886,10 +836,6 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
           if (part < parts && 4 * lane + 128 * h < hdc) o[u][h] = __ldcg(reinterpret_cast<const float4*>(p + 4 * lane + 128 * h));
         }
       }
-#ifdef SEQ_TUNE
-      JT(k == mine ? 2 : 4, ml[0].x + ml[1].x + ml[2].x + ml[3].x);
-      JT(k == mine ? 3 : 5, o[0][0].x + o[1][0].x + o[2][0].x + o[3][0].x);
-#endif
       const float top = fmaxf(m, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x))), keep = m == -INFINITY ? 0.f : exp2_fast(m - top);
       l *= keep;
 #pragma unroll
@@ -929,9 +875,6 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
         for (int j = 0; j < COLS; ++j) acc[j] = fmaf(f, met_s[i][j][lane], acc[j]);
       }
     }
-#ifdef SEQ_TUNE
-    JT(6, l);
-#endif
     const float inv = l == 0.f ? (seq_seen(nk - nq + token, nk, prefix, a.causal, a.window).hi > 0 ? NAN : 0.f) : 1.0f / l;
     unsigned short* const out = a.out + (int64_t)(q0 + token) * a.ld_out + (head0 + hh) * a.hd;
 #pragma unroll
@@ -939,9 +882,6 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
       if (4 * lane + 128 * h < a.hd)
         *reinterpret_cast<uint2*>(out + 4 * lane + 128 * h) = make_uint2(pack_bf16(acc[4 * h] * inv, acc[4 * h + 1] * inv), pack_bf16(acc[4 * h + 2] * inv, acc[4 * h + 3] * inv));
   }
-#ifdef SEQ_TUNE
-  if (threadIdx.x == 0 && blockIdx.y == 0) g_gt[jb][2] = gtimer();
-#endif
 }
 
 }  // namespace vla

@@ -69,11 +69,7 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   a.scale_log2 = x.scale * 1.44269504f;
   a.capped = x.cap > 0.f ? 1 : 0;
   a.cap_in = a.capped ? x.scale / x.cap : 0.f; a.cap_log2 = x.cap * 1.44269504f;
-#ifdef SEQ_TUNE
-  const int mode = getenv("SEQ_MODE") && a.hd <= 128 ? atoi(getenv("SEQ_MODE")) : seq_mode(a.tq, a.seqs, f.fold, a.hd), bn
-#else
   const int mode = seq_mode(a.tq, a.seqs, f.fold, a.hd), bn
-#endif
    = seq_bn(mode), nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
   // (blocks of one head of all sequences, at most, counted in 32 bits)
   const int64_t tokens = tiles * f.tokens, keys = a.offsets_k ? a.tk : (int64_t)a.max_pages * a.page_size;
@@ -100,9 +96,6 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
                                                                : (extra ? vla_op_sequences_kernel<SEQ_WIDE, true> : vla_op_sequences_kernel<SEQ_WIDE, false>));
   const int rc = op_launch(kernel, shares, seq_threads(mode), seq_smem(mode), 1, s, a, maps, op_fault());
   if (rc != VLA_OK) return rc;
-#ifdef SEQ_TUNE
-  if (getenv("SEQ_NOJOIN")) return rc;
-#endif
   // Rows that an item can have: those of its tiles, and those of all tokens; a warp each, or some one after another beyond sixteen blocks an SM.
   const int64_t rows = (int64_t)a.tq * a.fold;
   const int most = rows < seq_item_rows(mode) ? (int)rows : seq_item_rows(mode), blocks = seq_min(most, 16 * dev.sms / shares);
@@ -112,11 +105,6 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
 }  // namespace vla
 
 extern "C" {
-#ifdef SEQ_TUNE
-int vla_tune_gt(long long* out) { return cudaMemcpyFromSymbol(out, vla::g_gt, sizeof(long long) * 4096 * 4); }
-int vla_tune_j(long long* out) { return cudaMemcpyFromSymbol(out, vla::g_j, sizeof(long long) * 320 * 16); }
-int vla_tune_times(long long* out) { return cudaMemcpyFromSymbol(out, vla::g_tune, sizeof(long long) * 320 * 64); }
-#endif
 
 int vla_op_attention_sequences_scratch_bytes(int32_t hd, size_t* out_bytes) {
   if (!out_bytes || hd < 8 || hd > 256 || hd % 8) return VLA_ERR_INVALID;
