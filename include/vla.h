@@ -345,7 +345,7 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
  * offsets_k int32 [seqs + 1], prefix int32 [seqs], slopes fp32 [hq], all DEVICE and read by the kernel.  Offsets ascend; what lies outside of 0 .. tq (tk)
  * counts as the nearer end.  Rows of no sequence are not written.  Keys that a row does not see have no part in it, whatever their values.
  * A call's rows x keys are limited: (tq / 128 * hq / hkv + seqs) x tk / 64 stays below 2^31, about (a cache: max_pages * page_size for tk).
- * out overlaps no input.  scratch: DEVICE, 256-byte aligned, vla_op_attention_sequences_scratch_bytes(hd) or more; its first word is the call's
+ * out overlaps no input and scratch neither.  scratch: DEVICE, 256-byte aligned, vla_op_attention_sequences_scratch_bytes(hd) or more; its first word is the call's
  * error word, its contents matter to nobody afterwards, and calls that share it must not overlap on the GPU (two captured graphs among them). */
 int vla_op_attention_sequences_scratch_bytes(int32_t hd, size_t* out_bytes);
 typedef struct vla_attention_args {

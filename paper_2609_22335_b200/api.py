@@ -578,23 +578,28 @@ def _blocks(name, a, scale_a, w, scale_w, offsets, out, act, out_bf16, stream):
 def op_linear_bias(a, w, bias=None, residual=None, act=0, out_bf16=False, out=None, stream=None):
     """a [m,k], w [n,k]: CUDA bf16, contiguous; bias fp32 [n]; residual bf16 or fp32 [m,n], rows may lie apart.  Returns act(a w^T + bias) + residual as
     fp32 (or bf16) [m,n], in ``out`` where it is given, which may be the residual itself (see vla_op_linear_bias)."""
-    import torch
-    name, bf16 = "op_linear_bias", torch.bfloat16
-    if a.dtype != bf16 or w.dtype != bf16 or a.dim() != 2 or w.dim() != 2 or _elsewhere(a, w, bias, residual, out):
+    if _bf16 is None:
+        _look_up_types()
+    name, sa, sw, dev = "op_linear_bias", a.shape, w.shape, a.get_device()
+    elsewhere = dev < 0 or dev != _device_now() or w.get_device() != dev
+    for t in (bias, residual, out):
+        if t is not None and t.get_device() != dev:
+            elsewhere = True
+    if elsewhere or a.dtype != _bf16 or w.dtype != _bf16 or len(sa) != 2 or len(sw) != 2:
         _refuse(name, "a [m,k] and w [n,k] are bf16 on the current CUDA device, like all else")
-    m, k = a.shape
-    n = w.shape[0]
-    if w.shape[1] != k or not a.is_contiguous() or not w.is_contiguous() or (m | n | k) >> 31:
+    m, k = sa
+    n = sw[0]
+    if sw[1] != k or not a.is_contiguous() or not w.is_contiguous() or (m | n | k) >> 31:
         _refuse(name, "a and w are contiguous, rows of the same k, all sizes below 2^31")
-    if bias is not None and (bias.shape != (n,) or bias.dtype != torch.float32 or not bias.is_contiguous()):
+    if bias is not None and (bias.shape != (n,) or bias.dtype != _f32 or not bias.is_contiguous()):
         _refuse(name, "bias is contiguous fp32, [n]")
     f32, ld, res = False, 0, None
     if residual is not None:
-        f32 = residual.dtype == torch.float32
-        if not (f32 or residual.dtype == bf16) or residual.shape != (m, n) or (n > 1 and residual.stride(1) != 1):
+        f32 = residual.dtype == _f32
+        if not (f32 or residual.dtype == _bf16) or residual.shape != (m, n) or (n > 1 and residual.stride(1) != 1):
             _refuse(name, "residual is bf16 or fp32 [m,n], rows in one piece")
         ld, res = residual.stride(0) if m > 1 else n, residual.data_ptr()
-    result = bf16 if out_bf16 else torch.float32
+    result = _bf16 if out_bf16 else _f32
     if out is None:
         out = _new(stream, (m, n), result, a)
     elif out.shape != (m, n) or out.dtype != result or not out.is_contiguous():
@@ -701,19 +706,33 @@ def op_attention_sequences_scratch_bytes(hd) -> int:
     return out.value
 
 
+_bf16 = _f32 = _i32 = _u8 = _device_now = None
+
+
+def _look_up_types():
+    """torch's types as names of this module.  (The calls below ask some twenty questions each, and a statement that imports takes as long as two of them.)"""
+    global _bf16, _f32, _i32, _u8, _device_now
+    import torch
+    _f32, _i32, _u8, _device_now, _bf16 = torch.float32, torch.int32, torch.uint8, torch._C._cuda_getDevice, torch.bfloat16
+
+
 def _offsets(name, offsets, others):
     """The number of sequences, with the devices of all tensors looked at."""
-    import torch
-    seqs = offsets.shape[0] - 1 if offsets.dim() == 1 else 0
-    if seqs < 1 or offsets.dtype != torch.int32 or not offsets.is_contiguous() or _elsewhere(offsets, *others):
+    if _bf16 is None:
+        _look_up_types()
+    shape, dev = offsets.shape, offsets.get_device()
+    bad = len(shape) != 1 or shape[0] < 2 or offsets.dtype != _i32 or not offsets.is_contiguous() or dev < 0 or dev != _device_now()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            bad = True
+    if bad:
         _refuse(name, "offsets is contiguous int32 [seqs + 1], on the current CUDA device like all else")
-    return seqs
+    return shape[0] - 1
 
 
 def _row_step(name, what, x, rows, width):
     """Elements from one row of x [rows, width] (bf16) to the next."""
-    import torch
-    if x.dtype != torch.bfloat16 or x.shape != (rows, width):
+    if x.dtype != _bf16 or x.shape != (rows, width):
         _refuse(name, what)
     ld, one = x.stride()
     if one != 1:
@@ -723,7 +742,6 @@ def _row_step(name, what, x, rows, width):
 
 def _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream):
     """What the two attentions below have in common: (tq, ld_q, out, ld_out, scratch, its bytes, pointers of prefix and slopes, scale)."""
-    import torch
     if q.dim() != 2 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8:
         _refuse(name, "q is a matrix; hd a multiple of 8, at most 256")
     tq, width = q.shape[0], hq * hd
@@ -732,20 +750,23 @@ def _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, s
     ld_q = _row_step(name, "q is bf16 [tq, hq*hd]", q, tq, width)
     p_prefix = p_slopes = 0
     if prefix is not None:
-        if prefix.shape != (seqs,) or prefix.dtype != torch.int32 or not prefix.is_contiguous():
+        if prefix.shape != (seqs,) or prefix.dtype != _i32 or not prefix.is_contiguous():
             _refuse(name, "prefix is contiguous int32, [seqs]")
         p_prefix = prefix.data_ptr()
     if slopes is not None:
-        if slopes.shape != (hq,) or slopes.dtype != torch.float32 or not slopes.is_contiguous():
+        if slopes.shape != (hq,) or slopes.dtype != _f32 or not slopes.is_contiguous():
             _refuse(name, "slopes is contiguous fp32, [hq]")
         p_slopes = slopes.data_ptr()
     if out is None:
-        out, ld_out = _new(stream, (tq, width), torch.bfloat16, q), width
+        out, ld_out = _new(stream, (tq, width), _bf16, q), width
     else:
         ld_out = _row_step(name, "out is bf16 [tq, hq*hd]", out, tq, width)
     if scratch is None:                                             # (goes back to its stream's memory when the call returns)
-        scratch, size = _scratch(stream, hd, q)
-    elif scratch.dtype != torch.uint8 or not scratch.is_contiguous():
+        size = _scratch_sizes.get(hd)
+        if size is None:
+            size = _scratch_sizes[hd] = op_attention_sequences_scratch_bytes(hd)
+        scratch = _new(stream, (size,), _u8, q)
+    elif scratch.dtype != _u8 or not scratch.is_contiguous():
         _refuse(name, "scratch is contiguous uint8")
     else:
         size = scratch.numel()
@@ -753,14 +774,6 @@ def _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, s
 
 
 _scratch_sizes = {}
-
-
-def _scratch(stream, hd, like):
-    import torch
-    size = _scratch_sizes.get(hd)
-    if size is None:
-        size = _scratch_sizes[hd] = op_attention_sequences_scratch_bytes(hd)
-    return _new(stream, (size,), torch.uint8, like), size
 
 
 _ATTENTION_ARGS = struct.Struct("=18Q11i2fi")                        # vla_attention_args
@@ -797,9 +810,8 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
 
 def _cache(name, k_cache, v_cache, pages, lengths, seqs, width):
     """Sizes and strides of a cache's two tensors: (n_pages, page_size, max_pages, row_k, page_k, row_v, page_v)."""
-    import torch
-    shape, bf16, i32 = k_cache.shape, torch.bfloat16, torch.int32
-    if len(shape) != 3 or shape[2] != width or v_cache.shape != shape or k_cache.dtype != bf16 or v_cache.dtype != bf16:
+    shape = k_cache.shape
+    if len(shape) != 3 or shape[2] != width or v_cache.shape != shape or k_cache.dtype != _bf16 or v_cache.dtype != _bf16:
         _refuse(name, "k_cache and v_cache are bf16 [n_pages, page_size, hkv*hd]")
     n, size, _ = shape
     (page_k, row_k, one_k), (page_v, row_v, one_v) = k_cache.stride(), v_cache.stride()
@@ -809,9 +821,10 @@ def _cache(name, k_cache, v_cache, pages, lengths, seqs, width):
         row_k = row_v = width
     if n == 1:
         page_k, page_v = size * row_k, size * row_v
-    if pages.dim() != 2 or pages.dtype != i32 or not pages.is_contiguous() or lengths.shape != (seqs,) or lengths.dtype != i32 or not lengths.is_contiguous():
+    table = pages.shape
+    if len(table) != 2 or pages.dtype != _i32 or not pages.is_contiguous() or lengths.shape != (seqs,) or lengths.dtype != _i32 or not lengths.is_contiguous():
         _refuse(name, "pages [seqs, max_pages] and lengths [seqs] are contiguous int32")
-    rows, most = pages.shape
+    rows, most = table
     if rows != seqs or most < 1 or most >> 31:
         _refuse(name, "pages has a row of at least one entry for each sequence")
     return n, size, most, row_k, page_k, row_v, page_v

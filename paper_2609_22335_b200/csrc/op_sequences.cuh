@@ -803,7 +803,9 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
   const int share = (int)blockIdx.x, warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, hdc = seq_cols(a.hd), stride = seq_row_floats(a.hd);
   const int4* const rec = reinterpret_cast<const int4*>(a.scratch + SEQ_HEADER + share * SEQ_RECORD);
   const int4 x = __ldcg(rec), y = __ldcg(rec + 1);
-  const int parts = x.x, first = x.y, head0 = x.z, heads = x.w, q0 = y.x, nq = y.y, nk = y.z, prefix = y.w;
+  // (A scratch that another call writes meanwhile gives wrong results and no access outside of it or of the output.)
+  const int parts = min(x.x, (int)gridDim.x - share), first = max(x.y, 0), head0 = min(max(x.z, 0), a.hq), heads = min(x.w, a.hq - head0), q0 = max(y.x, 0), nq = min(y.y, a.tq - q0), nk = y.z,
+            prefix = y.w;
   if (parts <= 0) return;
   constexpr int AHEAD = 4, HALVES = WIDE ? 2 : 1, COLS = 4 * HALVES;
   __shared__ float met_s[SEQ_JOIN_WARPS][COLS + 2][32];
