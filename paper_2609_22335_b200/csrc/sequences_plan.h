@@ -93,9 +93,11 @@ inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
 // Shapes of the kernel.  Two: two tiles of 128 rows that share their blocks of 128 keys, an SM to a CTA (long sequences).  One: a tile, blocks of 64 keys, two
 // CTAs an SM.  Wide: the same for heads wider than 128, an SM to a CTA.
 enum { SEQ_TWO = 0, SEQ_ONE = 1, SEQ_WIDE = 2 };
+// Two tiles pay where sequences have many rows, on average: 8 x 1024 rows (12 heads of 64) 60 us for 69, 8192 rows (16 of 128) 472 for 525; 3 x 817 (16 of 72) 46 for 43,
+// 32 x 256 (16 of 128) 43 for 41.
 inline int seq_mode(int64_t tq, int seqs, int fold, int hd) {
   if (hd > 128) return SEQ_WIDE;
-  return tq * fold > (int64_t)seqs * 160 ? SEQ_TWO : SEQ_ONE;
+  return tq * fold > (int64_t)seqs * 900 ? SEQ_TWO : SEQ_ONE;
 }
 SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
 // What an item takes beside its blocks, in blocks: its first loads, the last block's chain, the result.

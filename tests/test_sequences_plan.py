@@ -89,7 +89,7 @@ def test_parts_fit_the_scratch_memory_and_tiles_the_sms(lib):
         for sms in (1, 74, 132, 148, 160, 400):
             for mode in ((2,) if hd > 128 else (0, 1)):
                 assert lib.seq_parts_end_host(mode, hd, sms) <= lib.seq_scratch_host(hd)
-        for tq, seqs in ((1, 1), (160, 1), (161, 1), (10000, 7), (64, 64)):
+        for tq, seqs in ((1, 1), (900, 1), (901, 1), (10000, 7), (64, 64)):
             mode = lib.seq_mode_host(tq, seqs, 1, hd)
             assert (mode == 2) == (hd > 128)
             nbox, bn = (hd + 63) // 64, lib.seq_bn_host(mode)
