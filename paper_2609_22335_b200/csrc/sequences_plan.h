@@ -100,7 +100,7 @@ inline int seq_mode(int64_t tq, int seqs, int fold, int hd) {
   return tq * fold > (int64_t)seqs * 900 ? SEQ_TWO : SEQ_ONE;
 }
 SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
-// What an item takes beside its blocks, in blocks: its first loads, the last block's chain, the result.
+// What an item takes beside its blocks, in blocks: its first scores, the last block's chain, the result (6000 cycles beside 3250 to 3850 a block with two tiles, 3200 beside 1100).
 SEQ_HD constexpr int seq_item_ticks(int mode) { return mode == SEQ_TWO ? 2 : 3; }
 SEQ_HD constexpr int seq_join_ticks(int mode) { return mode == SEQ_TWO ? 5 : 6; }
 SEQ_HD int seq_item_rows(int mode) { return mode == SEQ_TWO ? 2 * SEQ_ROWS : SEQ_ROWS; }
