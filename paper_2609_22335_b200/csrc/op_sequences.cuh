@@ -5,7 +5,7 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax.  A tile is 128 rows: the query heads that share a key head side by side,
 // then the next token, so that a key block serves all of them and ragged ends cost little.  Scores and result are tensor-core accumulators (tensor
-// memory), a row a lane; softmax threads own a row each and leave the probabilities, as bf16, in the scores' place, from where the second product
+// memory), a row a lane; softmax threads own a row each and leave the probabilities, as bf16 (one number, or two that add up), in the scores' place, from where the second product
 // takes them.  The running maximum may lag the true one by 2^8, so the result is rescaled on few blocks only.
 //
 // Shares of key blocks (sequences_plan.h) are dealt out evenly, lengths being read on the GPU: a call of one long sequence splits its keys over the
@@ -310,17 +310,16 @@ __device__ __forceinline__ void pair_to(uint32_t* v, uint64_t x) {
   unpack2(x, a, b);
   v[0] = __float_as_uint(a); v[1] = __float_as_uint(b);
 }
-// One block of a row's online softmax: BN scores in, BN / 2 pairs of bf16 probabilities out (front half of the registers).
-// `known`: the scores' largest absolute value, where the caller has it and they lie close together (else below 0): as good a reference as their maximum.
-template <int BN>
-__device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float known, float& m_run, float& l_run, float& alpha) {
-  float mx = fmaxf(m_run, known);
-  if (known < 0.f) {
-    float m4[4] = {m_run, __uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2])};
+// One block of a row's online softmax: BN scores in, BN / 2 pairs of bf16 probabilities out (front half of the registers).  TERMS 2: the pairs' rounding errors, in
+// bf16 themselves, in the other half.
+// (Relative to the maximum itself the largest probability is 1, which rounds to itself: a row of one key is that key's value, exactly.  The scores' largest absolute
+// value, which capped scores need anyway, in its place: 4 % less time, and rows of few keys that were 1.5 times as far from the exact result.)
+template <int BN, int TERMS>
+__device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float& m_run, float& l_run, float& alpha) {
+  float m4[4] = {m_run, __uint_as_float(sr[0]), __uint_as_float(sr[1]), __uint_as_float(sr[2])};
 #pragma unroll
-    for (int j = 3; j < BN - 1; j += 2) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
-    mx = fmaxf(max3(m4[0], m4[1], m4[2]), fmaxf(m4[3], __uint_as_float(sr[BN - 1])));
-  }
+  for (int j = 3; j < BN - 1; j += 2) m4[(j >> 1) & 3] = max3(m4[(j >> 1) & 3], __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
+  float mx = fmaxf(max3(m4[0], m4[1], m4[2]), fmaxf(m4[3], __uint_as_float(sr[BN - 1])));
   alpha = 1.0f;
   if (m_run != -INFINITY) {
     if ((mx - m_run) * sl2 <= ATTN_RESCALE_LOG2) mx = m_run;
@@ -329,6 +328,7 @@ __device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float known
   const float mb = mx == -INFINITY ? 0.f : -mx * sl2;
   const uint64_t sl2_2 = pack2(sl2, sl2), mb_2 = pack2(mb, mb);
   uint64_t s2[2] = {0ull, 0ull};
+  uint32_t low[TERMS == 2 ? BN / 2 : 1];
 #pragma unroll
   for (int j = 0; j < BN; j += 2) {
     float p0, p1;
@@ -336,6 +336,11 @@ __device__ __forceinline__ void seq_softmax(uint32_t* sr, float sl2, float known
     p0 = exp2_fast(p0); p1 = exp2_fast(p1);
     s2[(j >> 1) & 1] = add2(s2[(j >> 1) & 1], pack2(p0, p1));
     sr[j >> 1] = pack_bf16(p0, p1);
+    if (TERMS == 2) low[j >> 1] = pack_bf16(p0 - __uint_as_float(sr[j >> 1] << 16), p1 - __uint_as_float(sr[j >> 1] & 0xFFFF0000u));
+  }
+  if (TERMS == 2) {
+#pragma unroll
+    for (int j = 0; j < BN / 2; ++j) sr[BN / 2 + j] = low[j];
   }
   float x0, x1;
   unpack2(add2(s2[0], s2[1]), x0, x1);
@@ -363,8 +368,8 @@ __device__ __forceinline__ float* seq_part(const SeqArgs& a, int mode, int share
 }
 
 constexpr int seq_threads(int mode) { return mode == SEQ_TWO ? 384 : 192; }
-// EXTRA: scores are capped or have a bias by distance.
-template <int MODE, bool EXTRA>
+// EXTRA: scores are capped or have a bias by distance.  TERMS: bf16 numbers of a probability (seq_terms).
+template <int MODE, bool EXTRA, int TERMS>
 __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vla_op_sequences_kernel(const __grid_constant__ SeqArgs a, const __grid_constant__ SeqMaps maps, OpFault fault) {
   constexpr bool TWO = MODE == SEQ_TWO;
   constexpr int W = seq_item_ticks(MODE);
@@ -507,7 +512,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         const uint64_t vd = umma_desc_mn_sw128(ring + stage * stage_bytes, BN * 128);
         const uint32_t tp = tmem + (uint32_t)(BN * slot);
 #pragma unroll
-        for (int k = 0; k < BN / 16; ++k) umma_bf16_ta(to, tp + 8u * k, vd + (uint64_t)(k * (16 * 128 >> 4)), idesc_o, first && k == 0 ? 0u : 1u);
+        for (int k = 0; k < TERMS * (BN / 16); ++k) umma_bf16_ta(to, tp + 8u * k, vd + (uint64_t)(k % (BN / 16) * (16 * 128 >> 4)), idesc_o, first && k == 0 ? 0u : 1u);
       };
       for (; ok; ++items) {
         if (!(ok = mbar_wait(c, q_full, items & 1u))) break;
@@ -598,6 +603,16 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     bool ok = true;
     uint32_t ns[2] = {0, 0}, ring0 = 0, items = 0;      // blocks of a tile of scores, ring places and items so far
+    // Rows of V behind the last key (of other sequences, or what a page held before) may be anything, and 0 x inf is NaN: they become zeros.
+    auto zero_tail = [&](const SeqItem& w, int i, int n, int c0) {
+      const uint32_t place = ring0 + (uint32_t)(TWO ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1)), stage = place % (uint32_t)NS;
+      if (ok) ok = mbar_wait(c, full + 8u * stage, place / (uint32_t)NS & 1u);
+      const int from = max(w.nk - c0, 0);
+      char* const v0 = smem_dyn + (ring + stage * stage_bytes - smem_u32(smem_dyn));
+      for (int x = from * 8 + row; x < BN * 8; x += 128)
+        for (int b = 0; b < nbox; ++b) *reinterpret_cast<uint4*>(v0 + b * (BN * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    };
     for (; ok; ++items) {
       if (!(ok = mbar_wait(c, q_full, items & 1u))) break;
       __syncwarp();
@@ -618,11 +633,17 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         if (ok) ok = mbar_wait(c, s_full + 8u * slot, ns[slot] & 1u);
         __syncwarp();
         tc_fence_after();
+        if (!TWO && !__any_sync(0xffffffffu, valid)) {      // nobody's rows, as most warps' of a single token's tile: whatever lies there will do for probabilities
+          if (w.nk - c0 < BN) zero_tail(w, i, n, c0);
+          arrive_warp(p_full + 8u * slot, lane);
+          ++ns[slot];
+          continue;
+        }
         uint32_t sr[BN];
 #pragma unroll
         for (int k = 0; k < BN; k += 32) tmem_ld32_nowait(ts + k, sr + k);
         tmem_ld_wait();
-        float sl2 = a.scale_log2, known = -1.0f;
+        float sl2 = a.scale_log2;
         if (EXTRA) {
           const float d = (float)(p - c0);
           sl2 = a.capped ? a.cap_log2 : a.scale_log2;                  // what makes log2 units of the scores in the registers
@@ -648,8 +669,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
                 y = fma2(y, z, pack2(-3.333306908607483e-01f, -3.333306908607483e-01f));
                 pair_to(sr + j, mul2(fma2(y, z, pack2(1.0f, 1.0f)), x));
               }
-              // All scores lie within half the cap of 0, 46 powers of e at a cap of 50: nobody need look for the maximum.
-              if (a.cap_log2 <= 100.0f) known = top * a.cap_in;
             }
           }
           if (a.slopes) {
@@ -663,7 +682,6 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
               for (int j = 0; j < BN; ++j) sr[j] = __float_as_uint(fmaf(-slope, fabsf(d - (float)j), __uint_as_float(sr[j]) * sl2));
             }
             sl2 = 1.0f;
-            known = -1.0f;
           }
         }
         if (__any_sync(0xffffffffu, c0 + BN > seen.hi || (c0 < seen.lo && c0 + BN > w.prefix))) {
@@ -676,25 +694,16 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
           }
         }
         float alpha;
-        seq_softmax<BN>(sr, sl2, known, m_run, l_run, alpha);
+        seq_softmax<BN, TERMS>(sr, sl2, m_run, l_run, alpha);
         if (i > 0 && __any_sync(0xffffffffu, valid && alpha != 1.0f)) {      // (rows that nobody stores may be NaN)
           if (!TWO && ok) ok = mbar_wait(c, o_done + 8u * ((i - 1) & 1), (ns[(i - 1) & 1] - 1) & 1u);
           __syncwarp();
           tc_fence_after();
           attn_rescale(tmem_o + lanes + (TWO ? 128u * t : 0u), hdc, alpha);
         }
-        // Rows of V behind the last key (of other sequences, or what a page held before) may be anything, and 0 x inf is NaN: they become zeros.
-        if ((TWO ? t == 0 : true) && w.nk - c0 < BN) {
-          const uint32_t place = ring0 + (uint32_t)(TWO ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1)), stage = place % (uint32_t)NS;
-          if (ok) ok = mbar_wait(c, full + 8u * stage, place / (uint32_t)NS & 1u);
-          const int from = max(w.nk - c0, 0);
-          char* const v0 = smem_dyn + (ring + stage * stage_bytes - smem_u32(smem_dyn));
-          for (int x = from * 8 + row; x < BN * 8; x += 128)
-            for (int b = 0; b < nbox; ++b) *reinterpret_cast<uint4*>(v0 + b * (BN * 128) + x * 16) = make_uint4(0, 0, 0, 0);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
+        if ((TWO ? t == 0 : true) && w.nk - c0 < BN) zero_tail(w, i, n, c0);
 #pragma unroll
-        for (int k = 0; k < BN / 2; k += 16) tmem_st16u(ts + k, sr + k);
+        for (int k = 0; k < TERMS * BN / 2; k += 16) tmem_st16u(ts + k, sr + k);
         tmem_st_wait();
         tc_fence_before();
         arrive_warp(p_full + 8u * slot, lane);

@@ -15,9 +15,11 @@ static bool seq_look_up(int dev, SeqDevice* d) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, seq_smem(mode)) == cudaSuccess && cudaFuncGetAttributes(&fa, kernel) == cudaSuccess &&
            (mode != SEQ_TWO || fa.numRegs * 384 >= 128 * SEQ_REGS_SERVICE + 256 * SEQ_REGS_SOFTMAX);
   };
-  return ready(vla_op_sequences_kernel<SEQ_TWO, false>, SEQ_TWO) && ready(vla_op_sequences_kernel<SEQ_TWO, true>, SEQ_TWO) &&
-         ready(vla_op_sequences_kernel<SEQ_ONE, false>, SEQ_ONE) && ready(vla_op_sequences_kernel<SEQ_ONE, true>, SEQ_ONE) &&
-         ready(vla_op_sequences_kernel<SEQ_WIDE, false>, SEQ_WIDE) && ready(vla_op_sequences_kernel<SEQ_WIDE, true>, SEQ_WIDE);
+  return ready(vla_op_sequences_kernel<SEQ_TWO, false, 1>, SEQ_TWO) && ready(vla_op_sequences_kernel<SEQ_TWO, true, 1>, SEQ_TWO) &&
+         ready(vla_op_sequences_kernel<SEQ_ONE, false, 1>, SEQ_ONE) && ready(vla_op_sequences_kernel<SEQ_ONE, true, 1>, SEQ_ONE) &&
+         ready(vla_op_sequences_kernel<SEQ_ONE, false, 2>, SEQ_ONE) && ready(vla_op_sequences_kernel<SEQ_ONE, true, 2>, SEQ_ONE) &&
+         ready(vla_op_sequences_kernel<SEQ_WIDE, false, 1>, SEQ_WIDE) && ready(vla_op_sequences_kernel<SEQ_WIDE, true, 1>, SEQ_WIDE) &&
+         ready(vla_op_sequences_kernel<SEQ_WIDE, false, 2>, SEQ_WIDE) && ready(vla_op_sequences_kernel<SEQ_WIDE, true, 2>, SEQ_WIDE);
 }
 static bool seq_device(SeqDevice* d) {
   static PerDevice<SeqDevice> devices;
@@ -69,7 +71,7 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   a.scale_log2 = x.scale * 1.44269504f;
   a.capped = x.cap > 0.f ? 1 : 0;
   a.cap_in = a.capped ? x.scale / x.cap : 0.f; a.cap_log2 = x.cap * 1.44269504f;
-  const int mode = seq_mode(a.tq, a.seqs, f.fold, a.hd), bn
+  const int mode = seq_mode(a.tq, a.seqs, a.hq, f.fold, a.hd), bn
    = seq_bn(mode), nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
   // (blocks of one head of all sequences, at most, counted in 32 bits)
   const int64_t tokens = tiles * f.tokens, keys = a.offsets_k ? a.tk : (int64_t)a.max_pages * a.page_size;
@@ -91,9 +93,13 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   const int kb[4] = {64, 1, a.chunk, 1};
   if (!seq_encode(&maps.m[0], a.q, 3, qd, qs, qb) || !seq_encode(&maps.m[1], a.k, 4, kd, ks, kb) || !seq_encode(&maps.m[2], a.v, 4, kd, vs, kb)) return VLA_ERR_CUDA;
   const bool extra = a.capped || a.slopes;
-  const auto kernel = mode == SEQ_TWO ? (extra ? vla_op_sequences_kernel<SEQ_TWO, true> : vla_op_sequences_kernel<SEQ_TWO, false>)
-                                      : (mode == SEQ_ONE ? (extra ? vla_op_sequences_kernel<SEQ_ONE, true> : vla_op_sequences_kernel<SEQ_ONE, false>)
-                                                               : (extra ? vla_op_sequences_kernel<SEQ_WIDE, true> : vla_op_sequences_kernel<SEQ_WIDE, false>));
+  const auto pick = [extra](auto* plain, auto* with) { return extra ? with : plain; };
+  const bool two = seq_terms(a.tq, a.hq) == 2;
+  const auto kernel = mode == SEQ_TWO   ? pick(vla_op_sequences_kernel<SEQ_TWO, false, 1>, vla_op_sequences_kernel<SEQ_TWO, true, 1>)
+                      : mode == SEQ_ONE ? (two ? pick(vla_op_sequences_kernel<SEQ_ONE, false, 2>, vla_op_sequences_kernel<SEQ_ONE, true, 2>)
+                                               : pick(vla_op_sequences_kernel<SEQ_ONE, false, 1>, vla_op_sequences_kernel<SEQ_ONE, true, 1>))
+                                        : (two ? pick(vla_op_sequences_kernel<SEQ_WIDE, false, 2>, vla_op_sequences_kernel<SEQ_WIDE, true, 2>)
+                                               : pick(vla_op_sequences_kernel<SEQ_WIDE, false, 1>, vla_op_sequences_kernel<SEQ_WIDE, true, 1>));
   const int rc = op_launch(kernel, shares, seq_threads(mode), seq_smem(mode), 1, s, a, maps, op_fault());
   if (rc != VLA_OK) return rc;
   // Rows that an item can have: those of its tiles, and those of all tokens; a warp each, or some one after another beyond sixteen blocks an SM.

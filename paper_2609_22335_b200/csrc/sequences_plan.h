@@ -90,14 +90,18 @@ inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
   *shift = 31 + l;
 }
 
+// bf16 numbers that a probability is given in for the second product.  One puts an error beside the result's own rounding that is as large, on average over many rows: 1.41 times the
+// rounding in all.  Of few rows (tokens x heads) it may be more, 1.6 times over 8 rows of which each has a few keys that count; those calls wait for memory or for themselves, and
+// take two numbers: 1.00 to 1.02 times, at 12.4 us as before (one token, 1500 keys) and 223 for 215 (64 tokens over 1.3 GB).
+inline int seq_terms(int64_t tq, int hq) { return tq * hq <= 4096 ? 2 : 1; }
 // Shapes of the kernel.  Two: two tiles of 128 rows that share their blocks of 128 keys, an SM to a CTA (long sequences).  One: a tile, blocks of 64 keys, two
 // CTAs an SM.  Wide: the same for heads wider than 128, an SM to a CTA.
 enum { SEQ_TWO = 0, SEQ_ONE = 1, SEQ_WIDE = 2 };
 // Two tiles pay where sequences have many rows, on average: 8 x 1024 rows (12 heads of 64) 60 us for 69, 8192 rows (16 of 128) 472 for 525; 3 x 817 (16 of 72) 46 for 43,
 // 32 x 256 (16 of 128) 43 for 41.
-inline int seq_mode(int64_t tq, int seqs, int fold, int hd) {
+inline int seq_mode(int64_t tq, int seqs, int hq, int fold, int hd) {
   if (hd > 128) return SEQ_WIDE;
-  return tq * fold > (int64_t)seqs * 900 ? SEQ_TWO : SEQ_ONE;
+  return tq * fold > (int64_t)seqs * 900 && seq_terms(tq, hq) == 1 ? SEQ_TWO : SEQ_ONE;
 }
 SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
 // What an item takes beside its blocks, in blocks: its first scores, the last block's chain, the result (6000 cycles beside 3250 to 3850 a block with two tiles, 3200 beside 1100).

@@ -28,7 +28,7 @@ int64_t seq_scratch_host(int hd) { return vla::seq_scratch_bytes(hd); }
 int64_t seq_parts_end_host(int mode, int hd, int sms) {
   return vla::SEQ_HEADER + (int64_t)vla::SEQ_MAX_SHARES * vla::SEQ_RECORD + 2 * (int64_t)vla::seq_shares(mode, sms) * vla::seq_part_floats(mode, hd) * 4;
 }
-int seq_mode_host(int64_t tq, int seqs, int fold, int hd) { return vla::seq_mode(tq, seqs, fold, hd); }
+int seq_mode_host(int64_t tq, int seqs, int hq, int fold, int hd) { return vla::seq_mode(tq, seqs, hq, fold, hd); }
 int seq_smem_host(int mode) { return vla::seq_smem(mode); }
 int seq_ticks_host(int mode) { return vla::seq_item_ticks(mode); }
 int seq_bn_host(int mode) { return vla::seq_bn(mode); }

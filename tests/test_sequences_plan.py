@@ -21,7 +21,7 @@ def lib(tmp_path_factory):
     lib.seq_shares_host.argtypes = [C.c_int64, C.c_int]
     lib.seq_owner_host.argtypes = [C.c_int64, C.c_int, C.c_int64]
     lib.seq_quotient_host.argtypes, lib.seq_quotient_host.restype = [C.c_int, C.c_uint32], C.c_uint32
-    lib.seq_mode_host.argtypes = [C.c_int64, C.c_int, C.c_int, C.c_int]
+    lib.seq_mode_host.argtypes = [C.c_int64] + [C.c_int] * 4
     lib.seq_whole_host.argtypes = [C.c_int64, C.c_int, C.c_int64, C.c_int, C.c_int]
     return lib
 
@@ -90,7 +90,7 @@ def test_parts_fit_the_scratch_memory_and_tiles_the_sms(lib):
             for mode in ((2,) if hd > 128 else (0, 1)):
                 assert lib.seq_parts_end_host(mode, hd, sms) <= lib.seq_scratch_host(hd)
         for tq, seqs in ((1, 1), (900, 1), (901, 1), (10000, 7), (64, 64)):
-            mode = lib.seq_mode_host(tq, seqs, 1, hd)
+            mode = lib.seq_mode_host(tq, seqs, 16, 1, hd)
             assert (mode == 2) == (hd > 128)
             nbox, bn = (hd + 63) // 64, lib.seq_bn_host(mode)
             stages = (lib.seq_smem_host(mode) - 1024 - (2 if mode == 0 else 1) * nbox * 128 * 128) // (nbox * bn * 128)
