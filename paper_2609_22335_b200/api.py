@@ -706,14 +706,14 @@ def op_attention_sequences_scratch_bytes(hd) -> int:
     return out.value
 
 
-_bf16 = _f32 = _i32 = _u8 = _device_now = None
+_bf16 = _f32 = _i32 = _u8 = _device_now = _empty_like = None
 
 
 def _look_up_types():
     """torch's types as names of this module.  (The calls below ask some twenty questions each, and a statement that imports takes as long as two of them.)"""
-    global _bf16, _f32, _i32, _u8, _device_now
+    global _bf16, _f32, _i32, _u8, _device_now, _empty_like
     import torch
-    _f32, _i32, _u8, _device_now, _bf16 = torch.float32, torch.int32, torch.uint8, torch._C._cuda_getDevice, torch.bfloat16
+    _f32, _i32, _u8, _device_now, _empty_like, _bf16 = torch.float32, torch.int32, torch.uint8, torch._C._cuda_getDevice, torch.empty_like, torch.bfloat16
 
 
 def _offsets(name, offsets, others):
@@ -740,8 +740,9 @@ def _row_step(name, what, x, rows, width):
     return ld if rows > 1 else width                                # (the stride of one row says nothing)
 
 
-def _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream):
-    """What the two attentions below have in common: (tq, ld_q, out, ld_out, scratch, its bytes, pointers of prefix and slopes, scale)."""
+def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream):
+    """What the two attentions below have in common, ``keys`` being the most that a sequence may have: (tq, ld_q, out, ld_out, scratch, its pointer and bytes, pointers of
+    prefix and slopes, scale)."""
     if q.dim() != 2 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8:
         _refuse(name, "q is a matrix; hd a multiple of 8, at most 256")
     tq, width = q.shape[0], hq * hd
@@ -758,19 +759,22 @@ def _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, s
             _refuse(name, "slopes is contiguous fp32, [hq]")
         p_slopes = slopes.data_ptr()
     if out is None:
-        out, ld_out = _new(stream, (tq, width), _bf16, q), width
+        out, ld_out = _empty_like(q) if stream is None else _new(stream, (tq, width), _bf16, q), width      # (contiguous, whatever lies between q's rows)
     else:
         ld_out = _row_step(name, "out is bf16 [tq, hq*hd]", out, tq, width)
-    if scratch is None:                                             # (goes back to its stream's memory when the call returns)
-        size = _scratch_sizes.get(hd)
-        if size is None:
-            size = _scratch_sizes[hd] = op_attention_sequences_scratch_bytes(hd)
-        scratch = _new(stream, (size,), _u8, q)
+    if scratch is None:
+        size = at = 0
+        if keys > 512:                                              # (shorter calls need none; goes back to its stream's memory when the call returns)
+            size = _scratch_sizes.get(hd)
+            if size is None:
+                size = _scratch_sizes[hd] = op_attention_sequences_scratch_bytes(hd)
+            scratch = _new(stream, (size,), _u8, q)
+            at = scratch.data_ptr()
     elif scratch.dtype != _u8 or not scratch.is_contiguous():
         _refuse(name, "scratch is contiguous uint8")
     else:
-        size = scratch.numel()
-    return tq, ld_q, out, ld_out, scratch, size, p_prefix, p_slopes, hd ** -0.5 if scale is None else scale
+        size, at = scratch.numel(), scratch.data_ptr()
+    return tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, hd ** -0.5 if scale is None else scale
 
 
 _scratch_sizes = {}
@@ -789,8 +793,8 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
     sequence has are left as they were in ``out`` (without one: undefined), rows that see no key are zeros (see vla_op_attention_packed)."""
     name = "op_attention_packed"
     seqs = _offsets(name, offsets, (q, k, v, offsets_k, prefix, slopes, out, scratch))
-    tq, ld_q, out, ld_out, scratch, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     tk = k.shape[0]
+    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, tk, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     if offsets_k is None:
         offsets_k = offsets
         if tk != tq:
@@ -801,7 +805,7 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
         _refuse(name, "k and v have at least one row, below 2^31 of them")
     ld_k, ld_v = _row_step(name, "k is bf16 [tk, hkv*hd]", k, tk, hkv * hd), _row_step(name, "v is bf16 [tk, hkv*hd]", v, tk, hkv * hd)
     args = _ATTENTION_ARGS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, 0, 0, offsets.data_ptr(), offsets_k.data_ptr(), 0, 0,
-                                p_prefix, p_slopes, scratch.data_ptr(), size, seqs, tq, tk, 0, 0, 0, hq, hkv, hd, 1 if causal else 0, window, scale, cap, 0)
+                                p_prefix, p_slopes, at, size, seqs, tq, tk, 0, 0, 0, hq, hkv, hd, 1 if causal else 0, window, scale, cap, 0)
     rc = (_lib or load_library()).vla_op_attention_packed(args, _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_attention_packed failed")
@@ -838,10 +842,10 @@ def op_attention_paged(q, k_cache, v_cache, pages, lengths, offsets, hq, hkv, hd
     sequence's length are not looked at (see vla_op_attention_paged)."""
     name = "op_attention_paged"
     seqs = _offsets(name, offsets, (q, k_cache, v_cache, pages, lengths, prefix, slopes, out, scratch))
-    tq, ld_q, out, ld_out, scratch, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     n, page, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, hkv * hd)
+    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, most * page, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     args = _ATTENTION_ARGS.pack(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), ld_q, row_k, row_v, ld_out, page_k, page_v, offsets.data_ptr(), 0,
-                                lengths.data_ptr(), pages.data_ptr(), p_prefix, p_slopes, scratch.data_ptr(), size, seqs, tq, 0, n, page, most, hq, hkv, hd, 1 if causal else 0,
+                                lengths.data_ptr(), pages.data_ptr(), p_prefix, p_slopes, at, size, seqs, tq, 0, n, page, most, hq, hkv, hd, 1 if causal else 0,
                                 window, scale, cap, 0)
     rc = (_lib or load_library()).vla_op_attention_paged(args, _stream_ptr(stream))
     if rc != VLA_OK:

@@ -34,7 +34,8 @@ struct SeqArgs {
   const float* slopes;
   const unsigned short *q, *k, *v;             // (read key by key where a row's result is not finite)
   unsigned short* out;
-  char* scratch;                               // header (error word), records, parts
+  char* scratch;                               // header (error word), records, parts; null where all items stay whole
+  unsigned* err;
   long long ld_q, ld_k, ld_v, page_k, page_v, ld_out;
   int seqs, tq, tk, n_pages, page_size, max_pages, chunk;      // chunk: rows of a box of keys, all of one page
   uint32_t page_magic, page_shift;             // x / page_size = x * page_magic >> page_shift for x below 2^31
@@ -386,7 +387,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
                  o_free = o_done + 16, q_full = o_free + 16, q_empty = q_full + 8;
   const uint32_t tile_bytes = (uint32_t)nbox * (SEQ_ROWS * 128), stage_bytes = (uint32_t)nbox * (BN * 128);
   const uint32_t Qs = (smem_u32(smem_dyn) + 1023u) & ~1023u, ring = Qs + (TWO ? 2u : 1u) * tile_bytes;
-  unsigned* const err = reinterpret_cast<unsigned*>(a.scratch);
+  unsigned* const err = a.err;
   SeqRecord* const record = reinterpret_cast<SeqRecord*>(a.scratch + SEQ_HEADER) + blockIdx.x * (SEQ_RECORD / sizeof(SeqRecord));
   if (warp == SOFT) {
     if (lane < 2 * SEQ_MAX_STAGES + 10) {
@@ -401,7 +402,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   if (threadIdx.x < 3) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[threadIdx.x]) : "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (threadIdx.x == 0) {
-    record->parts = 0;
+    if (a.scratch) record->parts = 0;
     if (blockIdx.x == 0) *err = 0u;
   }
   const OpWaits c = {&failed_s, fault.wait_limit};

@@ -7,9 +7,12 @@
 namespace vla {
 
 // What the kernels need to know of a device, looked up on the first call made with it current.
-struct SeqDevice { int sms = 0; };
+static __device__ __align__(256) unsigned g_sequences_error[16];      // of calls without scratch memory
+struct SeqDevice { int sms = 0; unsigned* error = nullptr; };
 static bool seq_look_up(int dev, SeqDevice* d) {
-  if (cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return false;
+  void* e = nullptr;
+  if (cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || cudaGetSymbolAddress(&e, g_sequences_error) != cudaSuccess || !e) return false;
+  d->error = static_cast<unsigned*>(e);
   const auto ready = [](auto* kernel, int mode) {      // (what the warpgroups that raise their registers ask for has to be there)
     cudaFuncAttributes fa;
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, seq_smem(mode)) == cudaSuccess && cudaFuncGetAttributes(&fa, kernel) == cudaSuccess &&
@@ -64,7 +67,6 @@ static SeqArgs seq_args(const vla_attention_args& x) {
 }
 
 static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
-  if (!x.scratch || (reinterpret_cast<uintptr_t>(x.scratch) & 255) || (int64_t)x.scratch_bytes < seq_scratch_bytes(a.hd)) return VLA_ERR_NOMEM;
   const SeqFold f = seq_fold(a.hq, a.hkv);
   a.group = f.group; a.fold = f.fold; a.per_group = f.per_group; a.tokens = f.tokens;
   a.scratch = static_cast<char*>(x.scratch);
@@ -76,8 +78,11 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   // (blocks of one head of all sequences, at most, counted in 32 bits)
   const int64_t tokens = tiles * f.tokens, keys = a.offsets_k ? a.tk : (int64_t)a.max_pages * a.page_size;
   if ((a.tq / tokens + a.seqs) * (keys / bn + 1 + seq_item_ticks(mode)) > INT32_MAX) return VLA_ERR_INVALID;
+  const bool whole = seq_always_whole((int)((keys - 1) / bn) + 1 + seq_item_ticks(mode), seq_join_ticks(mode));
+  if (x.scratch ? (reinterpret_cast<uintptr_t>(x.scratch) & 255) || (int64_t)x.scratch_bytes < seq_scratch_bytes(a.hd) : !whole) return VLA_ERR_NOMEM;
   SeqDevice dev;
   if (!seq_device(&dev)) return VLA_ERR_CUDA;
+  a.err = x.scratch ? static_cast<unsigned*>(x.scratch) : dev.error;
   const int shares = seq_shares(mode, dev.sms);
   a.chunk = bn;
   if (!a.offsets_k)
@@ -101,11 +106,17 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
                                         : (two ? pick(vla_op_sequences_kernel<SEQ_WIDE, false, 2>, vla_op_sequences_kernel<SEQ_WIDE, true, 2>)
                                                : pick(vla_op_sequences_kernel<SEQ_WIDE, false, 1>, vla_op_sequences_kernel<SEQ_WIDE, true, 1>));
   const int rc = op_launch(kernel, shares, seq_threads(mode), seq_smem(mode), 1, s, a, maps, op_fault());
-  if (rc != VLA_OK) return rc;
+  if (rc != VLA_OK || whole) return rc;
   // Rows that an item can have: those of its tiles, and those of all tokens; a warp each, or some one after another beyond sixteen blocks an SM.
   const int64_t rows = (int64_t)a.tq * a.fold;
   const int most = rows < seq_item_rows(mode) ? (int)rows : seq_item_rows(mode), blocks = seq_min(most, 16 * dev.sms / shares);
   return op_launch_2d(mode == SEQ_WIDE ? vla_op_sequences_join_kernel<true> : vla_op_sequences_join_kernel<false>, shares, blocks, SEQ_JOIN_THREADS, s, a, mode);
+}
+
+// The error word of calls without scratch memory on the current device, or null.
+unsigned* sequences_error_word() {
+  SeqDevice dev;
+  return seq_device(&dev) ? dev.error : nullptr;
 }
 
 }  // namespace vla

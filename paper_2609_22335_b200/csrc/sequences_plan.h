@@ -81,6 +81,9 @@ SEQ_HD bool seq_whole(const SeqShares& s, int64_t items, int longest, int join) 
   const int64_t cut = s.each + join, fullest = seq_div(items + s.n - 1, s.n) * longest, mixed = s.each + longest - longest / 4;
   return (fullest < mixed ? fullest : mixed) <= cut;
 }
+// Whether they stay whole whatever the lengths are, if no item has more ticks than this: such a call needs neither a join nor scratch memory.  True of 512 keys in every shape.
+SEQ_HD bool seq_always_whole(int longest, int join) { return longest - longest / 4 <= join; }
+
 // x / d = x * magic >> shift for 0 <= x < 2^31, d from 2 to 2^30: with 2^(l-1) < d <= 2^l, magic = 2^(31+l) / d rounded up is below 2^32 and too large by less
 // than 1, which makes x * magic / 2^(31+l) too large by less than 2^-l <= 1 / d.
 inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
@@ -91,9 +94,9 @@ inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
 }
 
 // bf16 numbers that a probability is given in for the second product.  One puts an error beside the result's own rounding that is as large, on average over many rows: 1.41 times the
-// rounding in all.  Of few rows (tokens x heads) it may be more, 1.6 times over 8 rows of which each has a few keys that count; those calls wait for memory or for themselves, and
-// take two numbers: 1.00 to 1.02 times, at 12.4 us as before (one token, 1500 keys) and 223 for 215 (64 tokens over 1.3 GB).
-inline int seq_terms(int64_t tq, int hq) { return tq * hq <= 4096 ? 2 : 1; }
+// rounding in all.  Of few rows (tokens x heads) it may be more, 1.6 times over 8 rows of which each has a few keys that count; such calls are bound by latency and take two numbers:
+// 1.00 to 1.02 times, at 12.4 us as before (one token, 1500 keys).  64 tokens of 32 heads over 1.3 GB of cache would take 280 us for 240, in the long run of a card at its power limit.
+inline int seq_terms(int64_t tq, int hq) { return tq * hq <= 1024 ? 2 : 1; }
 // Shapes of the kernel.  Two: two tiles of 128 rows that share their blocks of 128 keys, an SM to a CTA (long sequences).  One: a tile, blocks of 64 keys, two
 // CTAs an SM.  Wide: the same for heads wider than 128, an SM to a CTA.
 enum { SEQ_TWO = 0, SEQ_ONE = 1, SEQ_WIDE = 2 };
@@ -106,7 +109,7 @@ inline int seq_mode(int64_t tq, int seqs, int hq, int fold, int hd) {
 SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
 // What an item takes beside its blocks, in blocks: its first scores, the last block's chain, the result (6000 cycles beside 3250 to 3850 a block with two tiles, 3200 beside 1100).
 SEQ_HD constexpr int seq_item_ticks(int mode) { return mode == SEQ_TWO ? 2 : 3; }
-SEQ_HD constexpr int seq_join_ticks(int mode) { return mode == SEQ_TWO ? 5 : 6; }
+SEQ_HD constexpr int seq_join_ticks(int mode) { return mode == SEQ_TWO ? 5 : 9; }
 SEQ_HD int seq_item_rows(int mode) { return mode == SEQ_TWO ? 2 * SEQ_ROWS : SEQ_ROWS; }
 SEQ_HD int seq_cols(int hd) { return (hd + 15) / 16 * 16; }      // columns of the result's accumulator
 inline int seq_shares(int mode, int sms) { return mode == SEQ_ONE ? seq_min(2 * sms, SEQ_MAX_SHARES) : seq_min(sms, SEQ_MAX_SHARES / 2); }

@@ -859,6 +859,7 @@ int vla_destroy(vla_ctx* c) {
 }  // extern "C"
 
 #include "ops_api.cuh"
+namespace vla { unsigned* sequences_error_word(); }      // (ops_sequences.cu)
 #include "tile_hooks.cuh"
 
 // ------------------------------------------------------------------------------------------------
@@ -914,6 +915,10 @@ int vla_op_status(int32_t op, const void* scratch, void* stream) {
       op == VLA_OP_LINEAR_BIAS) {
     vla::OpDevice d;
     return vla::op_device(&d) ? vla::op_status_of(d.error_of(op), s) : VLA_ERR_CUDA;
+  }
+  if (!scratch && (op == VLA_OP_ATTENTION_PACKED || op == VLA_OP_ATTENTION_PAGED)) {
+    const unsigned* p = vla::sequences_error_word();
+    return p ? vla::op_status_of(p, s) : VLA_ERR_CUDA;
   }
   if (op == VLA_OP_ATTENTION || op == VLA_OP_ATTENTION_PACKED || op == VLA_OP_ATTENTION_PAGED) {
     if (!scratch) return VLA_ERR_INVALID;

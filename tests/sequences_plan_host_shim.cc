@@ -31,6 +31,9 @@ int64_t seq_parts_end_host(int mode, int hd, int sms) {
 int seq_mode_host(int64_t tq, int seqs, int hq, int fold, int hd) { return vla::seq_mode(tq, seqs, hq, fold, hd); }
 int seq_smem_host(int mode) { return vla::seq_smem(mode); }
 int seq_ticks_host(int mode) { return vla::seq_item_ticks(mode); }
+int seq_always_whole_host(int mode, int keys) {
+  return vla::seq_always_whole((keys - 1) / vla::seq_bn(mode) + 1 + vla::seq_item_ticks(mode), vla::seq_join_ticks(mode)) ? 1 : 0;
+}
 int seq_bn_host(int mode) { return vla::seq_bn(mode); }
 int seq_whole_host(int64_t total, int most, int64_t items, int longest, int join) { return vla::seq_whole(vla::seq_shares_of(total, most), items, longest, join) ? 1 : 0; }
 }

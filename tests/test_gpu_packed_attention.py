@@ -227,3 +227,26 @@ def test_a_wait_that_runs_out_is_reported():
         finally:
             api.debug_op_fault(False)
         ref.check(run(q, k, v, e, *heads), ref.packed(q, k, v, e, e, *heads))
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (4, 4, 128), (2, 1, 256)])
+def test_short_sequences_need_no_scratch_memory(heads):
+    """Up to 512 keys the bits are those of the call with it; what went wrong is in a word of the library then."""
+    import torch
+    from paper_2609_22335_b200 import api
+    for lengths in ([512], [1, 200, 0, 311], [3] * 100):
+        e = ends(lengths)
+        q, k, v = make(e[-1], *heads, seed=19)
+        off = ints(e)
+        got = api.op_attention_packed(q, k, v, off, *heads, causal=True)
+        assert api.op_status(api.OP_ATTENTION_PACKED) == api.VLA_OK
+        assert torch.equal(got, run(q, k, v, e, *heads, causal=True))
+        ref.check(got, ref.packed(q, k, v, e, e, *heads, causal=True))
+        api.debug_op_fault(True, wait_limit_ns=1_000_000)
+        try:
+            api.op_attention_packed(q, k, v, off, *heads)
+            assert api.op_status(api.OP_ATTENTION_PACKED) == api.VLA_ERR_TIMEOUT
+        finally:
+            api.debug_op_fault(False)
+        api.op_attention_packed(q, k, v, off, *heads)
+        assert api.op_status(api.OP_ATTENTION_PACKED) == api.VLA_OK

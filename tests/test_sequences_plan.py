@@ -102,3 +102,20 @@ def test_whole_items_where_cutting_would_gain_nothing(lib):
     assert lib.seq_whole_host(8 * 27, 296, 8, 27, 6) == 0              # a token over a long cache: its keys over the chip
     assert lib.seq_whole_host(10 ** 6, 148, 1000, 1000, 5) == 0        # seven and a bit long ones a share: cut
     assert lib.seq_whole_host(148 * 30, 148, 148, 30, 5) == 1          # one each
+
+
+def test_short_sequences_are_never_cut(lib):
+    """What a call without scratch memory counts on: up to 512 keys every item stays whole, however many there are and of whatever lengths."""
+    rnd = random.Random(4)
+    for mode, join in ((0, 5), (1, 9), (2, 9)):
+        assert lib.seq_always_whole_host(mode, 1) and lib.seq_always_whole_host(mode, 512) and not lib.seq_always_whole_host(mode, 1000)
+        w, most = lib.seq_ticks_host(mode), w_blocks(lib, mode)
+        for _ in range(2000):
+            items = rnd.choice([1, 2, 7, 100, 147, 148, 149, 300, 1000, 50000])
+            longest = w + rnd.randint(1, most)
+            total = rnd.randint(longest + (items - 1) * (w + 1), items * longest) if items > 1 else longest
+            assert lib.seq_whole_host(total, 296 if mode == 1 else 148, items, longest, join)
+
+
+def w_blocks(lib, mode):
+    return 512 // lib.seq_bn_host(mode)

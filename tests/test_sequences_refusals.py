@@ -55,7 +55,8 @@ def test_attention(lib, mem, paged):
         bads += [dict(offsets_k=0), dict(offsets_k=p + 2), dict(tk=0), dict(tk=(1 << 30) + 1)]
     for bad in bads:
         assert call(lib, name, {**good(p, paged), **bad}) == api.VLA_ERR_INVALID, bad
-    for bad in (dict(scratch=0), dict(scratch=p + 128), dict(scratch_bytes=1000)):
+    # (none at all is for calls of at most 512 keys a sequence)
+    for bad in (dict(scratch=0, tk=1000, max_pages=200), dict(scratch=p + 128), dict(scratch_bytes=1000)):
         assert call(lib, name, {**good(p, paged), **bad}) == api.VLA_ERR_NOMEM, bad
     assert getattr(lib, name)(None, None) == api.VLA_ERR_INVALID
     # more key blocks of a head than are counted
