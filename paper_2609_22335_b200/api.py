@@ -874,7 +874,9 @@ def op_cache_store(k, v, k_cache, v_cache, pages, lengths, offsets, stream=None)
 
 
 def op_status(op, scratch=None, stream=None) -> int:
-    """Waits for ``stream`` (None: torch's current one) and returns the operator's status word as a VLA_* code (VLA_OK or VLA_ERR_TIMEOUT)."""
+    """Waits for ``stream`` (None: torch's current one) and returns the operator's status word as a VLA_* code (VLA_OK or VLA_ERR_TIMEOUT).
+    Calls with ``scratch`` have it there: pass the same.  Without, that of ``op_attention_packed`` and ``op_attention_paged`` is the one of calls that need none, at most
+    512 keys a sequence."""
     return load_library().vla_op_status(op, None if scratch is None else scratch.data_ptr(), _stream_ptr(stream))
 
 

@@ -50,7 +50,7 @@ static bool seq_cache_ok(int n_pages, int page_size, int max_pages) {
 // What both attentions ask of their arguments.
 static bool seq_shape_ok(const vla_attention_args& x) {
   if (x.seqs < 1 || x.seqs > 1 << 20 || x.tq < 1 || x.tq > 1 << 30 || x.hkv < 1 || x.hq < x.hkv || x.hq % x.hkv || x.hq > 65536 || x.hd < 8 || x.hd > 256 || x.hd % 8) return false;
-  if (!(x.scale > 0.f) || !(x.scale < 1e30f) || !(x.cap >= 0.f) || !(x.cap < 1e30f) || x.window < 0 || (!x.causal && (x.window || x.prefix)) || x.reserved) return false;
+  if (!(x.scale > 0.f) || !(x.scale < 1e30f) || !(x.cap >= 0.f) || !(x.cap < 1e30f) || (x.cap > 0.f && !(x.scale / x.cap < 1e30f)) || x.window < 0 || (!x.causal && (x.window || x.prefix)) || x.reserved) return false;
   if (!seq_rows_ok(x.q, x.ld_q, (int64_t)x.hq * x.hd) || !seq_rows_ok(x.out, x.ld_out, (int64_t)x.hq * x.hd)) return false;
   if (!seq_rows_ok(x.k, x.ld_k, (int64_t)x.hkv * x.hd) || !seq_rows_ok(x.v, x.ld_v, (int64_t)x.hkv * x.hd)) return false;
   return x.offsets_q && op_aligned(4, {x.offsets_q, x.prefix, x.slopes});
@@ -73,8 +73,7 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   a.scale_log2 = x.scale * 1.44269504f;
   a.capped = x.cap > 0.f ? 1 : 0;
   a.cap_in = a.capped ? x.scale / x.cap : 0.f; a.cap_log2 = x.cap * 1.44269504f;
-  const int mode = seq_mode(a.tq, a.seqs, a.hq, f.fold, a.hd), bn
-   = seq_bn(mode), nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
+  const int mode = seq_mode(a.tq, a.seqs, a.hq, f.fold, a.hd), bn = seq_bn(mode), nbox = (a.hd + 63) / 64, tiles = mode == SEQ_TWO ? 2 : 1;
   // (blocks of one head of all sequences, at most, counted in 32 bits)
   const int64_t tokens = tiles * f.tokens, keys = a.offsets_k ? a.tk : (int64_t)a.max_pages * a.page_size;
   if ((a.tq / tokens + a.seqs) * (keys / bn + 1 + seq_item_ticks(mode)) > INT32_MAX) return VLA_ERR_INVALID;

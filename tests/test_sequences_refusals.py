@@ -40,7 +40,7 @@ def call(lib, name, d):
 
 BOTH = [dict(q=0), dict(k=0), dict(v=0), dict(out=0), dict(offsets_q=0), dict(seqs=0), dict(seqs=-1), dict(seqs=(1 << 20) + 1), dict(tq=0), dict(tq=(1 << 30) + 1), dict(hq=0), dict(hkv=0),
         dict(hq=3, hkv=2, ld_q=192, ld_out=192, ld_k=128, ld_v=128), dict(hq=65538, ld_q=1 << 23, ld_out=1 << 23), dict(hd=0), dict(hd=4), dict(hd=60), dict(hd=264, ld_q=528, ld_out=528, ld_k=264, ld_v=264),
-        dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(cap=-1.0), dict(cap=math.nan), dict(cap=math.inf), dict(window=-1), dict(causal=0, window=4),
+        dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(cap=-1.0), dict(cap=math.nan), dict(cap=math.inf), dict(cap=1e-40), dict(window=-1), dict(causal=0, window=4),
         dict(causal=0, prefix=4096), dict(reserved=1), dict(ld_q=120), dict(ld_q=132), dict(ld_out=64), dict(ld_out=129), dict(ld_k=56), dict(ld_v=68), dict(ld_v=1 << 38)]
 
 
