@@ -603,15 +603,19 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
     const int t = warp >> 2, row = (int)threadIdx.x & 127, tt = row / a.fold, hh = row - tt * a.fold;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     bool ok = true;
-    uint32_t ns[2] = {0, 0}, ring0 = 0, items = 0;      // blocks of a tile of scores, ring places and items so far
+    uint32_t ns[2] = {0, 0}, ring0 = 0, items = 0;      // blocks of a tile of scores so far; ring place, twice around (odd rounds wait for the other phase); items so far
     // Rows of V behind the last key (of other sequences, or what a page held before) may be anything, and 0 x inf is NaN: they become zeros.
-    auto zero_tail = [&](const SeqItem& w, int i, int n, int c0) {
-      const uint32_t place = ring0 + (uint32_t)(TWO ? 2 * i + 1 : min(2 * i + 2, 2 * n - 1)), stage = place % (uint32_t)NS;
-      if (ok) ok = mbar_wait(c, full + 8u * stage, place / (uint32_t)NS & 1u);
-      const int from = max(w.nk - c0, 0);
+    // (The last block of an item alone has any, and its V is the item's last place of the ring.)
+    auto zero_tail = [&](const SeqItem& w, uint32_t end, int c0) {
+      const uint32_t place = end == 0 ? 2u * (uint32_t)NS - 1u : end - 1u, odd = place >= (uint32_t)NS ? 1u : 0u, stage = place - odd * (uint32_t)NS;
+      if (ok) ok = mbar_wait(c, full + 8u * stage, odd);
+      const int from = max(w.nk - c0, 0) * 8;
       char* const v0 = smem_dyn + (ring + stage * stage_bytes - smem_u32(smem_dyn));
-      for (int x = from * 8 + row; x < BN * 8; x += 128)
-        for (int b = 0; b < nbox; ++b) *reinterpret_cast<uint4*>(v0 + b * (BN * 128) + x * 16) = make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+      for (int b = 0; b < nbox; ++b)
+#pragma unroll
+        for (int x = 0; x < BN * 8; x += 128)
+          if (x + row >= from) *reinterpret_cast<uint4*>(v0 + b * (BN * 128) + (x + row) * 16) = make_uint4(0, 0, 0, 0);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     };
     for (; ok; ++items) {
@@ -627,6 +631,8 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       if (!valid) { seen.hi = INT_MAX / 2; seen.lo = 0; }              // (nobody stores it: nothing to mask)
       const float slope = EXTRA && a.slopes && valid ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
       float m_run = -INFINITY, l_run = 0.f;
+      ring0 += 2u * (uint32_t)n;               // (from here on the place behind the item's last)
+      if (ring0 >= 2u * (uint32_t)NS) ring0 = n < NS ? ring0 - 2u * (uint32_t)NS : ring0 % (2u * (uint32_t)NS);
 #pragma unroll 1
       for (int i = 0; i < n; ++i) {
         const int slot = TWO ? t : i & 1, c0 = seq_block(SeqBlocks{w.na, w.lo, 0}, w.b0 + i) * BN;
@@ -635,7 +641,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         __syncwarp();
         tc_fence_after();
         if (!TWO && !__any_sync(0xffffffffu, valid)) {      // nobody's rows, as most warps' of a single token's tile: whatever lies there will do for probabilities
-          if (w.nk - c0 < BN) zero_tail(w, i, n, c0);
+          if (w.nk - c0 < BN) zero_tail(w, ring0, c0);
           arrive_warp(p_full + 8u * slot, lane);
           ++ns[slot];
           continue;
@@ -702,7 +708,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
           tc_fence_after();
           attn_rescale(tmem_o + lanes + (TWO ? 128u * t : 0u), hdc, alpha);
         }
-        if ((TWO ? t == 0 : true) && w.nk - c0 < BN) zero_tail(w, i, n, c0);
+        if ((TWO ? t == 0 : true) && w.nk - c0 < BN) zero_tail(w, ring0, c0);
 #pragma unroll
         for (int k = 0; k < TERMS * BN / 2; k += 16) tmem_st16u(ts + k, sr + k);
         tmem_st_wait();
@@ -710,16 +716,8 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         arrive_warp(p_full + 8u * slot, lane);
         ++ns[slot];
       }
-      ring0 += 2u * (uint32_t)n;
       // ---------------- the row's result
       const bool whole = w.part < 0;
-      {
-        const int slot = TWO ? t : (n - 1) & 1;
-        const uint32_t count = TWO ? items : ns[slot] - 1;
-        if (ok) ok = mbar_wait(c, o_done + 8u * slot, count & 1u);
-      }
-      __syncwarp();
-      tc_fence_after();
       m_run *= EXTRA ? (a.slopes ? 1.0f : (a.capped ? a.cap_log2 : a.scale_log2)) : a.scale_log2;   // (log2 units from here on; -inf stays, scale > 0)
       const float inv = l_run == 0.f ? (seen.hi > 0 ? NAN : 0.f) : 1.0f / l_run;
       const int at = (TWO ? t * SEQ_ROWS : 0) + row;
@@ -730,6 +728,13 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       unsigned short* const o = a.out + (int64_t)(w.q0 + token) * a.ld_out + head * a.hd;
       const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ld_out * 2) | (uintptr_t)(a.hd * 2)) & 31) == 0;
       const uint32_t to = tmem_o + lanes + (TWO ? 128u * t : 0u);
+      {
+        const int slot = TWO ? t : (n - 1) & 1;
+        const uint32_t count = TWO ? items : ns[slot] - 1;
+        if (ok) ok = mbar_wait(c, o_done + 8u * slot, count & 1u);
+      }
+      __syncwarp();
+      tc_fence_after();
       uint64_t sum = 0ull;                    // of all values: not finite if one is not
       const uint64_t by = whole ? pack2(inv, inv) : pack2(1.0f, 1.0f);
 #pragma unroll 1
