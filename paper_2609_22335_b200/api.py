@@ -403,7 +403,7 @@ class Engine:
 
 
 POLICIES = {"two_phase": 0, "class_order": 1, "round_robin": 2, "two_phase_g": 3, "two_phase_r": 4}
-OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED, OP_LINEAR_BIAS, OP_ATTENTION_PACKED, OP_ATTENTION_PAGED = range(9)
+OP_LINEAR, OP_ATTENTION, OP_ATTENTION_STATIC, OP_LINEAR_SCALED, OP_LINEAR_GROUPED, OP_LINEAR_GROUPED_SCALED, OP_LINEAR_BIAS, OP_ATTENTION_PACKED, OP_ATTENTION_PAGED, OP_ATTENTION_SHORT = range(10)
 
 
 def policy_probe(taus, pending, feasible, cta_count, u, rr_start=0, u_max=0, policy=0, grid=None, res=None):
@@ -875,8 +875,8 @@ def op_cache_store(k, v, k_cache, v_cache, pages, lengths, offsets, stream=None)
 
 def op_status(op, scratch=None, stream=None) -> int:
     """Waits for ``stream`` (None: torch's current one) and returns the operator's status word as a VLA_* code (VLA_OK or VLA_ERR_TIMEOUT).
-    Calls with ``scratch`` have it there: pass the same.  Without, that of ``op_attention_packed`` and ``op_attention_paged`` is the one of calls that need none, at most
-    512 keys a sequence."""
+    Operators with ``scratch`` have it there: pass the same.  OP_ATTENTION_SHORT: of calls of ``op_attention_packed`` and ``op_attention_paged`` that need none (at most
+    512 keys a sequence) and were given none."""
     return load_library().vla_op_status(op, None if scratch is None else scratch.data_ptr(), _stream_ptr(stream))
 
 

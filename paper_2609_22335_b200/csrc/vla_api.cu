@@ -916,7 +916,7 @@ int vla_op_status(int32_t op, const void* scratch, void* stream) {
     vla::OpDevice d;
     return vla::op_device(&d) ? vla::op_status_of(d.error_of(op), s) : VLA_ERR_CUDA;
   }
-  if (!scratch && (op == VLA_OP_ATTENTION_PACKED || op == VLA_OP_ATTENTION_PAGED)) {
+  if (op == VLA_OP_ATTENTION_SHORT) {
     const unsigned* p = vla::sequences_error_word();
     return p ? vla::op_status_of(p, s) : VLA_ERR_CUDA;
   }

@@ -239,14 +239,14 @@ def test_short_sequences_need_no_scratch_memory(heads):
         q, k, v = make(e[-1], *heads, seed=19)
         off = ints(e)
         got = api.op_attention_packed(q, k, v, off, *heads, causal=True)
-        assert api.op_status(api.OP_ATTENTION_PACKED) == api.VLA_OK
+        assert api.op_status(api.OP_ATTENTION_SHORT) == api.VLA_OK
         assert torch.equal(got, run(q, k, v, e, *heads, causal=True))
         ref.check(got, ref.packed(q, k, v, e, e, *heads, causal=True))
         api.debug_op_fault(True, wait_limit_ns=1_000_000)
         try:
             api.op_attention_packed(q, k, v, off, *heads)
-            assert api.op_status(api.OP_ATTENTION_PACKED) == api.VLA_ERR_TIMEOUT
+            assert api.op_status(api.OP_ATTENTION_SHORT) == api.VLA_ERR_TIMEOUT
         finally:
             api.debug_op_fault(False)
         api.op_attention_packed(q, k, v, off, *heads)
-        assert api.op_status(api.OP_ATTENTION_PACKED) == api.VLA_OK
+        assert api.op_status(api.OP_ATTENTION_SHORT) == api.VLA_OK
