@@ -18,7 +18,7 @@
 //
 // Measured: 8192 tokens both ways, 16 heads of 128, 472 us (1.16 PFLOP/s), of 64 417 us (0.66), 8 over 1 of 256 525 us (1.05); causal 264, 236 and 285 us.  Bound by the chain of a block:
 // with two tiles 3850 cycles at heads of 128, of which the products take 1370 from the probabilities to the next scores, the maximum 460, the exponentials 1600.  64 single tokens over
-// 1650 to 8192 keys, 32 heads over 8 of 128, 237 us: 5.4 TB/s.  A call's first scores come 4 us after its start.
+// 1650 to 8192 keys, 32 heads over 8 of 128, 222 to 237 us: 5.4 to 5.8 TB/s.  A call's first scores come 4 us after its start.
 #pragma once
 #include "op_common.cuh"
 #include "sequences_plan.h"

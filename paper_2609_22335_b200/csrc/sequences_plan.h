@@ -95,7 +95,7 @@ inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
 
 // bf16 numbers that a probability is given in for the second product.  One puts an error beside the result's own rounding that is as large, on average over many rows: 1.41 times the
 // rounding in all.  Of few rows (tokens x heads) it may be more, 1.6 times over 8 rows of which each has a few keys that count; such calls are bound by latency and take two numbers:
-// 1.00 to 1.02 times, at 12.4 us as before (one token, 1500 keys).  64 tokens of 32 heads over 1.3 GB of cache would take 280 us for 240, in the long run of a card at its power limit.
+// 1.00 to 1.02 times, at 12.4 us as before (one token, 1500 keys).  64 tokens of 32 heads over 1.3 GB of cache would take 280 us for 231, in the long run of a card at its power limit.
 inline int seq_terms(int64_t tq, int hq) { return tq * hq <= 1024 ? 2 : 1; }
 // Shapes of the kernel.  Two: two tiles of 128 rows that share their blocks of 128 keys, an SM to a CTA (long sequences).  One: a tile, blocks of 64 keys, two
 // CTAs an SM.  Wide: the same for heads wider than 128, an SM to a CTA.
