@@ -237,15 +237,31 @@ struct SeqWalk {
 };
 
 // ---------------------------------------------------------------- scores
-// tanh to 32-bit precision, (e - 1) / (e + 1) with e = 2^(2 x log2 e); the fast form is off by 2^-11, which a cap of 50 would turn into a logit's error of 0.02.
-__device__ __forceinline__ float seq_tanh(float x) {
-  const float t = fminf(fabsf(x), 15.0f);      // (NaN: fminf would drop it, see below)
+// tanh to 32-bit precision (the fast form is off by 2^-11, which a cap of 50 would turn into a logit's error of 0.02): an odd polynomial up to 1/2 (least largest relative
+// error there, 1.3e-8), a power and a reciprocal beyond.  Which of them is a matter of the score alone: what else lies in its block or warp changes no bit of it.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t seq_tanh_near2(uint64_t x) {      // two of them, up to 1/2
+  const uint64_t z = mul2(x, x);
+  uint64_t y = fma2(z, pack2(1.7135007306933403e-02f, 1.7135007306933403e-02f), pack2(-5.298607423901558e-02f, -5.298607423901558e-02f));
+  y = fma2(y, z, pack2(1.3324779272079468e-01f, 1.3324779272079468e-01f));
+  y = fma2(y, z, pack2(-3.333306908607483e-01f, -3.333306908607483e-01f));
+  return mul2(fma2(y, z, pack2(1.0f, 1.0f)), x);
+}
+__device__ __forceinline__ float seq_tanh_far(float x) {              // beyond: 1 - 2 / (1 + e^2x)
   float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t * 2.885390082f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 2.885390082f));
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-  const float y = copysignf(fmaf(-2.0f, r, 1.0f), x);
-  const float small = x * fmaf(x * x, fmaf(x * x, 0.133333333f, -0.333333333f), 1.0f);      // near 0, where 1 - 2 r has few bits left
-  return x != x ? x : (fabsf(x) < 0.07f ? small : y);
+  return fmaf(-2.0f, r, 1.0f);
+}
+__device__ __forceinline__ float seq_tanh_pick(float x, float near) { return fabsf(x) > 0.5f ? seq_tanh_far(x) : near; }      // (NaN: the polynomial's)
+__device__ __forceinline__ float seq_tanh(float x) {
+  float near, other;
+  unpack2(seq_tanh_near2(pack2(x, x)), near, other);
+  return seq_tanh_pick(x, near);
 }
 // A score in log2 units: capped, with the bias by distance (d = p - j).
 __device__ __forceinline__ float seq_score(const SeqArgs& a, float dot, float slope_log2, float d) {
@@ -300,11 +316,6 @@ __device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, i
   }
 }
 
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ uint64_t pair_of(const uint32_t* v) { return pack2(__uint_as_float(v[0]), __uint_as_float(v[1])); }
 __device__ __forceinline__ void pair_to(uint32_t* v, uint64_t x) {
   float a, b;
@@ -655,27 +666,37 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
           const float d = (float)(p - c0);
           sl2 = a.capped ? a.cap_log2 : a.scale_log2;                  // what makes log2 units of the scores in the registers
           if (a.capped) {
-            // cap tanh(x): an odd polynomial up to 1/2 (least largest relative error there, 1.3e-8), by powers and reciprocals where a score is beyond.
+            // cap tanh(x).  Where no score of the warp's rows, hidden ones among them, is beyond 1/2, none of them needs the far form; that saves its time and changes no result.
             float top = 0.f;
 #pragma unroll
             for (int j = 0; j < BN; j += 2) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(sr[j])), fabsf(__uint_as_float(sr[j + 1]))));
-            if (__any_sync(0xffffffffu, !(top * a.cap_in <= 0.5f))) {
+            const uint64_t in = pack2(a.cap_in, a.cap_in);
+            // (That form 32 columns at a time, through tensor memory: its code for 128 columns made calls that never run it 5 % slower, 514 -> 540 us at 8192 + 5660 tokens.)
+            if (__any_sync(0xffffffffu, top * a.cap_in > 0.5f)) {
+#pragma unroll 1
+              for (uint32_t k = ts; k < ts + BN; k += 32) {
+                uint32_t x[32];
+                tmem_ld32_nowait(k, x);
+                tmem_ld_wait();
 #pragma unroll
-              for (int j = 0; j < BN; ++j) {
-                float e, r;                   // 1 - 2 / (1 + e^2x), off by 2^-23 of the cap
-                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__uint_as_float(sr[j]) * (a.cap_in * 2.885390082f)));
-                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
-                sr[j] = __float_as_uint(fmaf(-2.0f, r, 1.0f));
+                for (int j = 0; j < 32; j += 2) {
+                  const uint64_t y = mul2(pair_of(x + j), in);
+                  float x0, x1, y0, y1;
+                  unpack2(y, x0, x1);
+                  unpack2(seq_tanh_near2(y), y0, y1);
+                  x[j] = __float_as_uint(seq_tanh_pick(x0, y0));
+                  x[j + 1] = __float_as_uint(seq_tanh_pick(x1, y1));
+                }
+                tmem_st16u(k, x);
+                tmem_st16u(k + 16, x + 16);
               }
+              tmem_st_wait();
+#pragma unroll
+              for (int k = 0; k < BN; k += 32) tmem_ld32_nowait(ts + k, sr + k);
+              tmem_ld_wait();
             } else {
 #pragma unroll
-              for (int j = 0; j < BN; j += 2) {
-                const uint64_t x = mul2(pair_of(sr + j), pack2(a.cap_in, a.cap_in)), z = mul2(x, x);
-                uint64_t y = fma2(z, pack2(1.7135007306933403e-02f, 1.7135007306933403e-02f), pack2(-5.298607423901558e-02f, -5.298607423901558e-02f));
-                y = fma2(y, z, pack2(1.3324779272079468e-01f, 1.3324779272079468e-01f));
-                y = fma2(y, z, pack2(-3.333306908607483e-01f, -3.333306908607483e-01f));
-                pair_to(sr + j, mul2(fma2(y, z, pack2(1.0f, 1.0f)), x));
-              }
+              for (int j = 0; j < BN; j += 2) pair_to(sr + j, seq_tanh_near2(mul2(pair_of(sr + j), in)));
             }
           }
           if (a.slopes) {
