@@ -342,7 +342,7 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
  * last of its tokens.  causal: row i sees keys j <= p, with window > 0 those with p - j < window, and of every row's keys the first prefix[s] (prefix NULL: none).
  * Not causal: all nk, and neither prefix nor window.  A row that sees no key becomes zeros.
  * bf16, rows ld_* elements apart, 16-byte aligned, rows too; hd a multiple of 8, at most 256; hq a multiple of hkv; scale > 0; cap 0, or such that scale / cap < 1e30 (tanh is good to
- * 2^-23, so capped scores to 2^-23 of the cap).  offsets_q,
+ * 2^-21, so capped scores to 2^-21 of the cap).  offsets_q,
  * offsets_k int32 [seqs + 1], prefix int32 [seqs], slopes fp32 [hq], all DEVICE and read by the kernel.  Offsets ascend; what lies outside of 0 .. tq (tk)
  * counts as the nearer end.  Rows of no sequence are not written.  Keys that a row does not see have no part in it, whatever their values.
  * A call's rows x keys are limited: (tq / 128 * hq / hkv + seqs) x tk / 64 stays below 2^31, about (a cache: max_pages * page_size for tk).

@@ -87,3 +87,20 @@ def test_a_score_beyond_half_the_cap_leaves_the_others_as_they_are(hd):
             keys[n // 2, 0] = at
             got.append(run(q, keys, v, e, 2, 1, hd, cap=1e4, scale=1.0))
         assert torch.equal(*got)
+
+
+@pytest.mark.parametrize("n,hd", [(200, 64), (6000, 64), (6000, 128), (2000, 256)])
+def test_scores_below_zero_are_as_good_as_those_above(n, hd):
+    """tanh is odd: two keys whose scores change sign change places, bit for bit.  (A cap times log2 e that rounds to 2^20, so that nothing else rounds; the scores lie a few
+    units of the last place of the capped ones apart.)"""
+    import numpy as np
+    import torch
+    c = np.float32(2.0 ** 20 / np.log2(np.e))
+    cap = next(float(x) for x in (c, np.nextafter(c, np.float32(0)), np.nextafter(c, np.float32(1e9))) if x * np.float32(1.44269504) == np.float32(2 ** 20))
+    g = torch.Generator(device="cuda").manual_seed(n)
+    q, k, v = (torch.zeros(m, hd, dtype=torch.bfloat16, device="cuda") for m in (n, 2, 2))
+    q[:, 0] = 0.05 + 3 * torch.rand(n, device="cuda", generator=g)
+    q[:, 1] = torch.randint(1, 9, (n,), device="cuda", generator=g).bfloat16()
+    k[:, 0], k[1, 1], v[1] = 1, 2.0 ** -19, 1
+    up, down = (run(q, s * k, w, [0, n], 1, 1, hd, ends_k=[0, 2], scale=cap, cap=cap) for s, w in ((1, v), (-1, 1 - v)))
+    assert bool(((up > 0.5) & (up < 0.999)).any()) and torch.equal(up, down)
