@@ -271,10 +271,32 @@ __device__ __forceinline__ float seq_score(const SeqArgs& a, float dot, float sl
   return fmaf(-slope_log2, fabsf(d), s);
 }
 
+// Waits of this kernel: as mbar_wait of OpWaits, but none gives up while a warp of the CTA does rows again (below), nor for its limit afterwards.  That work ends by itself, after
+// as many steps as there are keys, and its partners have to wait for it.
+struct SeqWaits {
+  unsigned* words;                             // the CTA's error word; the time before which nobody gives up
+  uint32_t limit;                              // (times are in 1024 ns)
+};
+__device__ __forceinline__ uint32_t seq_now() { return (uint32_t)(gtimer() >> 10); }
+__device__ __forceinline__ bool mbar_wait(const SeqWaits& c, uint32_t bar, uint32_t parity) {
+  if (mbar_try_wait(bar, parity, 20000u)) return true;
+  const uint32_t until = seq_now() + c.limit;
+  while (!mbar_try_wait(bar, parity, 20000u)) {
+    if (*reinterpret_cast<volatile unsigned*>(c.words) != 0u) return false;
+    const uint32_t now = seq_now();
+    if ((int)(now - until) > 0 && (int)(now - *reinterpret_cast<volatile unsigned*>(c.words + 1)) > 0) {
+      atomicCAS(c.words, 0u, (unsigned)DEV_ERR_WAIT_MBAR);
+      return false;
+    }
+  }
+  return true;
+}
+__device__ __forceinline__ void seq_at_work(const SeqWaits& c) { *reinterpret_cast<volatile unsigned*>(c.words + 1) = seq_now() + c.limit; }
+
 // A row's result key by key, from the keys it sees alone, by one warp: eight head dims a lane.  Where a value that a row does not see is infinite or
 // NaN, the tensor core's 0 x inf spoils the row; such rows are done again this way, which also is what the kernels are checked against.
 struct SeqRow { float m, l, acc[8]; };
-__device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, int bn, int token, int head, SeqRow& r) {
+__device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, int bn, int token, int head, const SeqWaits& c, SeqRow& r) {
   const int lane = threadIdx.x & 31, d0 = 8 * lane, p = q.nk - q.nq + token;
   const bool have = d0 < a.hd;
   const SeqSeen seen = seq_seen(p, q.nk, q.prefix, a.causal, a.window);
@@ -315,6 +337,7 @@ __device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, i
       for (int i = 0; i < 8; ++i) r.acc[i] = fmaf(r.acc[i], keep, e * y[i]);
       r.m = m;
     }
+    seq_at_work(c);
   }
 }
 
@@ -392,7 +415,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   extern __shared__ char smem_dyn[];
   __shared__ __align__(8) uint64_t bars[2 * SEQ_MAX_STAGES + 10];
   __shared__ uint32_t tmem_base_s;
-  __shared__ unsigned failed_s;
+  __shared__ unsigned failed_s[2];             // (see SeqWaits)
   __shared__ SeqItem item_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, NS = a.stages;
   const int nbox = (a.hd + 63) / 64, hdc = seq_cols(a.hd), tokens = (TWO ? 2 : 1) * a.tokens;
@@ -408,7 +431,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       mbar_init(full + 8u * lane, i == 2 || i == 3 || i == 6 || i == 7 ? 4 : (i == 9 ? 1 + SOFT : 1));
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (lane == 0) failed_s = 0;
+    if (lane == 0) { failed_s[0] = 0; failed_s[1] = seq_now(); }
   } else if (warp == SOFT + 1) {
     tmem_alloc(&tmem_base_s, COLS);
   }
@@ -418,7 +441,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
     if (a.scratch) record->parts = 0;
     if (blockIdx.x == 0) *err = 0u;
   }
-  const OpWaits c = {&failed_s, fault.wait_limit};
+  const SeqWaits c = {failed_s, fault.wait_limit};
   tc_fence_before();
   __syncthreads();
   op_let_next_start();
@@ -810,7 +833,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
         const float r_m = __shfl_sync(0xffffffffu, m_run, src);
         const bool r_sees = __shfl_sync(0xffffffffu, seen.hi, src) > 0;
         SeqRow r;
-        seq_row_alone(a, w, BN, r_token, r_head, r);
+        seq_row_alone(a, w, BN, r_token, r_head, c, r);
         if (8 * lane < a.hd) {
           if (whole) {
             const float i_ = r.l != 0.f ? 1.0f / r.l : (r_sees ? NAN : 0.f);
@@ -831,7 +854,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
   }
   __syncthreads();
   if (warp == SOFT + 1) tmem_dealloc(tmem, COLS);
-  if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(&failed_s) != 0u) *err = (unsigned)DEV_ERR_WAIT_MBAR;
+  if (threadIdx.x == 0 && *reinterpret_cast<volatile unsigned*>(failed_s) != 0u) *err = (unsigned)DEV_ERR_WAIT_MBAR;
 }
 
 // Parts of the items that were cut, put together: a warp a row, or four where there are many parts, each with every fourth part.  Bound by the way to the L2
