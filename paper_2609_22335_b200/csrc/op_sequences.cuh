@@ -293,51 +293,179 @@ __device__ __forceinline__ bool mbar_wait(const SeqWaits& c, uint32_t bar, uint3
 }
 __device__ __forceinline__ void seq_at_work(const SeqWaits& c) { *reinterpret_cast<volatile unsigned*>(c.words + 1) = seq_now() + c.limit; }
 
-// A row's result key by key, from the keys it sees alone, by one warp: eight head dims a lane.  Where a value that a row does not see is infinite or
-// NaN, the tensor core's 0 x inf spoils the row; such rows are done again this way, which also is what the kernels are checked against.
+// ---------------------------------------------------------------- rows next to values that are not finite
+// Where a value that a row does not see is infinite or NaN, the tensor core's 0 x inf makes NaN of that column of the row's result (a column that is not NaN had no such product in it).
+// Whether it rightly is NaN decides a look at V: it is if the row sees a NaN there.  Otherwise the row's columns in question are worked out again, from the keys it sees alone.
+// 4096 tokens both ways, 8 heads over 4 of 128, a NaN or infinity that all see: 0.47 ms for 0.10, the look.  Causal, a NaN in the middle of a tile, 1365 keys: 3.8 ms for
+// 0.08, the 32 rows of a warp one after another in that tile; an infinity in every tile, 8.3 ms, all rows.
+struct SeqPlace { const unsigned short *k, *v; };      // of the item's key head; null: a page that does not exist, which reads as zeros
+__device__ __forceinline__ SeqPlace seq_place(const SeqArgs& a, const SeqItem& w, int j) {
+  long long k, v;
+  if (a.offsets_k) {
+    k = (w.k0 + j) * a.ld_k; v = (w.k0 + j) * a.ld_v;
+  } else {
+    const int slot = (int)((uint64_t)(uint32_t)j * a.page_magic >> a.page_shift), page = __ldcg(a.pages + (long long)w.s * a.max_pages + slot), in = j - slot * a.page_size;
+    if (page < 0 || page >= a.n_pages) return SeqPlace{nullptr, nullptr};
+    k = page * a.page_k + in * a.ld_k; v = page * a.page_v + in * a.ld_v;
+  }
+  return SeqPlace{a.k + k + w.kvh * a.hd, a.v + v + w.kvh * a.hd};
+}
+// The first and the last of an item's keys whose value is NaN, for each of the columns 8 * lane .. + 7.  (A warp reads as many keys at once as their columns leave lanes for.)
+struct SeqNan { int first[8], last[8]; };
+__device__ __forceinline__ void seq_nan_keys(const SeqArgs& a, const SeqItem& w, int bn, const SeqWaits& c, SeqNan& n) {
+  constexpr int AHEAD = 8;
+  const int lane = threadIdx.x & 31, per = a.hd / 8, side = 32 / per, at = lane / per, d0 = (lane - at * per) * 8;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { n.first[i] = INT_MAX; n.last[i] = -1; }
+#pragma unroll 1
+  for (int b = w.b0; b < w.b0 + w.n; ++b) {
+    const int c0 = seq_block(SeqBlocks{w.na, w.lo, 0}, b) * bn, end = min(c0 + bn, w.nk);
+#pragma unroll 1
+    for (int j0 = c0 + at; j0 < end + at; j0 += AHEAD * side) {
+      uint4 x[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int j = j0 + u * side;
+        x[u] = make_uint4(0, 0, 0, 0);
+        if (at < side && j < end) {
+          const SeqPlace p = seq_place(a, w, j);
+          if (p.v) x[u] = *reinterpret_cast<const uint4*>(p.v + d0);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        float y[8];
+        unpack8(x[u], y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (y[i] != y[i]) { n.first[i] = min(n.first[i], j0 + u * side); n.last[i] = max(n.last[i], j0 + u * side); }
+      }
+    }
+    if (b % 8 == 0) seq_at_work(c);
+  }
+  for (int k = 1; k < side; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int first = __shfl_sync(0xffffffffu, n.first[i], (lane + k * per) & 31), last = __shfl_sync(0xffffffffu, n.last[i], (lane + k * per) & 31);
+      if (lane < per) { n.first[i] = min(n.first[i], first); n.last[i] = max(n.last[i], last); }
+    }
+}
+// One row, by one warp: scores of 32 keys at once, a key a lane, then their values, eight columns a lane and as many keys side by side as these leave lanes for.  Returns whether
+// there is something to store: not where all columns that are asked for (`open`, bits of the columns 8 * lane .. + 7) have become NaN, which then they stay.
 struct SeqRow { float m, l, acc[8]; };
-__device__ __noinline__ void seq_row_alone(const SeqArgs& a, const SeqItem& q, int bn, int token, int head, const SeqWaits& c, SeqRow& r) {
-  const int lane = threadIdx.x & 31, d0 = 8 * lane, p = q.nk - q.nq + token;
-  const bool have = d0 < a.hd;
-  const SeqSeen seen = seq_seen(p, q.nk, q.prefix, a.causal, a.window);
+__device__ __forceinline__ bool seq_row_alone(const SeqArgs& a, const SeqItem& w, int bn, const SeqWaits& c, int token, int head, SeqSeen seen, unsigned open, SeqRow& r) {
+  constexpr int AHEAD = 8;
+  const int lane = threadIdx.x & 31, per = a.hd / 8, side = 32 / per, at = lane / per, d0 = (lane - at * per) * 8, p = w.nk - w.nq + token;
   const float slope = a.slopes ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
-  float x[8], y[8];
-  uint4 w = make_uint4(0, 0, 0, 0);
-  if (have) w = *reinterpret_cast<const uint4*>(a.q + (q.q0 + token) * a.ld_q + head * a.hd + d0);
-  unpack8(w, x);
+  const unsigned short* const q = a.q + (w.q0 + token) * a.ld_q + head * a.hd;
   r.m = -INFINITY; r.l = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.acc[i] = 0.f;
 #pragma unroll 1
-  for (int b = q.b0; b < q.b0 + q.n; ++b) {
-    const int c0 = seq_block(SeqBlocks{q.na, q.lo, 0}, b) * bn;
+  for (int b = w.b0; b < w.b0 + w.n; ++b) {
+    const int c0 = seq_block(SeqBlocks{w.na, w.lo, 0}, b) * bn;
 #pragma unroll 1
-    for (int j = c0; j < min(c0 + bn, seen.hi); ++j) {
-      if (j < seen.lo && j >= q.prefix) continue;
-      const unsigned short *kp = a.k + q.kvh * a.hd + d0, *vp = a.v + q.kvh * a.hd + d0;
-      bool there = have;
-      if (a.offsets_k) {
-        kp += (q.k0 + j) * a.ld_k; vp += (q.k0 + j) * a.ld_v;
-      } else {
-        const int page = __ldcg(a.pages + (long long)q.s * a.max_pages + j / a.page_size), in = j % a.page_size;
-        there = have && page >= 0 && page < a.n_pages;             // (a page that does not exist reads as zeros)
-        kp += page * a.page_k + in * a.ld_k; vp += page * a.page_v + in * a.ld_v;
-      }
-      uint4 kw = make_uint4(0, 0, 0, 0), vw = kw;
-      if (there) { kw = *reinterpret_cast<const uint4*>(kp); vw = *reinterpret_cast<const uint4*>(vp); }
-      unpack8(kw, y);
+    for (int j0 = c0; j0 < c0 + bn; j0 += 32) {
+      const int j = j0 + lane;
+      const bool sees = j < seen.hi && (j >= seen.lo || j < w.prefix);
+      const unsigned some = __ballot_sync(0xffffffffu, sees);
+      if (!some) continue;
+      SeqPlace place = {nullptr, nullptr};
+      if (sees) place = seq_place(a, w, j);
       float dot = 0.f;
+      if (place.k) {
+#pragma unroll 8
+        for (int x = 0; x < a.hd; x += 8) {
+          float f[8], g[8];
+          unpack8(*reinterpret_cast<const uint4*>(q + x), f);
+          unpack8(*reinterpret_cast<const uint4*>(place.k + x), g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) dot = fmaf(x[i], y[i], dot);
-      const float sc = seq_score(a, warp_sum(dot), slope, (float)(p - j));
-      const float m = fmaxf(r.m, sc), keep = r.m == -INFINITY ? 0.f : exp2_fast(r.m - m), e = m == -INFINITY && sc == sc ? 0.f : exp2_fast(sc - m);
-      unpack8(vw, y);
-      r.l = fmaf(r.l, keep, e);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r.acc[i] = fmaf(r.acc[i], keep, e * y[i]);
+          for (int i = 0; i < 8; ++i) dot = fmaf(f[i], g[i], dot);
+        }
+      }
+      const float sc = sees ? seq_score(a, dot, slope, (float)(p - j)) : -INFINITY;
+      const float m = fmaxf(warp_max(sc), r.m), keep = r.m == -INFINITY ? 0.f : exp2_fast(r.m - m), e = sc == -INFINITY ? 0.f : exp2_fast(sc - m);
       r.m = m;
+      r.l = fmaf(r.l, keep, warp_sum(e));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.acc[i] *= keep;
+      const unsigned long long v = reinterpret_cast<unsigned long long>(place.v);
+#pragma unroll 1
+      for (int s0 = at; s0 < 32 + at; s0 += AHEAD * side) {
+        float f[AHEAD];
+        uint4 x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          const int s = s0 + u * side;
+          f[u] = __shfl_sync(0xffffffffu, e, s & 31);
+          const unsigned short* const row = reinterpret_cast<const unsigned short*>(__shfl_sync(0xffffffffu, v, s & 31));
+          x[u] = make_uint4(0, 0, 0, 0);
+          if (at < side && s < 32 && (some >> s & 1u) && row) x[u] = *reinterpret_cast<const uint4*>(row + d0);
+          else f[u] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          float y[8];
+          unpack8(x[u], y);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) r.acc[i] = fmaf(f[u], y[i], r.acc[i]);
+        }
+      }
     }
+    unsigned nan = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) nan |= r.acc[i] != r.acc[i] ? 1u << i : 0u;
+    for (int k = 0, all = nan; k < side; ++k) nan |= __shfl_sync(0xffffffffu, all, (lane + k * per) & 31);
+    if (__all_sync(0xffffffffu, (open & ~nan) == 0)) return false;
+    if (b % 8 == 0) seq_at_work(c);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float sum = r.acc[i];
+    for (int k = 1; k < side; ++k) sum += __shfl_sync(0xffffffffu, r.acc[i], (lane + k * per) & 31);
+    r.acc[i] = sum;                            // (of the lanes below `per`)
+  }
+  return true;
+}
+// The rows of the lanes `again`, which have been stored already: to `out`, or to `part` (this lane's row of it) relative to the maximum m_run.
+__device__ __forceinline__ void seq_rows_again(const SeqArgs& a, const SeqItem& w, int bn, const SeqWaits& c, unsigned again, int token, int head, int lo, int hi, float m_run, float* part) {
+  const int d0 = 8 * (threadIdx.x & 31);
+  SeqNan n;
+  seq_nan_keys(a, w, bn, c, n);
+  __syncwarp();                                // (a row was stored by its lane and is read by all)
+  while (again) {
+    const int src = __ffs(again) - 1;
+    again &= again - 1;
     seq_at_work(c);
+    const int r_token = __shfl_sync(0xffffffffu, token, src), r_head = __shfl_sync(0xffffffffu, head, src);
+    const SeqSeen seen = {__shfl_sync(0xffffffffu, lo, src), __shfl_sync(0xffffffffu, hi, src)};
+    const float r_m = __shfl_sync(0xffffffffu, m_run, src);
+    float* const r_part = reinterpret_cast<float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(part), src));
+    unsigned short* const out = a.out + (int64_t)(w.q0 + r_token) * a.ld_out + r_head * a.hd + d0;
+    unsigned open = 0;
+    if (d0 < a.hd) {
+      float y[8];
+      if (r_part) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = r_part[d0 + i];
+      } else {
+        unpack8(*reinterpret_cast<const uint4*>(out), y);
+      }
+      auto sees = [&](int j) { return j < seen.hi && (j >= seen.lo || j < w.prefix); };
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (y[i] != y[i] && !(n.last[i] >= 0 && (sees(n.first[i]) || sees(n.last[i])))) open |= 1u << i;
+    }
+    if (!__any_sync(0xffffffffu, open != 0)) continue;
+    SeqRow r;
+    if (!seq_row_alone(a, w, bn, c, r_token, r_head, seen, open, r)) continue;
+    const float by = r_part ? (r.m == -INFINITY ? 0.f : exp2_fast(r.m - r_m)) : (r.l != 0.f ? 1.0f / r.l : (seen.hi > 0 ? NAN : 0.f));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (open >> i & 1u) {
+        if (r_part) r_part[d0 + i] = r.acc[i] * by;
+        else out[i] = (unsigned short)(pack_bf16(r.acc[i] * by, 0.f) & 0xFFFFu);
+      }
   }
 }
 
@@ -392,11 +520,6 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t* v) {      
 __device__ __forceinline__ uint32_t seq_mask_word(int hi, int lo, int prefix, int w) {
   auto below = [w](int n) { const int k = min(max(n - 32 * w, 0), 32); return k == 32 ? 0xFFFFFFFFu : (1u << k) - 1u; };
   return below(hi) & (~below(lo) | below(prefix));
-}
-// Eight or sixteen columns of a finished row.
-__device__ __forceinline__ void seq_put(unsigned short* o, const float* v, int cols) {
-  *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-  if (cols >= 16) *reinterpret_cast<uint4*>(o + 8) = make_uint4(pack_bf16(v[8], v[9]), pack_bf16(v[10], v[11]), pack_bf16(v[12], v[13]), pack_bf16(v[14], v[15]));
 }
 // Part `which` (1: of the item that the share begins and does not end, 0: of the one that began before) of a share: rows of seq_row_floats, the row's
 // maximum (log2 units) and sum behind its columns.
@@ -825,31 +948,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       if (!whole && valid) *reinterpret_cast<float2*>(part_row + hdc) = make_float2(m_run, l_run);
       tc_fence_before();
       arrive_warp(o_free + 8u * (TWO ? t : 0), lane);
-      // Those rows once more, from the keys they see alone.
-      while (again) {
-        const int src = __ffs(again) - 1;
-        again &= again - 1;
-        const int r_token = __shfl_sync(0xffffffffu, token, src), r_head = __shfl_sync(0xffffffffu, head, src), r_at = __shfl_sync(0xffffffffu, at, src);
-        const float r_m = __shfl_sync(0xffffffffu, m_run, src);
-        const bool r_sees = __shfl_sync(0xffffffffu, seen.hi, src) > 0;
-        SeqRow r;
-        seq_row_alone(a, w, BN, r_token, r_head, c, r);
-        if (8 * lane < a.hd) {
-          if (whole) {
-            const float i_ = r.l != 0.f ? 1.0f / r.l : (r_sees ? NAN : 0.f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r.acc[j] *= i_;
-            seq_put(a.out + (int64_t)(w.q0 + r_token) * a.ld_out + r_head * a.hd + 8 * lane, r.acc, 8);
-          } else {                             // (relative to the maximum that the row's sum, which is as it was, is relative to)
-            const float as = r.m == -INFINITY ? 0.f : exp2_fast(r.m - r_m);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r.acc[j] *= as;
-            float4* const x = reinterpret_cast<float4*>(part + r_at * seq_row_floats(a.hd) + 8 * lane);
-            x[0] = make_float4(r.acc[0], r.acc[1], r.acc[2], r.acc[3]);
-            x[1] = make_float4(r.acc[4], r.acc[5], r.acc[6], r.acc[7]);
-          }
-        }
-      }
+      if (again) seq_rows_again(a, w, BN, c, again, token, head, seen.lo, seen.hi, m_run, whole ? nullptr : part_row);
     }
   }
   __syncthreads();
