@@ -1009,8 +1009,8 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
       m = top;
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const float f = ml[u].x == -INFINITY ? (ml[u].y == 0.f ? 0.f : ml[u].y) : exp2_fast(ml[u].x - top);      // (no maximum: no keys, or scores that are all NaN)
-        if (f == 0.f) continue;                // (a part without keys of this row: whatever lies there)
+        if (ml[u].x == -INFINITY && ml[u].y == 0.f) continue;      // (a part without keys of this row: whatever lies there)
+        const float f = ml[u].x == -INFINITY ? ml[u].y : exp2_fast(ml[u].x - top);      // (no maximum: scores that are all NaN.  0 where the part weighs nothing: times NaN it is NaN all the same)
         l = fmaf(f, ml[u].y, l);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
@@ -1034,8 +1034,8 @@ __global__ void __launch_bounds__(SEQ_JOIN_THREADS) vla_op_sequences_join_kernel
       for (int j = 0; j < COLS; ++j) acc[j] = 0.f;
 #pragma unroll
       for (int i = 0; i < SEQ_JOIN_WARPS; ++i) {
-        const float x = met_s[i][COLS][lane], y = met_s[i][COLS + 1][lane], f = x == -INFINITY ? (y == 0.f ? 0.f : y) : exp2_fast(x - top);
-        if (f == 0.f) continue;
+        const float x = met_s[i][COLS][lane], y = met_s[i][COLS + 1][lane], f = x == -INFINITY ? y : exp2_fast(x - top);
+        if (x == -INFINITY && y == 0.f) continue;
         l = fmaf(f, y, l);
 #pragma unroll
         for (int j = 0; j < COLS; ++j) acc[j] = fmaf(f, met_s[i][j][lane], acc[j]);

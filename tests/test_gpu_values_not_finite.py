@@ -125,3 +125,17 @@ def test_a_value_that_rows_see_costs_a_look_at_the_values(hq, hkv, hd, value, ev
                 best = min(best, a.elapsed_time(b))
             took.append(best)
         assert took[1] < 40 * took[0], took
+
+
+@pytest.mark.parametrize("new,keys", [(1, 700), (1, 3000), (1, 20000), (40, 3000), (600, 6000)])
+@pytest.mark.parametrize("hq,hkv,hd", [(8, 2, 64), (4, 1, 256)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_a_key_without_any_weight_is_seen_all_the_same(new, keys, hq, hkv, hd, value):
+    """Its probability underflows, and 0 times a value that is not finite is NaN, whichever part of the keys it lies in."""
+    import torch
+    q, k, v = make(new, hq, hkv, hd, seed=5, keys=keys)
+    q[:, 0::hd], k[:, 0::hd] = 1.0, -400.0
+    k[:keys // 5, 0::hd] = 400.0
+    v[keys - 3, 5] = value
+    got = run(q, k, v, [0, new], hq, hkv, hd, ends_k=[0, keys], scale=1.0).view(new, hq, hd)[:, :hq // hkv]
+    assert not bool(got[:, :, 5].isfinite().any()) and bool(got[:, :, :5].isfinite().all()) and bool(got[:, :, 6:].isfinite().all())
