@@ -348,7 +348,8 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
  * A call's rows x keys are limited: (tq / 128 * hq / hkv + seqs) x tk / 64 stays below 2^31, about (a cache: max_pages * page_size for tk).
  * out overlaps no input and scratch neither.  scratch: DEVICE, 256-byte aligned, vla_op_attention_sequences_scratch_bytes(hd) or more; its first word is the call's
  * error word, its contents matter to nobody afterwards, and calls that share it must not overlap on the GPU (two captured graphs among them).  It may be
- * NULL where a sequence has at most 512 keys (tk, or max_pages * page_size): such calls need none, and share an error word per device (VLA_OP_ATTENTION_SHORT). */
+ * NULL where a sequence has at most 512 keys (tk, or max_pages * page_size): such calls need none, and share an error word per device (VLA_OP_ATTENTION_SHORT), as do those whose
+ * status says so: for scratch that does not outlive the call. */
 int vla_op_attention_sequences_scratch_bytes(int32_t hd, size_t* out_bytes);
 typedef struct vla_attention_args {
   const void *q, *k, *v;                     /* k, v: rows of the packed sequences, or k_cache and v_cache */
@@ -365,7 +366,7 @@ typedef struct vla_attention_args {
   int32_t n_pages, page_size, max_pages;     /* paged */
   int32_t hq, hkv, hd, causal, window;
   float scale, cap;
-  int32_t reserved;                          /* 0 */
+  int32_t status;                            /* whose error word the call uses: 0, as above; VLA_OP_ATTENTION_SHORT, that one though there is scratch */
 } vla_attention_args;
 int vla_op_attention_packed(const vla_attention_args* args, void* stream);
 
@@ -395,7 +396,7 @@ int vla_op_cache_store(const vla_cache_store_args* args, void* stream);
  * (the word at the start of `scratch`, DEVICE), VLA_OP_ATTENTION_STATIC (the library's fixed array), or VLA_OP_LINEAR_SCALED,
  * VLA_OP_LINEAR_GROUPED, VLA_OP_LINEAR_GROUPED_SCALED and VLA_OP_LINEAR_BIAS (a word per device each, as for VLA_OP_LINEAR; vla_op_quantize and
  * vla_op_qk_norm_rope wait for nothing, nor does vla_op_cache_store), or VLA_OP_ATTENTION_PACKED and VLA_OP_ATTENTION_PAGED (the word at the start
- * of `scratch`), or VLA_OP_ATTENTION_SHORT (those two's calls with scratch NULL: a word per device). */
+ * of `scratch`), or VLA_OP_ATTENTION_SHORT (those two's calls with scratch NULL, or with that as their status: a word per device). */
 enum { VLA_OP_LINEAR = 0, VLA_OP_ATTENTION = 1, VLA_OP_ATTENTION_STATIC = 2, VLA_OP_LINEAR_SCALED = 3, VLA_OP_LINEAR_GROUPED = 4,
        VLA_OP_LINEAR_GROUPED_SCALED = 5, VLA_OP_LINEAR_BIAS = 6, VLA_OP_ATTENTION_PACKED = 7, VLA_OP_ATTENTION_PAGED = 8, VLA_OP_ATTENTION_SHORT = 9 };
 int vla_op_status(int32_t op, const void* scratch, void* stream);

@@ -742,7 +742,7 @@ def _row_step(name, what, x, rows, width):
 
 def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream):
     """What the two attentions below have in common, ``keys`` being the most that a sequence may have: (tq, ld_q, out, ld_out, scratch, its pointer and bytes, pointers of
-    prefix and slopes, scale)."""
+    prefix and slopes, scale, whose status word)."""
     if q.dim() != 2 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8:
         _refuse(name, "q is a matrix; hd a multiple of 8, at most 256")
     tq, width = q.shape[0], hq * hd
@@ -762,9 +762,10 @@ def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, 
         out, ld_out = _empty_like(q) if stream is None else _new(stream, (tq, width), _bf16, q), width      # (contiguous, whatever lies between q's rows)
     else:
         ld_out = _row_step(name, "out is bf16 [tq, hq*hd]", out, tq, width)
+    status = 0
     if scratch is None:
-        size = at = 0
-        if keys > 512:                                              # (shorter calls need none; goes back to its stream's memory when the call returns)
+        size, at, status = 0, 0, OP_ATTENTION_SHORT
+        if keys > 512:                                              # (shorter calls need none; goes back to its stream's memory when the call returns, so the status lies elsewhere)
             size = _scratch_sizes.get(hd)
             if size is None:
                 size = _scratch_sizes[hd] = op_attention_sequences_scratch_bytes(hd)
@@ -774,7 +775,7 @@ def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, 
         _refuse(name, "scratch is contiguous uint8")
     else:
         size, at = scratch.numel(), scratch.data_ptr()
-    return tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, hd ** -0.5 if scale is None else scale
+    return tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, hd ** -0.5 if scale is None else scale, status
 
 
 _scratch_sizes = {}
@@ -794,7 +795,7 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
     name = "op_attention_packed"
     seqs = _offsets(name, offsets, (q, k, v, offsets_k, prefix, slopes, out, scratch))
     tk = k.shape[0]
-    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, tk, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
+    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status = _sequences(name, q, seqs, tk, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     if offsets_k is None:
         offsets_k = offsets
         if tk != tq:
@@ -805,7 +806,7 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
         _refuse(name, "k and v have at least one row, below 2^31 of them")
     ld_k, ld_v = _row_step(name, "k is bf16 [tk, hkv*hd]", k, tk, hkv * hd), _row_step(name, "v is bf16 [tk, hkv*hd]", v, tk, hkv * hd)
     args = _ATTENTION_ARGS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ld_q, ld_k, ld_v, ld_out, 0, 0, offsets.data_ptr(), offsets_k.data_ptr(), 0, 0,
-                                p_prefix, p_slopes, at, size, seqs, tq, tk, 0, 0, 0, hq, hkv, hd, 1 if causal else 0, window, scale, cap, 0)
+                                p_prefix, p_slopes, at, size, seqs, tq, tk, 0, 0, 0, hq, hkv, hd, 1 if causal else 0, window, scale, cap, status)
     rc = (_lib or load_library()).vla_op_attention_packed(args, _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_attention_packed failed")
@@ -843,10 +844,10 @@ def op_attention_paged(q, k_cache, v_cache, pages, lengths, offsets, hq, hkv, hd
     name = "op_attention_paged"
     seqs = _offsets(name, offsets, (q, k_cache, v_cache, pages, lengths, prefix, slopes, out, scratch))
     n, page, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, hkv * hd)
-    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale = _sequences(name, q, seqs, most * page, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
+    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status = _sequences(name, q, seqs, most * page, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
     args = _ATTENTION_ARGS.pack(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), ld_q, row_k, row_v, ld_out, page_k, page_v, offsets.data_ptr(), 0,
                                 lengths.data_ptr(), pages.data_ptr(), p_prefix, p_slopes, at, size, seqs, tq, 0, n, page, most, hq, hkv, hd, 1 if causal else 0,
-                                window, scale, cap, 0)
+                                window, scale, cap, status)
     rc = (_lib or load_library()).vla_op_attention_paged(args, _stream_ptr(stream))
     if rc != VLA_OK:
         raise VlaError(rc, "vla_op_attention_paged failed")
@@ -875,8 +876,8 @@ def op_cache_store(k, v, k_cache, v_cache, pages, lengths, offsets, stream=None)
 
 def op_status(op, scratch=None, stream=None) -> int:
     """Waits for ``stream`` (None: torch's current one) and returns the operator's status word as a VLA_* code (VLA_OK or VLA_ERR_TIMEOUT).
-    Operators with ``scratch`` have it there: pass the same.  OP_ATTENTION_SHORT: of calls of ``op_attention_packed`` and ``op_attention_paged`` that need none (at most
-    512 keys a sequence) and were given none."""
+    Operators with ``scratch`` have it there: pass the same.  OP_ATTENTION_SHORT: of calls of ``op_attention_packed`` and ``op_attention_paged`` that were given
+    none (a word per device: ask before another such call is made)."""
     return load_library().vla_op_status(op, None if scratch is None else scratch.data_ptr(), _stream_ptr(stream))
 
 

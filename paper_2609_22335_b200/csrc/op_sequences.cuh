@@ -34,8 +34,8 @@ struct SeqArgs {
   const float* slopes;
   const unsigned short *q, *k, *v;             // (read key by key where a row's result is not finite)
   unsigned short* out;
-  char* scratch;                               // header (error word), records, parts; null where all items stay whole
-  unsigned* err;
+  char* scratch;                               // header, records, parts; null where all items stay whole
+  unsigned* err;                               // the header's first word, or the device's
   long long ld_q, ld_k, ld_v, page_k, page_v, ld_out;
   int seqs, tq, tk, n_pages, page_size, max_pages, chunk;      // chunk: rows of a box of keys, all of one page
   uint32_t page_magic, page_shift;             // x / page_size = x * page_magic >> page_shift for x below 2^31

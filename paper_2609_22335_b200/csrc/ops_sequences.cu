@@ -7,7 +7,7 @@
 namespace vla {
 
 // What the kernels need to know of a device, looked up on the first call made with it current.
-static __device__ __align__(256) unsigned g_sequences_error[16];      // of calls without scratch memory
+static __device__ __align__(256) unsigned g_sequences_error[16];      // of calls without scratch memory of the caller's own
 struct SeqDevice { int sms = 0; unsigned* error = nullptr; };
 static bool seq_look_up(int dev, SeqDevice* d) {
   void* e = nullptr;
@@ -50,7 +50,8 @@ static bool seq_cache_ok(int n_pages, int page_size, int max_pages) {
 // What both attentions ask of their arguments.
 static bool seq_shape_ok(const vla_attention_args& x) {
   if (x.seqs < 1 || x.seqs > 1 << 20 || x.tq < 1 || x.tq > 1 << 30 || x.hkv < 1 || x.hq < x.hkv || x.hq % x.hkv || x.hq > 65536 || x.hd < 8 || x.hd > 256 || x.hd % 8) return false;
-  if (!(x.scale > 0.f) || !(x.scale < 1e30f) || !(x.cap >= 0.f) || !(x.cap < 1e30f) || (x.cap > 0.f && !(x.scale / x.cap < 1e30f)) || x.window < 0 || (!x.causal && (x.window || x.prefix)) || x.reserved) return false;
+  if (!(x.scale > 0.f) || !(x.scale < 1e30f) || !(x.cap >= 0.f) || !(x.cap < 1e30f) || (x.cap > 0.f && !(x.scale / x.cap < 1e30f)) || x.window < 0 || (!x.causal && (x.window || x.prefix))) return false;
+  if (x.status != 0 && x.status != VLA_OP_ATTENTION_SHORT) return false;
   if (!seq_rows_ok(x.q, x.ld_q, (int64_t)x.hq * x.hd) || !seq_rows_ok(x.out, x.ld_out, (int64_t)x.hq * x.hd)) return false;
   if (!seq_rows_ok(x.k, x.ld_k, (int64_t)x.hkv * x.hd) || !seq_rows_ok(x.v, x.ld_v, (int64_t)x.hkv * x.hd)) return false;
   return x.offsets_q && op_aligned(4, {x.offsets_q, x.prefix, x.slopes});
@@ -81,7 +82,7 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   if (x.scratch ? (reinterpret_cast<uintptr_t>(x.scratch) & 255) || (int64_t)x.scratch_bytes < seq_scratch_bytes(a.hd) : !whole) return VLA_ERR_NOMEM;
   SeqDevice dev;
   if (!seq_device(&dev)) return VLA_ERR_CUDA;
-  a.err = x.scratch ? static_cast<unsigned*>(x.scratch) : dev.error;
+  a.err = x.scratch && x.status == 0 ? static_cast<unsigned*>(x.scratch) : dev.error;
   const int shares = seq_shares(mode, dev.sms);
   a.chunk = bn;
   if (!a.offsets_k)
@@ -112,7 +113,7 @@ static int seq_run(SeqArgs& a, const vla_attention_args& x, cudaStream_t s) {
   return op_launch_2d(mode == SEQ_WIDE ? vla_op_sequences_join_kernel<true> : vla_op_sequences_join_kernel<false>, shares, blocks, SEQ_JOIN_THREADS, s, a, mode);
 }
 
-// The error word of calls without scratch memory on the current device, or null.
+// The error word of calls without scratch memory of the caller's own on the current device, or null.
 unsigned* sequences_error_word() {
   SeqDevice dev;
   return seq_device(&dev) ? dev.error : nullptr;
