@@ -721,7 +721,7 @@ def _offsets(name, offsets, others):
     if _bf16 is None:
         _look_up_types()
     shape, dev = offsets.shape, offsets.get_device()
-    bad = len(shape) != 1 or shape[0] < 2 or offsets.dtype != _i32 or not offsets.is_contiguous() or dev < 0 or dev != _device_now()
+    bad = len(shape) != 1 or shape[0] < 2 or shape[0] >> 31 or offsets.dtype != _i32 or not offsets.is_contiguous() or dev < 0 or dev != _device_now()
     for t in others:
         if t is not None and t.get_device() != dev:
             bad = True
@@ -740,7 +740,7 @@ def _row_step(name, what, x, rows, width):
     return ld if rows > 1 else width                                # (the stride of one row says nothing)
 
 
-def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream):
+def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, cap, slopes, scale, out, scratch, stream):
     """What the two attentions below have in common, ``keys`` being the most that a sequence may have: (tq, ld_q, out, ld_out, scratch, its pointer and bytes, pointers of
     prefix and slopes, scale, whose status word)."""
     if q.dim() != 2 or hq < 1 or hkv < 1 or hd < 8 or hd > 256 or hd % 8:
@@ -748,6 +748,10 @@ def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, 
     tq, width = q.shape[0], hq * hd
     if tq < 1 or (tq | width | hkv * hd) >> 31 or window >> 31:
         _refuse(name, "at least one row, below 2^31 of them, window a number from 0 to 2^31 - 1")
+    if scale is None:
+        scale = hd ** -0.5
+    if not (0.0 <= cap < 1e30 and 0.0 < scale < 1e30):
+        _refuse(name, "cap a number from 0, scale one above 0, both below 1e30")
     ld_q = _row_step(name, "q is bf16 [tq, hq*hd]", q, tq, width)
     p_prefix = p_slopes = 0
     if prefix is not None:
@@ -775,7 +779,7 @@ def _sequences(name, q, seqs, keys, hq, hkv, hd, prefix, window, slopes, scale, 
         _refuse(name, "scratch is contiguous uint8")
     else:
         size, at = scratch.numel(), scratch.data_ptr()
-    return tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, hd ** -0.5 if scale is None else scale, status
+    return tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status
 
 
 _scratch_sizes = {}
@@ -795,7 +799,7 @@ def op_attention_packed(q, k, v, offsets, hq, hkv, hd, offsets_k=None, causal=Fa
     name = "op_attention_packed"
     seqs = _offsets(name, offsets, (q, k, v, offsets_k, prefix, slopes, out, scratch))
     tk = k.shape[0]
-    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status = _sequences(name, q, seqs, tk, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
+    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status = _sequences(name, q, seqs, tk, hq, hkv, hd, prefix, window, cap, slopes, scale, out, scratch, stream)
     if offsets_k is None:
         offsets_k = offsets
         if tk != tq:
@@ -844,7 +848,7 @@ def op_attention_paged(q, k_cache, v_cache, pages, lengths, offsets, hq, hkv, hd
     name = "op_attention_paged"
     seqs = _offsets(name, offsets, (q, k_cache, v_cache, pages, lengths, prefix, slopes, out, scratch))
     n, page, most, row_k, page_k, row_v, page_v = _cache(name, k_cache, v_cache, pages, lengths, seqs, hkv * hd)
-    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status = _sequences(name, q, seqs, most * page, hq, hkv, hd, prefix, window, slopes, scale, out, scratch, stream)
+    tq, ld_q, out, ld_out, scratch, at, size, p_prefix, p_slopes, scale, status = _sequences(name, q, seqs, most * page, hq, hkv, hd, prefix, window, cap, slopes, scale, out, scratch, stream)
     args = _ATTENTION_ARGS.pack(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), ld_q, row_k, row_v, ld_out, page_k, page_v, offsets.data_ptr(), 0,
                                 lengths.data_ptr(), pages.data_ptr(), p_prefix, p_slopes, at, size, seqs, tq, 0, n, page, most, hq, hkv, hd, 1 if causal else 0,
                                 window, scale, cap, status)
