@@ -377,7 +377,7 @@ int vla_op_attention_packed(const vla_attention_args* args, void* stream);
 int vla_op_attention_paged(const vla_attention_args* args, void* stream);
 
 /* New rows of such a cache: rows offsets[s] <= i < offsets[s + 1] of k and v [t, width] (width = hkv*hd, a multiple of 8) become tokens lengths[s] -
- * (offsets[s + 1] - i) of sequence s.  lengths count the new tokens.  A row whose token is below 0 or behind the table, or on a page that does
+ * (offsets[s + 1] - i) of sequence s; offsets ascend, and what lies outside of 0 .. t counts as the nearer end.  lengths count the new tokens.  A row whose token is below 0 or behind the table, or on a page that does
  * not exist, is not written; two rows for one place are the caller's mistake.  Any page_size.  Strides and alignment as above. */
 typedef struct vla_cache_store_args {
   const void *k, *v;

@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(STORE_THREADS) vla_op_cache_store_kernel(const
     if (found) { s = at + __ffs(found) - 1; break; }
   }
   if (s >= g.seqs || __ldcg(g.offsets + s) > token) return;
-  const long long pos = (long long)__ldcg(g.lengths + s) - __ldcg(g.offsets + s + 1) + token;
+  const long long pos = (long long)__ldcg(g.lengths + s) - min(__ldcg(g.offsets + s + 1), g.t) + token;      // (ends behind the rows count as the last row's, as for the attention)
   if (pos < 0 || pos >= (long long)g.max_pages * g.page_size) return;
   const int slot = (int)(pos / g.page_size), page = __ldcg(g.pages + (long long)s * g.max_pages + slot), in = (int)(pos - (long long)slot * g.page_size);
   if (page < 0 || page >= g.n_pages) return;
