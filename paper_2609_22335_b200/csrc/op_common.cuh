@@ -80,7 +80,9 @@ __device__ __forceinline__ bool mbar_wait(const OpWaits& c, uint32_t bar, uint32
 // nothing of global memory is touched before op_wait_previous has returned, that is before all earlier work on the stream is
 // complete and visible.  op_let_next_start lets the next call's kernel do the same.  It takes effect once every block of this
 // grid has come to it, and stands behind the block's tensor-memory allocation: a block that waits for this grid can then
-// neither keep one of its blocks out nor hold columns that one of them still needs.  Back to back: linear 50x2048x720
+// neither keep one of its blocks out nor hold columns that one of them still needs.  The kernel in front may thus write an
+// operand while this one already runs, so operands are read by plain loads, not as memory that is constant for the kernel's
+// lifetime (__ldg).  Back to back: linear 50x2048x720
 // 8.2 -> 6.1 us, 288x11008x4096 45.9 -> 43.9, attention 1024x1024 (12 heads of 64) 16.4 -> 14.5.
 __device__ __forceinline__ void op_wait_previous(const OpMaps& maps, int n) {
   if ((int)threadIdx.x < n) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[threadIdx.x]) : "memory");

@@ -162,10 +162,10 @@ __device__ __forceinline__ void bias_load(const LinearArgs& g, float* b, int f, 
   for (int i = 0; i < 4; ++i) {
     const int c = f + 8 * i + 2 * q;
     if (VEC >= 2) {
-      const float2 v = __ldg(reinterpret_cast<const float2*>(g.bias + min(c, g.n - 2)));
+      const float2 v = *reinterpret_cast<const float2*>(g.bias + min(c, g.n - 2));
       b[2 * i] = v.x; b[2 * i + 1] = v.y;
     } else {
-      b[2 * i] = __ldg(g.bias + min(c, g.n - 1)); b[2 * i + 1] = __ldg(g.bias + min(c + 1, g.n - 1));
+      b[2 * i] = g.bias[min(c, g.n - 1)]; b[2 * i + 1] = g.bias[min(c + 1, g.n - 1)];
     }
   }
 }

@@ -356,7 +356,7 @@ struct SeqRow { float m, l, acc[8]; };
 __device__ __forceinline__ bool seq_row_alone(const SeqArgs& a, const SeqItem& w, int bn, const SeqWaits& c, int token, int head, SeqSeen seen, unsigned open, SeqRow& r) {
   constexpr int AHEAD = 8;
   const int lane = threadIdx.x & 31, per = a.hd / 8, side = 32 / per, at = lane / per, d0 = (lane - at * per) * 8, p = w.nk - w.nq + token;
-  const float slope = a.slopes ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
+  const float slope = a.slopes ? a.slopes[head] * 1.44269504f : 0.f;
   const unsigned short* const q = a.q + (w.q0 + token) * a.ld_q + head * a.hd;
   r.m = -INFINITY; r.l = 0.f;
 #pragma unroll
@@ -788,7 +788,7 @@ __global__ void __launch_bounds__(seq_threads(MODE), MODE == SEQ_ONE ? 2 : 1) vl
       const int p = w.nk - w.nq + token;
       SeqSeen seen = seq_seen(p, w.nk, w.prefix, a.causal, a.window);
       if (!valid) { seen.hi = INT_MAX / 2; seen.lo = 0; }              // (nobody stores it: nothing to mask)
-      const float slope = EXTRA && a.slopes && valid ? __ldg(a.slopes + head) * 1.44269504f : 0.f;
+      const float slope = EXTRA && a.slopes && valid ? a.slopes[head] * 1.44269504f : 0.f;
       float m_run = -INFINITY, l_run = 0.f;
       ring0 += 2u * (uint32_t)n;               // (from here on the place behind the item's last)
       if (ring0 >= 2u * (uint32_t)NS) ring0 = n < NS ? ring0 - 2u * (uint32_t)NS : ring0 % (2u * (uint32_t)NS);
