@@ -341,10 +341,13 @@ int vla_op_qk_norm_rope(const void* q, const void* k, int32_t in_f32, int64_t ld
  * [tk, hkv*hd] (the two may be the same array), nq and nk of them, and attends within itself.  Its row i is at position p = nk - nq + i: the rows are the
  * last of its tokens.  causal: row i sees keys j <= p, with window > 0 those with p - j < window, and of every row's keys the first prefix[s] (prefix NULL: none).
  * Not causal: all nk, and neither prefix nor window.  A row that sees no key becomes zeros.
- * bf16, rows ld_* elements apart, 16-byte aligned, rows too; hd a multiple of 8, at most 256; hq a multiple of hkv; scale > 0; cap 0, or such that scale / cap < 1e30 (tanh is good to
+ * bf16, rows ld_* elements apart, 16-byte aligned, rows too; hd a multiple of 8, at most 256; hq a multiple of hkv; 0 < scale < 1e30; cap 0, or below 1e30 and such that scale / cap < 1e30 (tanh is good to
  * 2^-21, so capped scores to 2^-21 of the cap).  offsets_q,
- * offsets_k int32 [seqs + 1], prefix int32 [seqs], slopes fp32 [hq], all DEVICE and read by the kernel.  Offsets ascend; what lies outside of 0 .. tq (tk)
- * counts as the nearer end.  Rows of no sequence are not written.  Keys that a row does not see have no part in it, whatever their values.
+ * offsets_k int32 [seqs + 1], prefix int32 [seqs], slopes fp32 [hq] (below 2e38), all DEVICE and read by the kernel.  Offsets ascend; what lies outside of 0 .. tq (tk)
+ * counts as the nearer end.  Rows of no sequence are not written.  Keys that a row does not see have no part in it, whatever their values (a NaN or infinity among the
+ * values of keys that some of 128 or 256 neighbouring rows see and others do not makes these rows slow, though: they are worked out again on the side).
+ * Scores, maxima and sums are in 32 bits.  For the product with V a probability is rounded to bf16 (by 2^-8 of it at most); calls of tq * hq <= 1024 carry what that leaves in a
+ * second bf16 number.
  * A call's rows x keys are limited: (tq / 128 * hq / hkv + seqs) x tk / 64 stays below 2^31, about (a cache: max_pages * page_size for tk).
  * out overlaps no input and scratch neither.  scratch: DEVICE, 256-byte aligned, vla_op_attention_sequences_scratch_bytes(hd) or more; its first word is the call's
  * error word, its contents matter to nobody afterwards, and calls that share it must not overlap on the GPU (two captured graphs among them).  It may be

@@ -16,9 +16,11 @@
 // tiles S0(0) S1(0), then for each block PV0 S0(next) PV1 S1(next), else S(0) S(1), then PV(i) S(i + 2): while one softmax works, the tensor core has
 // the other's products.  S of a later block is issued behind the P V that reads the probabilities in the same columns; MMAs run in the order of issue.
 //
-// Measured: 8192 tokens both ways, 16 heads of 128, 472 us (1.16 PFLOP/s), of 64 417 us (0.66), 8 over 1 of 256 525 us (1.05); causal 264, 236 and 285 us.  Bound by the chain of a block:
-// with two tiles 3850 cycles at heads of 128, of which the products take 1370 from the probabilities to the next scores, the maximum 460, the exponentials 1600.  64 single tokens over
-// 1650 to 8192 keys, 32 heads over 8 of 128, 222 to 237 us: 5.4 to 5.8 TB/s.  A call's first scores come 4 us after its start.
+// Measured: 8192 tokens both ways, 16 heads of 128, 467 us (1.18 PFLOP/s), of 64 414 us (0.66), 8 over 1 of 256 470 us (1.17); causal 263, 235 and 265 us.  Bound by the chain of a block:
+// with two tiles 4000 cycles at heads of 128 and 3400 of 64, of which the tensor core works 2048 and 1024 and the special-function unit 2048 (an exponential a score); a cap adds 1600 to 2500
+// cycles, scores beyond half of it as much as 3700 more.  64 single tokens over 1650 to 8192 keys, 32 heads over 8 of 128, 212 to 237 us: 5.4 to 6.1 TB/s.  A call's first scores come
+// 4 us after its start, later where there are many sequences: a share's start reads offsets and lengths 32 sequences at a time, twice, and steps over those without rows one by one (ten
+// single tokens over 1000 keys in 10, 64, 256 and 1024 places 17.8, 18.6, 27.6 and 69 us).
 #pragma once
 #include "op_common.cuh"
 #include "sequences_plan.h"
@@ -32,7 +34,7 @@ struct SeqArgs {
   const int *lengths, *pages;                  // keys of each sequence, [seqs, max_pages]
   const int* prefix;
   const float* slopes;
-  const unsigned short *q, *k, *v;             // (read key by key where a row's result is not finite)
+  const unsigned short *q, *k, *v;             // (read by plain loads where a row's result is not finite)
   unsigned short* out;
   char* scratch;                               // header, records, parts; null where all items stay whole
   unsigned* err;                               // the header's first word, or the device's

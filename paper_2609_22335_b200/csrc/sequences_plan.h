@@ -93,9 +93,9 @@ inline void seq_divisor(int d, uint32_t* magic, uint32_t* shift) {
   *shift = 31 + l;
 }
 
-// bf16 numbers that a probability is given in for the second product.  One puts an error beside the result's own rounding that is as large, on average over many rows: 1.41 times the
-// rounding in all.  Of few rows (tokens x heads) it may be more, 1.6 times over 8 rows of which each has a few keys that count; such calls are bound by latency and take two numbers:
-// 1.00 to 1.02 times, at 12.4 us as before (one token, 1500 keys).  64 tokens of 32 heads over 1.3 GB of cache would take 280 us for 231, in the long run of a card at its power limit.
+// bf16 numbers that a probability is given in for the second product.  One puts an error beside the result's own rounding that is about as large (relative 2-norm against 64 bits 2.3e-3
+// for 1.65e-3), two put none (1.00 to 1.02 times the rounding).  Where a call has few rows (tokens x heads) it is bound by latency, and the second number is free: 12.4 us as before
+// (one token, 1500 keys).  Elsewhere it has a price, 280 us for 231 with 64 tokens of 32 heads over 1.3 GB of cache.  So a row's precision is a matter of its call's size.
 inline int seq_terms(int64_t tq, int hq) { return tq * hq <= 1024 ? 2 : 1; }
 // Shapes of the kernel.  Two: two tiles of 128 rows that share their blocks of 128 keys, an SM to a CTA (long sequences).  One: a tile, blocks of 64 keys, two
 // CTAs an SM.  Wide: the same for heads wider than 128, an SM to a CTA.
@@ -107,7 +107,8 @@ inline int seq_mode(int64_t tq, int seqs, int hq, int fold, int hd) {
   return tq * fold > (int64_t)seqs * 900 && seq_terms(tq, hq) == 1 ? SEQ_TWO : SEQ_ONE;
 }
 SEQ_HD int seq_bn(int mode) { return mode == SEQ_TWO ? 128 : 64; }
-// What an item takes beside its blocks, in blocks: its first scores, the last block's chain, the result (6000 cycles beside 3250 to 3850 a block with two tiles, 3200 beside 1100).
+// What an item takes beside its blocks, in blocks: its first scores, the last block's chain, the result.  (Cycles, from the times of calls of two to eight items a CTA of four and eight
+// blocks each: 3700 and 5900 beside 3400 and 4000 a block with two tiles, heads of 64 and 128; 4400 and 7000 beside 1900 and 2650 with two CTAs an SM; 10400 beside 2650 of heads of 256.)
 SEQ_HD constexpr int seq_item_ticks(int mode) { return mode == SEQ_TWO ? 2 : 3; }
 SEQ_HD constexpr int seq_join_ticks(int mode) { return mode == SEQ_TWO ? 5 : 9; }
 SEQ_HD int seq_item_rows(int mode) { return mode == SEQ_TWO ? 2 * SEQ_ROWS : SEQ_ROWS; }
