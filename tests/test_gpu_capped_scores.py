@@ -104,3 +104,24 @@ def test_scores_below_zero_are_as_good_as_those_above(n, hd):
     k[:, 0], k[1, 1], v[1] = 1, 2.0 ** -19, 1
     up, down = (run(q, s * k, w, [0, n], 1, 1, hd, ends_k=[0, 2], scale=cap, cap=cap) for s, w in ((1, v), (-1, 1 - v)))
     assert bool(((up > 0.5) & (up < 0.999)).any()) and torch.equal(up, down)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("hd", [8, 256])
+def test_a_capped_score_is_off_by_what_is_stated(sign, hd):
+    """One capped score beside one that is 0, with a bias by distance that makes up for it, so that the weight tells the score to a fraction of the cap's last places.  Units of 2^-23 of
+    the cap: tanh 2.2, the bias' and the score's roundings 0.5 each, half a step of a result between 0.1 and 0.9 0.4 -- below 4, which the header promises, in all."""
+    import torch
+    from paper_2609_22335_b200 import api
+    cap, heads = 2.0 ** 20, 512
+    for seed in range(8):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x = (sign * cap * (0.02 + 3.5 * torch.rand(heads, device="cuda", generator=g))).bfloat16()
+        exact = cap * torch.tanh(x.double() / cap)
+        slopes = (exact - (2 * torch.rand(heads, device="cuda", generator=g) - 1)).float()
+        q, k, v = (torch.zeros(n, hd, dtype=torch.bfloat16, device="cuda") for n in (heads, 2, 2))
+        q[:, 0], k[0, 0], v[0] = x, 1, 1
+        y = api.op_attention_packed(q.view(1, -1), k, v, ints([0, 1]), heads, 1, hd, offsets_k=ints([0, 2]), scale=1.0, cap=cap, slopes=slopes).view(heads, hd)[:, 0].double()
+        assert bool(((y > 0.1) & (y < 0.9)).all())
+        off = (torch.log(y) - torch.log1p(-y) - (exact - slopes.double())).abs()
+        assert float(off.max()) <= 3.6 * 2.0 ** -23 * cap, float(off.max()) / cap * 2 ** 23
